@@ -358,6 +358,112 @@ fog_status fog_fp8_gemm(fog_layout layout, int64_t M, int64_t N, int64_t K,
 size_t fog_fp8_gemm_workspace(fog_layout layout, int64_t M, int64_t N, int64_t K);
 
 /*
+ * Casts with a scale for each block of 128 elements (Appendix E's cast with rho taken over a block instead of the tensor: an
+ * outlier costs the range of its own block only).  Blocks are
+ *     along the row:     128 consecutive columns of a row,        q_row with s_row[block of columns][row]
+ *     along the column:  128 consecutive rows of a column,        q_col with s_col[block of rows][column]
+ *     tiles:             128 rows x 128 columns,                  q with s[block of rows][block of columns]
+ * the last block of a row or column being shorter where 128 does not divide it.  A product contracts along its blocks: the row form of
+ * X and of dY serves the forward and the data gradient, their column form the weight gradient, and tiles serve either.
+ * The scale is a power of two: with a = max |x| over the block
+ *     k = floor(log2(FP8MAX / (2^margin a))), limited to -126 .. 126;  0 where a is zero or not finite
+ *     q = sat_rne_fmt( 2^k x )  (the product is exact),          scale byte = 127 - k:  x ~ q 2^(byte - 127).
+ *   x_bf16 : [rows, cols], leading dimension ldx.   margin : as in fog_scale.
+ *   q_row, q_col, q : [rows, cols] bytes, leading dimensions ldq_*.  fog_quantize_block wants q_row with s_row, q_col with s_col, or
+ *            both pairs (one pass over x); a pair that is not wanted is NULL.
+ *   s_row  : [ceil(cols / 128)][rows] bytes, leading dimension lds_row >= rows;  s_col : [ceil(rows / 128)][cols] bytes,
+ *            lds_col >= cols;  s : [ceil(rows / 128)][ceil(cols / 128)] bytes, lds >= ceil(cols / 128).  Any alignment.
+ * NaN and infinities as in fog_quantize.  The fast path needs cols and ldx multiples of 8 and 16-byte aligned x, codes 8-byte aligned with
+ * leading dimensions that are multiples of 8; other shapes go element by element with identical results.
+ * Errors: NULL (also half of a pair), SHAPE (negative sizes, leading dimensions, margin), ALIGN (odd x), UNSUPPORTED (format).
+ */
+fog_status fog_quantize_block(const void* x_bf16, int64_t rows, int64_t cols, int64_t ldx, fog_fp8 fmt, int margin,
+                              uint8_t* q_row, int64_t ldq_row, uint8_t* s_row, int64_t lds_row,
+                              uint8_t* q_col, int64_t ldq_col, uint8_t* s_col, int64_t lds_col, void* stream);
+fog_status fog_quantize_tile(const void* x_bf16, int64_t rows, int64_t cols, int64_t ldx, fog_fp8 fmt, int margin,
+                             uint8_t* q, int64_t ldq, uint8_t* s, int64_t lds, void* stream);
+
+/*
+ * fog_fp8_gemm on operands with a scale for each block of 128 contraction indices:
+ *     C[m, n] = bf16( sum over blocks b of 2^(sA(m, b) - 127) 2^(sB(n, b) - 127) sum_{k in b} decode(A) decode(B) ),
+ * accumulated in binary32; the matrix instruction applies the scales.  Block b holds contraction indices 128 b .. 128 b + 127.
+ *   block_A, block_B : how the operand's scales lie:
+ *     FOG_BLOCK_VECTOR  a byte for each row (column) of the product and block: scales[b][i], leading dimension lds >= M (A) or N (B):
+ *                       s_row of fog_quantize_block where the operand is stored with the contraction along its rows (A of NT and NN,
+ *                       B of NT), s_col where it is stored with the contraction down its columns (A of TN, B of NN and TN)
+ *     FOG_BLOCK_TILE    a byte for each 128 x 128 tile of the operand as it is stored: s of fog_quantize_tile, whichever
+ *                       way the product contracts it
+ *   Bytes 1 .. 254 (byte 255 gives NaN).  Any alignment.
+ *   workspace : NULL, or fog_fp8_gemm_block_workspace(layout, M, N, K) bytes, as for fog_fp8_gemm.
+ * NT products of up to 64 rows (the tokens of a decoding step) read B once, straight into the matrix instruction.
+ * Layouts, other arguments, requirements and errors as for fog_fp8_gemm.
+ */
+typedef enum { FOG_BLOCK_VECTOR = 0, FOG_BLOCK_TILE = 1 } fog_block;
+fog_status fog_fp8_gemm_block(fog_layout layout, int64_t M, int64_t N, int64_t K,
+                              const uint8_t* A, fog_fp8 fmtA, int64_t lda, fog_block block_A, const uint8_t* scales_A, int64_t lds_A,
+                              const uint8_t* B, fog_fp8 fmtB, int64_t ldb, fog_block block_B, const uint8_t* scales_B, int64_t lds_B,
+                              void* C_bf16, int64_t ldc, void* workspace, size_t workspace_bytes, void* stream);
+size_t fog_fp8_gemm_block_workspace(fog_layout layout, int64_t M, int64_t N, int64_t K);
+
+/*
+ * Embedding rows as the residual stream of the first block, fused with the FP8 cast of that block's first operand (the block has no
+ * pre-normalisation, so the scaled row is the first GEMM's input as it is):
+ *     x[t, :] = bf16( factor * E[tokens[t], :] ),     q = sat_rne_fmt( fl32( x * scale ) ),     amax_out = max |x|.
+ * A token outside 0 .. vocab - 1 (padding) gives a row of zeros.
+ *   tokens : count ids of token_bytes (4 or 8) bytes, signed.   table_bf16 : [vocab, cols], leading dimension ld_table.
+ *   factor : finite.   scale : one float; may be NULL without q.
+ *   x_bf16 : [count, cols], leading dimension ldx.   q : NULL or [count, cols] bytes, leading dimension ldq.
+ *   amax_out : NULL or one float, overwritten.
+ * The fast path needs cols and leading dimensions multiples of 8, table and x 16-byte and q 8-byte aligned.
+ * Errors: NULL, SHAPE, ALIGN, UNSUPPORTED (token_bytes, format, factor).
+ */
+fog_status fog_embed_quantize(const void* tokens, int token_bytes, int64_t count, const void* table_bf16, int64_t vocab, int64_t cols,
+                              int64_t ld_table, float factor, fog_fp8 fmt, const float* scale, void* x_bf16, int64_t ldx,
+                              uint8_t* q, int64_t ldq, float* amax_out, void* stream);
+
+/*
+ * The embedding table's gradient:  dE[v, :] = factor * sum over t with tokens[t] == v of dx[t, :]   (binary32 sums in a fixed order:
+ * deterministic, no atomics).  accumulate == 0: the whole of dE is overwritten, rows of ids that do not occur with zeros;
+ * otherwise the sums are added to dE (rounded once) and other rows are left alone (a table shared with the output projection).
+ * Tokens outside 0 .. vocab - 1 contribute nothing.
+ *   dx_bf16 : [count, cols], leading dimension ld_dx.   type : of dE, [vocab, cols] with leading dimension ld_dE.
+ *   workspace : fog_embed_grad_workspace(count, vocab, cols) bytes, 16-byte aligned; contents on entry do not matter.  Calls that may
+ *            overlap in time need a workspace each.
+ * Limits: count and cols below 2^31, vocab up to 4194302.  The tokens are sorted in tiles of 1024 that are merged by
+ * searching every tile for every token, which grows with count^2 / 1024 and stays below the sums up to about 10^5 tokens.
+ * Errors: NULL, SHAPE, ALIGN, WORKSPACE, UNSUPPORTED (token_bytes, type, factor, limits).
+ */
+typedef enum { FOG_BF16 = 0, FOG_F32 = 1 } fog_real;
+fog_status fog_embed_grad(const void* tokens, int token_bytes, int64_t count, const void* dx_bf16, int64_t ld_dx, int64_t vocab, int64_t cols,
+                          float factor, fog_real type, void* dE, int64_t ld_dE, int accumulate, void* workspace, size_t workspace_bytes,
+                          void* stream);
+size_t fog_embed_grad_workspace(int64_t count, int64_t vocab, int64_t cols);
+
+/*
+ * The global norm of a step's gradients, and their clipping to it:
+ *     sumsq = sum over all jobs of sum g^2   (binary64),      norm = sqrt(sumsq),
+ *     out = g * c,   c = fl32(max_norm / norm) where norm is finite and above max_norm, 1 otherwise.
+ * Two calls, so that a job over several GPUs can add up the ranks' sums in between (one 8-byte all-reduce).  c is a binary32 number: below
+ * 2^-126 it loses places.  A norm that is not finite leaves the gradients as they are and shows in `norm`: skip that step.
+ *   jobs  : HOST array of `count` descriptions, read before the call returns; any number of tensors, 120 to a launch.
+ *   g, out : n contiguous elements of `type`, aligned to their size (16-byte aligned ones are faster); out may be g (nothing is
+ *            written then where c is 1) and must not overlap any other gradient; fog_grad_sumsq does not look at it.
+ *   sumsq : one double, overwritten by fog_grad_sumsq, 8-byte aligned.   norm : NULL or one float, overwritten
+ *            (with FLT_MAX for a finite norm beyond it).
+ *   workspace : fog_grad_sumsq_workspace(count) bytes, 8-byte aligned; contents on entry do not matter.
+ * Errors: NULL, SHAPE (count, n), ALIGN, WORKSPACE, UNSUPPORTED (type, n above 2^37, max_norm negative or NaN).
+ */
+typedef struct {
+  const void* g;
+  void* out;
+  int64_t n;
+  fog_real type;
+} fog_grad_job;
+fog_status fog_grad_sumsq(const fog_grad_job* jobs, int count, double* sumsq, void* workspace, size_t workspace_bytes, void* stream);
+size_t fog_grad_sumsq_workspace(int count);
+fog_status fog_grad_clip(const fog_grad_job* jobs, int count, const double* sumsq, float max_norm, float* norm, void* stream);
+
+/*
  * FP8 dot-product attention forward (Appendix B, eq. P; Appendix E, FP8DPA row):
  *     O = Softmax(s Q K^T + M) V   per (batch, head), M the causal mask when causal != 0,
  * with Q~, K~, V~ in E4M3 and the probabilities cast to E4M3 for the P V product.

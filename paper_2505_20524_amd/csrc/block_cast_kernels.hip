@@ -1,0 +1,236 @@
+// Casts to FP8 with a scale for each block of 128 elements: along a row, along a column, or for each 128 x 128 tile.
+//
+// The scale of a block is a power of two, 2^k with the largest k that keeps FP8MAX >= 2^margin 2^k max|x|, and is kept as the byte
+// 127 - k of its reciprocal.  Multiplying by it is exact, so that the one rounding of an element is the cast's own, and the matrix
+// instruction takes the byte as it is.  The price is up to one binary place of the format's range, not of its precision.
+//
+// One workgroup of 256 threads reads a tile of 128 x 128 elements once, 16 bytes a lane, 16 lanes a row, and keeps it in registers (32
+// a thread): the maxima along rows are a reduction over 16 lanes, those along columns one over a thread's rows, the wave's four lanes
+// of a column group and, through LDS, the four waves.  Both forms of codes then come from the same registers: a tensor that a step
+// multiplies along its rows and along its columns is read once for the two casts.  Bound by memory: 2 bytes read and 1 written (2 for
+// both forms) per element.
+#include "common.h"
+#include "launch.h"
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int BLK = 128;
+constexpr int PASSES = BLK * BLK / 8 / kThreads;    // row groups of 16 that a thread holds: 8
+
+struct BlockCastArgs {
+  const uint16_t* x;
+  uint8_t *q_row, *s_row, *q_col, *s_col;   // tile form: q_row, s_row
+  int64_t ldx, ldq_row, lds_row, ldq_col, lds_col;
+  int64_t rows, cols;
+  int64_t tiles_c;
+  int margin;
+};
+
+// k of the block's scale from the magnitude pattern of its abs-max (bf16 without sign; 0x7F80 and above: not finite)
+template <int FMT>
+FOG_DEVICE int block_exponent(uint32_t a, int margin) {
+  if (a == 0u || a >= 0x7F80u) return 0;
+  int e = (int)(a >> 7) - 127;
+  uint32_t frac = a & 0x7Fu;
+  if (a < 0x80u) {                  // subnormal: the leading one is the highest set bit
+    const int top = 31 - __builtin_clz(a);
+    e = top - 133;
+    frac = (a << (7 - top)) & 0x7Fu;
+  }
+  // FP8MAX = 1.75 * 2^8 or 1.75 * 2^15; 1.75 has the fraction 0x60
+  const int k = (FMT == FOG_E4M3 ? 8 : 15) - e - (frac > 0x60u ? 1 : 0) - margin;
+  return k < -126 ? -126 : k > 126 ? 126 : k;
+}
+FOG_DEVICE float pow2(int k) { return __uint_as_float((uint32_t)(k + 127) << 23); }
+
+// maximum of packed pairs of magnitudes over the lanes of a group of 16, to all of them
+FOG_DEVICE uint32_t pkmax(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(us2, a), __builtin_bit_cast(us2, b)));
+}
+FOG_DEVICE uint32_t max_over_16(uint32_t v) {
+  v = pkmax(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x128, 0xF, 0xF, true));   // row_ror:8, 4, 2, 1
+  v = pkmax(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x124, 0xF, 0xF, true));
+  v = pkmax(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x122, 0xF, 0xF, true));
+  v = pkmax(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x121, 0xF, 0xF, true));
+  return v;
+}
+
+// Eight elements under eight scales.  NAN_TEST: they may hold NaN (a block that is not finite).
+template <int FMT, bool NAN_TEST>
+FOG_DEVICE uint2 cast8(uint4 v, const float* f) {
+  const float a = bf16lo(v.x) * f[0], b = bf16hi(v.x) * f[1], c = bf16lo(v.y) * f[2], d = bf16hi(v.y) * f[3];
+  const float e = bf16lo(v.z) * f[4], g = bf16hi(v.z) * f[5], h = bf16lo(v.w) * f[6], i = bf16hi(v.w) * f[7];
+  if (NAN_TEST) return make_uint2(cvt4_fp8_nan<FMT>(a, b, c, d), cvt4_fp8_nan<FMT>(e, g, h, i));
+  return make_uint2(cvt4_fp8<FMT>(a, b, c, d), cvt4_fp8<FMT>(e, g, h, i));
+}
+
+template <bool VEC>
+FOG_DEVICE void store8(uint8_t* q, int64_t at, uint2 v, int n) {
+  if (VEC) {
+    st_nt8(q + at, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) q[at + i] = (uint8_t)((i < 4 ? v.x : v.y) >> (8 * (i & 3)));
+  }
+}
+
+// VEC: x in 16-byte pieces, codes in 8-byte pieces (leading dimensions and cols multiples of 8, aligned pointers).
+template <int FMT, bool ROW, bool COL, bool TILE, bool VEC>
+__global__ __launch_bounds__(kThreads) void block_cast_kernel(BlockCastArgs a) {
+  __shared__ uint32_t colmax[4][64];      // per wave: 128 columns' maxima in pairs
+  __shared__ uint8_t rowbyte[BLK];
+  const int t = threadIdx.x, l = t & 63, w = t >> 6;
+  const int64_t tr = (int64_t)blockIdx.x / a.tiles_c, tc = (int64_t)blockIdx.x - tr * a.tiles_c;
+  const int64_t r0 = tr * BLK, c0 = tc * BLK;
+  const int nrows = (int)(a.rows - r0 < BLK ? a.rows - r0 : BLK), ncols = (int)(a.cols - c0 < BLK ? a.cols - c0 : BLK);
+  const int rr = t >> 4, cc = 8 * (t & 15);      // row of pass p: 16 p + rr
+  const int n = ncols - cc < 0 ? 0 : ncols - cc < 8 ? ncols - cc : 8;
+  const uint16_t* x = a.x + (r0 + rr) * a.ldx + c0 + cc;
+
+  uint4 v[PASSES];
+#pragma unroll
+  for (int p = 0; p < PASSES; ++p) {
+    v[p] = make_uint4(0, 0, 0, 0);
+    if (16 * p + rr < nrows) {
+      if (VEC) {
+        if (n > 0) v[p] = ld_nt16(x + 16 * p * a.ldx);
+      } else {
+        uint32_t wv[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (i < n) wv[i >> 1] |= (uint32_t)x[16 * p * a.ldx + i] << (16 * (i & 1));
+        v[p] = make_uint4(wv[0], wv[1], wv[2], wv[3]);
+      }
+    }
+  }
+  // maxima: of each row over the 16 lanes that hold it, of each column over this thread's rows
+  uint32_t rowmax[PASSES];
+  uint32_t cm[4] = {0, 0, 0, 0};
+#pragma unroll
+  for (int p = 0; p < PASSES; ++p) {
+    if (ROW) rowmax[p] = max_of_pair(max_over_16(pkmax_abs_bf16(pkmax_abs_bf16(pkmax_abs_bf16(pkmax_abs_bf16(0u, v[p].x), v[p].y), v[p].z), v[p].w)));
+    if (COL || TILE) {
+      cm[0] = pkmax_abs_bf16(cm[0], v[p].x);
+      cm[1] = pkmax_abs_bf16(cm[1], v[p].y);
+      cm[2] = pkmax_abs_bf16(cm[2], v[p].z);
+      cm[3] = pkmax_abs_bf16(cm[3], v[p].w);
+    }
+  }
+  if (ROW) {
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+      const int k = block_exponent<FMT>(rowmax[p], a.margin);
+      const float f1 = pow2(k);
+      const float f[8] = {f1, f1, f1, f1, f1, f1, f1, f1};
+      const int r = 16 * p + rr;
+      if ((t & 15) == 0) rowbyte[r] = (uint8_t)(127 - k);
+      if (r < nrows && n > 0) {
+        const uint2 o = __builtin_expect(rowmax[p] >= 0x7F80u, 0) ? cast8<FMT, true>(v[p], f) : cast8<FMT, false>(v[p], f);
+        store8<VEC>(a.q_row, (r0 + r) * a.ldq_row + c0 + cc, o, n);
+      }
+    }
+  }
+  if (COL || TILE) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      cm[i] = pkmax(cm[i], (uint32_t)__shfl_xor((int)cm[i], 16, 64));
+      cm[i] = pkmax(cm[i], (uint32_t)__shfl_xor((int)cm[i], 32, 64));
+    }
+    if (l < 16) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) colmax[w][4 * l + i] = cm[i];
+    }
+  }
+  __syncthreads();
+  if (ROW && t < nrows) a.s_row[tc * a.lds_row + r0 + t] = rowbyte[t];
+  if (COL) {
+    float f[8];
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int at = 4 * (t & 15) + i;
+      const uint32_t m = pkmax(pkmax(colmax[0][at], colmax[1][at]), pkmax(colmax[2][at], colmax[3][at]));
+      const int k0 = block_exponent<FMT>(m & 0xFFFFu, a.margin), k1 = block_exponent<FMT>(m >> 16, a.margin);
+      f[2 * i] = pow2(k0);
+      f[2 * i + 1] = pow2(k1);
+      odd = odd || max_of_pair(m) >= 0x7F80u;
+      if (t < 16) {
+        uint8_t* s = a.s_col + tr * a.lds_col + c0 + cc + 2 * i;
+        if (2 * i < n) s[0] = (uint8_t)(127 - k0);
+        if (2 * i + 1 < n) s[1] = (uint8_t)(127 - k1);
+      }
+    }
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+      const int r = 16 * p + rr;
+      if (r < nrows && n > 0) {
+        const uint2 o = __builtin_expect(odd, 0) ? cast8<FMT, true>(v[p], f) : cast8<FMT, false>(v[p], f);
+        store8<VEC>(a.q_col, (r0 + r) * a.ldq_col + c0 + cc, o, n);
+      }
+    }
+  }
+  if (TILE) {
+    uint32_t m = pkmax(pkmax(colmax[0][l], colmax[1][l]), pkmax(colmax[2][l], colmax[3][l]));
+    m = wave_max_u32(max_of_pair(m));
+    const int k = block_exponent<FMT>(m, a.margin);
+    const float f1 = pow2(k);
+    const float f[8] = {f1, f1, f1, f1, f1, f1, f1, f1};
+    if (t == 0) a.s_row[tr * a.lds_row + tc] = (uint8_t)(127 - k);
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+      const int r = 16 * p + rr;
+      if (r < nrows && n > 0) {
+        const uint2 o = __builtin_expect(m >= 0x7F80u, 0) ? cast8<FMT, true>(v[p], f) : cast8<FMT, false>(v[p], f);
+        store8<VEC>(a.q_row, (r0 + r) * a.ldq_row + c0 + cc, o, n);
+      }
+    }
+  }
+}
+
+inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+template <bool ROW, bool COL, bool TILE>
+fog_status launch(BlockCastArgs a, fog_fp8 fmt, hipStream_t s) {
+  a.tiles_c = (a.cols + BLK - 1) / BLK;
+  const int64_t tiles = a.tiles_c * ((a.rows + BLK - 1) / BLK);
+  if (tiles > 0x7FFFFFFF) return FOG_ERR_UNSUPPORTED;
+  const bool vec = a.cols % 8 == 0 && a.ldx % 8 == 0 && aligned(a.x, 16) && (!(ROW || TILE) || (aligned(a.q_row, 8) && a.ldq_row % 8 == 0)) &&
+                   (!COL || (aligned(a.q_col, 8) && a.ldq_col % 8 == 0));
+  const int grid = (int)tiles;
+#define FOG_BC(F, V) block_cast_kernel<F, ROW, COL, TILE, V><<<grid, kThreads, 0, s>>>(a)
+  if (fmt == FOG_E4M3) { if (vec) FOG_BC(FOG_E4M3, true); else FOG_BC(FOG_E4M3, false); }
+  else                 { if (vec) FOG_BC(FOG_E5M2, true); else FOG_BC(FOG_E5M2, false); }
+#undef FOG_BC
+  return fog_launch_status();
+}
+
+}  // namespace
+
+extern "C" fog_status fog_quantize_block(const void* x_bf16, int64_t rows, int64_t cols, int64_t ldx, fog_fp8 fmt, int margin,
+                                         uint8_t* q_row, int64_t ldq_row, uint8_t* s_row, int64_t lds_row,
+                                         uint8_t* q_col, int64_t ldq_col, uint8_t* s_col, int64_t lds_col, void* stream) {
+  if (rows < 0 || cols < 0 || margin < -64 || margin > 64) return FOG_ERR_SHAPE;
+  if (fmt != FOG_E4M3 && fmt != FOG_E5M2) return FOG_ERR_UNSUPPORTED;
+  if (rows == 0 || cols == 0) return FOG_OK;
+  if (!x_bf16 || (!q_row && !q_col) || (!q_row) != (!s_row) || (!q_col) != (!s_col)) return FOG_ERR_NULL;
+  if (ldx < cols || (q_row && (ldq_row < cols || lds_row < rows)) || (q_col && (ldq_col < cols || lds_col < cols))) return FOG_ERR_SHAPE;
+  if (!aligned(x_bf16, 2)) return FOG_ERR_ALIGN;
+  const BlockCastArgs a{reinterpret_cast<const uint16_t*>(x_bf16), q_row, s_row, q_col, s_col, ldx, ldq_row, lds_row, ldq_col, lds_col, rows, cols, 0, margin};
+  hipStream_t s = (hipStream_t)stream;
+  if (q_row && q_col) return launch<true, true, false>(a, fmt, s);
+  return q_row ? launch<true, false, false>(a, fmt, s) : launch<false, true, false>(a, fmt, s);
+}
+
+extern "C" fog_status fog_quantize_tile(const void* x_bf16, int64_t rows, int64_t cols, int64_t ldx, fog_fp8 fmt, int margin,
+                                        uint8_t* q, int64_t ldq, uint8_t* s, int64_t lds, void* stream) {
+  if (rows < 0 || cols < 0 || margin < -64 || margin > 64) return FOG_ERR_SHAPE;
+  if (fmt != FOG_E4M3 && fmt != FOG_E5M2) return FOG_ERR_UNSUPPORTED;
+  if (rows == 0 || cols == 0) return FOG_OK;
+  if (!x_bf16 || !q || !s) return FOG_ERR_NULL;
+  if (ldx < cols || ldq < cols || lds < (cols + BLK - 1) / BLK) return FOG_ERR_SHAPE;
+  if (!aligned(x_bf16, 2)) return FOG_ERR_ALIGN;
+  const BlockCastArgs a{reinterpret_cast<const uint16_t*>(x_bf16), q, s, nullptr, nullptr, ldx, ldq, lds, 0, 0, rows, cols, 0, margin};
+  return launch<false, false, true>(a, fmt, (hipStream_t)stream);
+}

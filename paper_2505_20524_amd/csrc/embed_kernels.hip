@@ -1,0 +1,495 @@
+// The embedding in front of the first block: scaled rows of the table as the residual stream and as FP8 codes, and the table's gradient.
+//
+// Forward: x = bf16(factor E[t]), its codes and abs-max in the same pass.  Bound by memory: 2 bytes read, 2 written and 1 for the codes
+// per element.
+//
+// Gradient: dE[v] = factor sum over the tokens t with id v of dx[t], in binary32 and in the order of the tokens.  The tokens are
+// sorted by id first, so that every sum is a run of the sorted order and no two writers meet: no atomics on sums, the same result on
+// every run.
+//   1. sort_tiles: a workgroup sorts 1024 tokens by (id, position) in LDS.
+//   2. merge_ranks: a token's place in the whole order is its place in its tile plus, for every other tile, the number of that tile's
+//      tokens before it (a binary search); stable, because earlier tiles count their equal ids and later ones do not.
+//   3. sum_runs: a wave adds `chunk` consecutive tokens of the order on 512 columns and writes each run that begins and ends in
+//      the chunk; what a run has in a chunk that it does not begin and end in goes to the workspace.  Other waves of the same
+//      launch write zeros to the rows of absent ids.
+//   4. join_runs: adds the pieces of the runs that cross chunks, in order.
+#include "common.h"
+#include "launch.h"
+
+namespace {
+
+constexpr int kThreads = 256;
+
+__global__ void zero_u32e(uint32_t* p) { *p = 0u; }
+
+FOG_DEVICE int64_t token_at(const void* tokens, int wide, int64_t i) {
+  return wide ? reinterpret_cast<const int64_t*>(tokens)[i] : (int64_t)reinterpret_cast<const int32_t*>(tokens)[i];
+}
+
+// ---------------------------------------------------------------- forward
+struct EmbedArgs {
+  const void* tokens;
+  int wide;
+  int64_t count, vocab, cols, ld_table, ldx, ldq;
+  const uint16_t* table;
+  float factor;
+  const float* scale;
+  uint16_t* x;
+  uint8_t* q;
+  uint32_t* amax_out;
+  int lanes;    // threads of a row, a power of two
+};
+
+// VEC: rows of the table, of x and of q in pieces of eight elements.
+template <int FMT, bool VEC>
+__global__ __launch_bounds__(kThreads) void embed_kernel(EmbedArgs a) {
+  const float rho = a.q ? *a.scale : 0.0f;
+  const int per_wg = kThreads / a.lanes, lane = threadIdx.x & (a.lanes - 1);
+  uint32_t m = 0u;
+  for (int64_t r = (int64_t)blockIdx.x * per_wg + threadIdx.x / a.lanes; r < a.count; r += (int64_t)gridDim.x * per_wg) {
+    const int64_t id = token_at(a.tokens, a.wide, r);
+    const bool in = id >= 0 && id < a.vocab;
+    const uint16_t* e = a.table + (in ? id : 0) * a.ld_table;
+    if (VEC) {
+      for (int64_t c = 8 * (int64_t)lane; c < a.cols; c += 8 * (int64_t)a.lanes) {
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (in) {
+          v = *reinterpret_cast<const uint4*>(e + c);
+          v = make_uint4(pack_bf16x2(bf16lo(v.x) * a.factor, bf16hi(v.x) * a.factor), pack_bf16x2(bf16lo(v.y) * a.factor, bf16hi(v.y) * a.factor),
+                         pack_bf16x2(bf16lo(v.z) * a.factor, bf16hi(v.z) * a.factor), pack_bf16x2(bf16lo(v.w) * a.factor, bf16hi(v.w) * a.factor));
+        }
+        m = pkmax_abs_bf16(m, v.x); m = pkmax_abs_bf16(m, v.y); m = pkmax_abs_bf16(m, v.z); m = pkmax_abs_bf16(m, v.w);
+        st_nt16(a.x + r * a.ldx + c, v);
+        if (a.q)
+          st_nt8(a.q + r * a.ldq + c, make_uint2(cvt4_fp8_nan<FMT>(bf16lo(v.x) * rho, bf16hi(v.x) * rho, bf16lo(v.y) * rho, bf16hi(v.y) * rho),
+                                                 cvt4_fp8_nan<FMT>(bf16lo(v.z) * rho, bf16hi(v.z) * rho, bf16lo(v.w) * rho, bf16hi(v.w) * rho)));
+      }
+    } else {
+      for (int64_t c = lane; c < a.cols; c += a.lanes) {
+        const uint32_t b = in ? f32_to_bf16(bf16lo(e[c]) * a.factor) : 0u;
+        const uint32_t mag = b & 0x7FFFu;
+        m = max_of_pair(m) > mag ? max_of_pair(m) : mag;
+        a.x[r * a.ldx + c] = (uint16_t)b;
+        if (a.q) {
+          const float t = bf16lo(b) * rho;
+          a.q[r * a.ldq + c] = (uint8_t)(cvt4_fp8_nan<FMT>(t, t, t, t) & 0xFFu);
+        }
+      }
+    }
+  }
+  if (a.amax_out) {
+    const uint32_t top = wave_max_u32(max_of_pair(m)) << 16;     // the float with that bf16 pattern
+    if ((threadIdx.x & 63) == 0 && top > __hip_atomic_load(a.amax_out, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(a.amax_out, top);
+  }
+}
+
+// ---------------------------------------------------------------- gradient: order of the tokens
+constexpr int SORT_TILE = 1024;
+constexpr int POS_BITS = 10;
+// ids, the id behind the last (for tokens outside the table) and one more (the padding's) fit beside a position in the tile
+constexpr int64_t VOCAB_MAX = ((int64_t)1 << (32 - POS_BITS)) - 2;
+
+// Ids outside the table become `vocab`, which sorts last and is skipped.
+FOG_DEVICE uint32_t sort_key(const void* tokens, int wide, int64_t count, int64_t vocab, int64_t i, int local) {
+  if (i >= count) return 0xFFFFFFFFu;
+  const int64_t id = token_at(tokens, wide, i);
+  return (uint32_t)((id >= 0 && id < vocab ? id : vocab) << POS_BITS) | (uint32_t)local;
+}
+
+// keys: tiles * SORT_TILE words.  With one tile the order is final: ids and positions are written instead.
+__global__ __launch_bounds__(SORT_TILE / 2) void sort_tiles_kernel(const void* tokens, int wide, int64_t count, int64_t vocab, uint32_t* keys, uint32_t* ids,
+                                                                  uint32_t* positions) {
+  __shared__ uint32_t k[SORT_TILE];
+  const int t = threadIdx.x;
+  const int64_t base = (int64_t)blockIdx.x * SORT_TILE;
+  for (int i = t; i < SORT_TILE; i += SORT_TILE / 2) k[i] = sort_key(tokens, wide, count, vocab, base + i, i);
+  for (int size = 2; size <= SORT_TILE; size *= 2)
+    for (int stride = size / 2; stride > 0; stride /= 2) {
+      __syncthreads();
+      const int i = 2 * t - (t & (stride - 1)), j = i + stride;
+      const uint32_t x = k[i], y = k[j];
+      const bool up = (i & size) == 0;
+      if ((x > y) == up) {
+        k[i] = y;
+        k[j] = x;
+      }
+    }
+  __syncthreads();
+  for (int i = t; i < SORT_TILE; i += SORT_TILE / 2) {
+    if (gridDim.x > 1) {
+      keys[base + i] = k[i];
+    } else if (i < count) {
+      ids[i] = k[i] >> POS_BITS;
+      positions[i] = k[i] & (SORT_TILE - 1);
+    }
+  }
+}
+
+// Number of a sorted tile's keys below `limit`.
+FOG_DEVICE int keys_below(const uint32_t* tile, uint32_t limit) {
+  int at = 0;
+#pragma unroll
+  for (int step = SORT_TILE / 2; step > 0; step /= 2)
+    if (tile[at + step - 1] < limit) at += step;
+  return at + (tile[at] < limit ? 1 : 0);
+}
+
+constexpr int MERGE_TILES = 16;    // tiles in LDS at a time
+__global__ __launch_bounds__(SORT_TILE) void merge_ranks_kernel(const uint32_t* __restrict__ keys, int64_t count, int tiles, uint32_t* __restrict__ ids,
+                                                                uint32_t* __restrict__ positions) {
+  __shared__ uint32_t k[MERGE_TILES][SORT_TILE];
+  const int mine = blockIdx.x, t = threadIdx.x;
+  const uint32_t key = keys[(int64_t)mine * SORT_TILE + t], id = key >> POS_BITS;
+  int64_t rank = t;
+  for (int base = 0; base < tiles; base += MERGE_TILES) {
+    const int n = min(MERGE_TILES, tiles - base);
+    __syncthreads();
+    for (int b = 0; b < n; ++b) k[b][t] = keys[(int64_t)(base + b) * SORT_TILE + t];
+    __syncthreads();
+    for (int b = 0; b < n; ++b) {
+      const int tile = base + b;
+      if (tile == mine) continue;
+      // a key of an earlier tile with the same id comes first; one of a later tile does not (id + 1 of a token
+      // fits its bits; the padding behind the last tile's tokens sorts behind all of them and takes no place)
+      rank += keys_below(k[b], (tile < mine ? id + 1u : id) << POS_BITS);
+    }
+  }
+  const int64_t pos = (int64_t)mine * SORT_TILE + (key & (SORT_TILE - 1));
+  if (key != 0xFFFFFFFFu) {
+    ids[rank] = id;
+    positions[rank] = (uint32_t)pos;
+  }
+}
+
+// ---------------------------------------------------------------- gradient: sums
+constexpr int SLAB = 512;    // columns of a wave
+
+struct GradArgs {
+  const uint32_t *ids, *positions;
+  const uint16_t* dx;
+  void* dE;
+  float *head, *tail;       // [chunks][cols]: what a chunk has of the run that began before it / that goes on behind it
+  int64_t count, vocab, cols, ld_dx, ld_dE;
+  float factor;
+  int accumulate;
+  int chunk;                // tokens of a wave, a power of two up to 64
+  int slabs;                // ceil(cols / SLAB)
+  int64_t chunks;
+  int64_t units;            // waves of sums: chunks * slabs; waves behind them write zeros
+};
+
+template <bool F32, bool VEC>
+struct Row {
+  float v[8];
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+  }
+  // + the row of dx at p (n of its elements are inside)
+  static __device__ __forceinline__ uint4 load(const uint16_t* p, int n) {
+    if (VEC) return n > 0 ? ld_nt16(p) : make_uint4(0, 0, 0, 0);
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) w[i >> 1] |= (uint32_t)p[i] << (16 * (i & 1));
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  __device__ __forceinline__ void add(uint4 x) {
+    v[0] += bf16lo(x.x); v[1] += bf16hi(x.x); v[2] += bf16lo(x.y); v[3] += bf16hi(x.y);
+    v[4] += bf16lo(x.z); v[5] += bf16hi(x.z); v[6] += bf16lo(x.w); v[7] += bf16hi(x.w);
+  }
+  __device__ __forceinline__ void add_floats(const float* p, int n) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) v[i] += p[i];
+  }
+  __device__ __forceinline__ void put_floats(float* p, int n) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) p[i] = v[i];
+  }
+  // the finished sum times the factor (added to what is there) to the table's gradient
+  __device__ __forceinline__ void finish(const GradArgs& a, int64_t id, int64_t col, int n) const {
+    if (n <= 0) return;
+    float r[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = v[i] * a.factor;
+    if (F32) {
+      float* p = reinterpret_cast<float*>(a.dE) + id * a.ld_dE + col;
+      if (VEC) {
+        if (a.accumulate) {
+          const float4 x = *reinterpret_cast<const float4*>(p), y = *reinterpret_cast<const float4*>(p + 4);
+          r[0] += x.x; r[1] += x.y; r[2] += x.z; r[3] += x.w; r[4] += y.x; r[5] += y.y; r[6] += y.z; r[7] += y.w;
+        }
+        st_nt16(p, make_uint4(__float_as_uint(r[0]), __float_as_uint(r[1]), __float_as_uint(r[2]), __float_as_uint(r[3])));
+        st_nt16(p + 4, make_uint4(__float_as_uint(r[4]), __float_as_uint(r[5]), __float_as_uint(r[6]), __float_as_uint(r[7])));
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (i < n) p[i] = a.accumulate ? p[i] + r[i] : r[i];
+      }
+    } else {
+      uint16_t* p = reinterpret_cast<uint16_t*>(a.dE) + id * a.ld_dE + col;
+      if (VEC) {
+        if (a.accumulate) {
+          const uint4 x = *reinterpret_cast<const uint4*>(p);
+          r[0] += bf16lo(x.x); r[1] += bf16hi(x.x); r[2] += bf16lo(x.y); r[3] += bf16hi(x.y);
+          r[4] += bf16lo(x.z); r[5] += bf16hi(x.z); r[6] += bf16lo(x.w); r[7] += bf16hi(x.w);
+        }
+        st_nt16(p, make_uint4(pack_bf16x2(r[0], r[1]), pack_bf16x2(r[2], r[3]), pack_bf16x2(r[4], r[5]), pack_bf16x2(r[6], r[7])));
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (i < n) p[i] = (uint16_t)f32_to_bf16(a.accumulate ? bf16lo(p[i]) + r[i] : r[i]);
+      }
+    }
+  }
+};
+
+// Is id among the sorted ids?
+FOG_DEVICE bool present(const uint32_t* ids, int64_t count, uint32_t id) {
+  int64_t lo = 0, hi = count;
+  while (lo < hi) {
+    const int64_t mid = (lo + hi) >> 1;
+    if (ids[mid] < id) lo = mid + 1;
+    else hi = mid;
+  }
+  return lo < count && ids[lo] == id;
+}
+
+constexpr int ZERO_ROWS = 16;    // rows of the table a wave looks up and clears
+
+template <bool F32, bool VEC>
+FOG_DEVICE void zero_rows(const GradArgs& a, int64_t group, int l) {
+  const int64_t first = group * ZERO_ROWS;
+  if (first >= a.vocab) return;
+  const int64_t row = first + (l & (ZERO_ROWS - 1));
+  const uint64_t there = __ballot(row >= a.vocab || present(a.ids, a.count, (uint32_t)row));
+  for (int i = 0; i < ZERO_ROWS; ++i) {
+    if (there >> i & 1) continue;
+    const int64_t at = (first + i) * a.ld_dE;
+    if (VEC) {
+      constexpr int E = F32 ? 4 : 8;
+      uint8_t* p = reinterpret_cast<uint8_t*>(a.dE) + at * (F32 ? 4 : 2);
+      for (int64_t c = (int64_t)E * l; c < a.cols; c += E * 64) st_nt16(p + c * (F32 ? 4 : 2), make_uint4(0, 0, 0, 0));
+    } else {
+      for (int64_t c = l; c < a.cols; c += 64) {
+        if (F32) reinterpret_cast<float*>(a.dE)[at + c] = 0.0f;
+        else     reinterpret_cast<uint16_t*>(a.dE)[at + c] = 0;
+      }
+    }
+  }
+}
+
+template <bool F32, bool VEC>
+__global__ __launch_bounds__(kThreads) void sum_runs_kernel(GradArgs a) {
+  const int l = threadIdx.x & 63;
+  const int64_t unit = (int64_t)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (unit >= a.units) {
+    if (!a.accumulate) zero_rows<F32, VEC>(a, unit - a.units, l);
+    return;
+  }
+  const int64_t c = unit / a.slabs, p0 = c * a.chunk;
+  const int64_t col = (unit - c * a.slabs) * SLAB + 8 * l;
+  const int n = a.cols - col >= 8 ? 8 : a.cols > col ? (int)(a.cols - col) : 0;
+  const int len = (int)(a.count - p0 < a.chunk ? a.count - p0 : a.chunk);
+  // a lane keeps one token of the chunk
+  const int mine = l < len ? l : len - 1;
+  const uint32_t id_l = a.ids[p0 + mine], pos_l = a.positions[p0 + mine];
+  const uint32_t before = p0 > 0 ? a.ids[p0 - 1] : 0xFFFFFFFFu;
+  const uint32_t after = p0 + len < a.count ? a.ids[p0 + len] : 0xFFFFFFFFu;
+  constexpr int AHEAD = 8;
+  Row<F32, VEC> sum;
+  sum.clear();
+  uint32_t cur = (uint32_t)__builtin_amdgcn_readlane((int)id_l, 0);
+  bool began = cur != before;       // the current run begins in this chunk
+  for (int i0 = 0; i0 < len; i0 += AHEAD) {
+    uint4 v[AHEAD];
+    uint32_t id[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const int i = i0 + u < len ? i0 + u : len - 1;
+      id[u] = (uint32_t)__builtin_amdgcn_readlane((int)id_l, i);
+      const uint32_t pos = (uint32_t)__builtin_amdgcn_readlane((int)pos_l, i);
+      v[u] = make_uint4(0, 0, 0, 0);
+      if (i0 + u < len && id[u] < (uint32_t)a.vocab) v[u] = Row<F32, VEC>::load(a.dx + (int64_t)pos * a.ld_dx + col, n);
+    }
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      if (i0 + u >= len) break;
+      if (id[u] != cur) {
+        if (began) sum.finish(a, cur, col, n);
+        else       sum.put_floats(a.head + c * a.cols + col, n);
+        sum.clear();
+        cur = id[u];
+        began = true;
+      }
+      sum.add(v[u]);
+    }
+  }
+  if (cur >= (uint32_t)a.vocab) return;     // ids outside the table come last
+  if (!began)            sum.put_floats(a.head + c * a.cols + col, n);
+  else if (cur == after) sum.put_floats(a.tail + c * a.cols + col, n);
+  else                   sum.finish(a, cur, col, n);
+}
+
+// A workgroup for each chunk and slab; those whose chunk ends inside a run that it began add up the run's pieces: the four waves a
+// quarter of the chunks each, then the four sums in order.
+template <bool F32, bool VEC>
+__global__ __launch_bounds__(kThreads) void join_runs_kernel(GradArgs a) {
+  const int64_t c = (int64_t)blockIdx.x / a.slabs;
+  const int64_t next = (c + 1) * a.chunk;              // first token of the next chunk
+  if (next >= a.count) return;
+  const uint32_t id = a.ids[next];
+  if (id >= (uint32_t)a.vocab || a.ids[next - 1] != id) return;
+  if (c * a.chunk > 0 && a.ids[c * a.chunk] == id && a.ids[c * a.chunk - 1] == id) return;      // begun before this chunk
+  // end of the run: first token behind it
+  int64_t lo = next, hi = a.count;
+  while (lo < hi) {
+    const int64_t mid = (lo + hi) >> 1;
+    if (a.ids[mid] <= id) lo = mid + 1;
+    else hi = mid;
+  }
+  const int64_t last = (lo - 1) / a.chunk, m = last - c;   // chunks c + 1 .. last have a head of this run
+  const int w = threadIdx.x >> 6, l = threadIdx.x & 63;
+  const int64_t col = ((int64_t)blockIdx.x - c * a.slabs) * SLAB + 8 * l;
+  const int n = a.cols - col >= 8 ? 8 : a.cols > col ? (int)(a.cols - col) : 0;
+  const int64_t per = (m + 3) / 4, b = c + 1 + w * per, e = b + per < last + 1 ? b + per : last + 1;
+  Row<F32, VEC> sum;
+  sum.clear();
+  if (w == 0) sum.add_floats(a.tail + c * a.cols + col, n);
+#pragma unroll 4
+  for (int64_t i = b; i < e; ++i) sum.add_floats(a.head + i * a.cols + col, n);
+  __shared__ float part[3][8][64];
+  if (w > 0) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) part[w - 1][i][l] = sum.v[i];
+  }
+  __syncthreads();
+  if (w > 0) return;
+  for (int k = 0; k < 3; ++k)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum.v[i] += part[k][i][l];
+  sum.finish(a, id, col, n);
+}
+
+// Tokens of a wave: as many as still give every compute unit eight waves, 64 at most, 8 at least (a load of eight rows is in flight).
+int chunk_of(int64_t count, int64_t cols) {
+  const int64_t slabs = (cols + SLAB - 1) / SLAB;
+  int chunk = 64;
+  while (chunk > 8 && (count + chunk - 1) / chunk * slabs < 8 * (int64_t)fog_compute_units()) chunk /= 2;
+  return chunk;
+}
+
+struct GradRoom {   // the workspace in bytes
+  size_t keys, order, pieces, total;
+};
+GradRoom room_of(int64_t count, int64_t cols) {
+  GradRoom r;
+  const int64_t tiles = (count + SORT_TILE - 1) / SORT_TILE;
+  const int chunk = chunk_of(count, cols);
+  r.keys = (size_t)tiles * SORT_TILE * 4;
+  r.order = ((size_t)count * 4 + 15) / 16 * 16;
+  r.pieces = ((size_t)((count + chunk - 1) / chunk) * (size_t)cols * 4 + 15) / 16 * 16;
+  r.total = r.keys + 2 * r.order + 2 * r.pieces;
+  return r;
+}
+
+inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+}  // namespace
+
+extern "C" fog_status fog_embed_quantize(const void* tokens, int token_bytes, int64_t count, const void* table_bf16, int64_t vocab, int64_t cols,
+                                         int64_t ld_table, float factor, fog_fp8 fmt, const float* scale, void* x_bf16, int64_t ldx,
+                                         uint8_t* q, int64_t ldq, float* amax_out, void* stream) {
+  if (count < 0 || vocab < 0 || cols < 0) return FOG_ERR_SHAPE;
+  if (token_bytes != 4 && token_bytes != 8) return FOG_ERR_UNSUPPORTED;
+  if (fmt != FOG_E4M3 && fmt != FOG_E5M2) return FOG_ERR_UNSUPPORTED;
+  if (!(factor - factor == 0.0f)) return FOG_ERR_UNSUPPORTED;
+  const bool any = count > 0 && cols > 0;
+  if (any) {
+    if (!tokens || !x_bf16 || (vocab > 0 && !table_bf16) || (q && !scale)) return FOG_ERR_NULL;
+    if (ld_table < cols || ldx < cols || (q && ldq < cols)) return FOG_ERR_SHAPE;
+    if (!aligned(tokens, token_bytes) || !aligned(table_bf16, 2) || !aligned(x_bf16, 2)) return FOG_ERR_ALIGN;
+  }
+  hipStream_t s = (hipStream_t)stream;
+  if (amax_out) zero_u32e<<<1, 1, 0, s>>>(reinterpret_cast<uint32_t*>(amax_out));
+  if (!any) return amax_out ? fog_launch_status() : FOG_OK;
+  EmbedArgs a{tokens, token_bytes == 8, count, vocab, cols, ld_table, ldx, ldq, reinterpret_cast<const uint16_t*>(table_bf16), factor, scale,
+              reinterpret_cast<uint16_t*>(x_bf16), q, reinterpret_cast<uint32_t*>(amax_out), kThreads};
+  const bool vec = cols % 8 == 0 && ld_table % 8 == 0 && ldx % 8 == 0 && aligned(table_bf16, 16) && aligned(x_bf16, 16) &&
+                   (!q || (ldq % 8 == 0 && aligned(q, 8)));
+  const int64_t pieces = vec ? cols / 8 : cols;
+  while (a.lanes > 16 && a.lanes / 2 >= pieces) a.lanes /= 2;
+  const int64_t per_wg = kThreads / a.lanes;
+  int64_t blocks = (count + per_wg - 1) / per_wg;
+  const int64_t most = 8 * (int64_t)fog_compute_units();
+  if (blocks > most) blocks = most;
+#define FOG_EM(F, V) embed_kernel<F, V><<<(int)blocks, kThreads, 0, s>>>(a)
+  if (fmt == FOG_E4M3) { if (vec) FOG_EM(FOG_E4M3, true); else FOG_EM(FOG_E4M3, false); }
+  else                 { if (vec) FOG_EM(FOG_E5M2, true); else FOG_EM(FOG_E5M2, false); }
+#undef FOG_EM
+  return fog_launch_status();
+}
+
+extern "C" size_t fog_embed_grad_workspace(int64_t count, int64_t vocab, int64_t cols) {
+  if (count <= 0 || vocab <= 0 || cols <= 0 || count > 0x7FFFFFFF || vocab > VOCAB_MAX || cols > 0x7FFFFFFF) return 0;
+  return room_of(count, cols).total;
+}
+
+extern "C" fog_status fog_embed_grad(const void* tokens, int token_bytes, int64_t count, const void* dx_bf16, int64_t ld_dx, int64_t vocab,
+                                     int64_t cols, float factor, fog_real type, void* dE, int64_t ld_dE, int accumulate, void* workspace,
+                                     size_t workspace_bytes, void* stream) {
+  if (count < 0 || vocab < 0 || cols < 0) return FOG_ERR_SHAPE;
+  if (token_bytes != 4 && token_bytes != 8) return FOG_ERR_UNSUPPORTED;
+  if (type != FOG_BF16 && type != FOG_F32) return FOG_ERR_UNSUPPORTED;
+  if (!(factor - factor == 0.0f)) return FOG_ERR_UNSUPPORTED;
+  if (count > 0x7FFFFFFF || vocab > VOCAB_MAX || cols > 0x7FFFFFFF) return FOG_ERR_UNSUPPORTED;
+  if (vocab == 0 || cols == 0 || (count == 0 && accumulate)) return FOG_OK;
+  const int size = type == FOG_F32 ? 4 : 2;
+  if (!dE || (count > 0 && (!tokens || !dx_bf16))) return FOG_ERR_NULL;
+  if (ld_dE < cols || (count > 0 && ld_dx < cols)) return FOG_ERR_SHAPE;
+  if (!aligned(dE, size) || (count > 0 && (!aligned(tokens, token_bytes) || !aligned(dx_bf16, 2)))) return FOG_ERR_ALIGN;
+  const GradRoom room = count > 0 ? room_of(count, cols) : GradRoom{};
+  if (count > 0) {
+    if (!workspace || workspace_bytes < room.total) return FOG_ERR_WORKSPACE;
+    if (!aligned(workspace, 16)) return FOG_ERR_ALIGN;
+  }
+  hipStream_t s = (hipStream_t)stream;
+  uint8_t* ws = reinterpret_cast<uint8_t*>(workspace);
+  uint32_t *keys = reinterpret_cast<uint32_t*>(ws), *ids = reinterpret_cast<uint32_t*>(ws + room.keys);
+  uint32_t* positions = reinterpret_cast<uint32_t*>(ws + room.keys + room.order);
+  float* head = reinterpret_cast<float*>(ws + room.keys + 2 * room.order);
+  const int wide = token_bytes == 8;
+  if (count > 0) {
+    const int tiles = (int)((count + SORT_TILE - 1) / SORT_TILE);
+    sort_tiles_kernel<<<tiles, SORT_TILE / 2, 0, s>>>(tokens, wide, count, vocab, keys, ids, positions);
+    if (tiles > 1) merge_ranks_kernel<<<tiles, SORT_TILE, 0, s>>>(keys, count, tiles, ids, positions);
+  }
+  GradArgs a{};
+  a.ids = ids; a.positions = positions;
+  a.dx = reinterpret_cast<const uint16_t*>(dx_bf16);
+  a.dE = dE;
+  a.head = head;
+  a.tail = reinterpret_cast<float*>(ws + room.keys + 2 * room.order + room.pieces);
+  a.count = count; a.vocab = vocab; a.cols = cols; a.ld_dx = ld_dx; a.ld_dE = ld_dE;
+  a.factor = factor;
+  a.accumulate = accumulate != 0;
+  a.chunk = count > 0 ? chunk_of(count, cols) : 64;
+  a.slabs = (int)((cols + SLAB - 1) / SLAB);
+  a.chunks = (count + a.chunk - 1) / a.chunk;
+  a.units = a.chunks * a.slabs;
+  const int64_t waves = a.units + (accumulate ? 0 : (vocab + ZERO_ROWS - 1) / ZERO_ROWS);
+  const int64_t groups = (waves + kThreads / 64 - 1) / (kThreads / 64);
+  if (groups > 0x7FFFFFFF || a.units > 0x7FFFFFFF) return FOG_ERR_UNSUPPORTED;
+  const bool vec = cols % 8 == 0 && ld_dE % 8 == 0 && aligned(dE, 16) && (count == 0 || (ld_dx % 8 == 0 && aligned(dx_bf16, 16)));
+#define FOG_EG(F, V)                                                                            \
+  do {                                                                                          \
+    sum_runs_kernel<F, V><<<(int)groups, kThreads, 0, s>>>(a);                                  \
+    if (a.chunks > 1) join_runs_kernel<F, V><<<(int)a.units, kThreads, 0, s>>>(a);              \
+  } while (0)
+  if (type == FOG_F32) { if (vec) FOG_EG(true, true); else FOG_EG(true, false); }
+  else                 { if (vec) FOG_EG(false, true); else FOG_EG(false, false); }
+#undef FOG_EG
+  return fog_launch_status();
+}

@@ -20,11 +20,25 @@ struct GemmArgs {
   // floats in the register order of the accumulators
   int splits, k_chunk;
   float* partial;
+  // products with a scale for each block of 128 (sinv_a and sinv_b are NULL then): the scale byte of row or column i of the
+  // operand for contraction block b is s[(i >> shift) * i_stride + b * k_stride], blocks 0 .. k_blocks - 1
+  struct BlockScales {
+    const uint8_t* s;
+    uint32_t bytes, i_stride, k_stride;
+    int shift;
+  } sa, sb;
+  int k_blocks;
 };
 
-// Launches one of the small-tile kernels (gemm_tile_kernels.hip) on checked arguments.
+// Which kernel computes a product (gemm_kernels.hip); tile: GemmTile, or -1 for the 256 x 256 kernel.
+struct ProductPlan { int tile, splits, k_chunk; };
+
+// Launches one of the small-tile kernels (gemm_tile_kernels.hip) on checked arguments; with g.sa.s set its block-scaled form.
 enum GemmTile { TILE_256x128, TILE_128x128, TILE_128x128_2WG, TILE_64x64 };
 __attribute__((visibility("hidden"))) fog_status gemm_tile_launch(GemmTile tile, fog_layout layout, fog_fp8 fmt_a, fog_fp8 fmt_b, GemmArgs g, hipStream_t s);
+// Launches the kernel of block-scaled NT products with up to ROWS_MAX rows (gemm_rows_kernel.hip).
+constexpr int ROWS_MAX = 64;
+__attribute__((visibility("hidden"))) fog_status gemm_rows_launch(fog_fp8 fmt_a, fog_fp8 fmt_b, GemmArgs g, hipStream_t s);
 // Adds up the partial tiles of a split product whose tiles are 64 ti x 64 tj.
 __attribute__((visibility("hidden"))) void gemm_reduce_launch(const GemmArgs& g, int ti, int tj, hipStream_t s);
 
@@ -42,6 +56,14 @@ typedef __attribute__((address_space(3))) v2i* lds_v2i_ptr;
 // awaited explicitly with s_waitcnt vmcnt + barrier in the main loop.
 FOG_DEVICE void load_to_lds(v4i rsrc, uint32_t voff, uint32_t lds_addr_uniform) {
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
+               :
+               : "v"(voff), "s"(rsrc), "s"(lds_addr_uniform)
+               : "memory", "m0");
+}
+
+// The same for one byte per lane, zero-extended to LDS[m0 + 4 * lane].
+FOG_DEVICE void load_byte_to_lds(v4i rsrc, uint32_t voff, uint32_t lds_addr_uniform) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_ubyte %0, %1, 0 offen lds"
                :
                : "v"(voff), "s"(rsrc), "s"(lds_addr_uniform)
                : "memory", "m0");

@@ -51,6 +51,10 @@ constexpr int EPI_STRIDE = 64 + 16;           // epilogue staging: 32 rows x 32 
 constexpr int EPI_BUF = 32 * EPI_STRIDE;      // one staged block
 constexpr int EPI_BYTES = 2 * EPI_BUF;        // per wave: two blocks
 constexpr int LDS_BYTES = RING_BYTES + 4 * EPI_BYTES;  // 151552
+// Block-scaled products: behind all that, per pair stage a dword for each of the 256 rows of A and columns of B (the scale byte of
+// the stage's 128 contraction indices: a pair stage is one block).
+constexpr int SCALES_OPERAND = 256 * 4, SCALES_STAGE = 2 * SCALES_OPERAND;
+constexpr int LDS_BYTES_BLOCKS = LDS_BYTES + 2 * SCALES_STAGE;  // 155648
 
 // Per-thread state of one operand's direct loads.  A wave fetches 8 pieces of 1 KB per pair of
 // K-steps; piece j of wave w lands at byte 8192 w + 1024 j of the operand's pair stage.  The
@@ -209,7 +213,11 @@ FOG_DEVICE void tile_origin(int logical, int tiles_m, int tiles_n, int& m0, int&
 // PRODUCTS_ONLY (measurement helper fog_probe_gemm_products_only, never the product path): interior tiles skip
 // their epilogue, so that the launch shows what the conversion, staging and stores of the finished tiles cost.
 // SPLIT: the work items are (tile, contraction chunk) pairs, and the epilogue leaves the binary32 accumulators in the workspace.
-template <int LAYOUT, int FA, int FB, bool SPLIT, bool PRODUCTS_ONLY = false>
+// BLOCKS: every 128 contraction indices of a row of A or column of B have a scale byte of their own, 2^(byte - 127), that the matrix
+// instruction applies (a lane's 32 contraction bytes take the byte in its own scale register; a pair stage is one block).  The bytes
+// travel beside the operands: one direct load of 64 of them per wave, operand and pair, read a step ahead like the fragments and
+// packed four to a register, whose byte the instruction selects.
+template <int LAYOUT, int FA, int FB, bool SPLIT, bool BLOCKS, bool PRODUCTS_ONLY = false>
 __global__ __launch_bounds__(kThreads) void fp8_gemm_kernel(GemmArgs g) {
   extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
   constexpr bool A_KM = LAYOUT == FOG_TN;
@@ -236,7 +244,45 @@ __global__ __launch_bounds__(kThreads) void fp8_gemm_kernel(GemmArgs g) {
     fb_addr.a[i] += RING_B;
     asm volatile("" : "+v"(fa_addr.a[i]), "+v"(fb_addr.a[i]));
   }
-  const float alpha = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int((*g.sinv_a) * (*g.sinv_b))));
+  const float alpha = BLOCKS ? 1.0f : __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int((*g.sinv_a) * (*g.sinv_b))));
+
+  // Block scales.  Waves 0 and 1 fetch the bytes of the tile's rows of A, waves 2 and 3 those of its columns of B, 128 each in two loads
+  // (so that a wave keeps one descriptor).  Rows past the matrix fetch whatever byte lies there, or zero behind the array: it scales
+  // rows of C that are not stored.
+  const v4i rsrc_s = BLOCKS ? make_rsrc(w < 2 ? g.sa.s : g.sb.s, w < 2 ? g.sa.bytes : g.sb.bytes) : v4i{};
+  const uint32_t lds_s = (uint32_t)__builtin_amdgcn_readfirstlane((int)((uint32_t)(uintptr_t)smem + LDS_BYTES + 512u * w));
+  const int smask = BLOCKS && (w < 2 ? g.sa.shift : g.sb.shift) == 0 ? 127 : 0;      // a byte for each of the 128, or one for all
+  const uint32_t sstep = BLOCKS ? (w < 2 ? g.sa.k_stride : g.sb.k_stride) : 0;
+  uint32_t soff = 0;                                        // offset of the next pair's first byte
+  int sleft = 0;                                            // pairs until the end of the chunk
+  uint32_t sa_x = 0, sb_x = 0, sa_y = 0, sb_y = 0;          // packed bytes of the wave's four row and column blocks: this pair's, the next one's
+  auto scales_of_tile = [&](int m0, int n0, int kb, int klen) {
+    const int first = (w < 2 ? m0 : n0) + 128 * (w & 1);
+    soff = (uint32_t)__builtin_amdgcn_readfirstlane((int)((uint32_t)(first >> (smask ? 0 : 7)) * (w < 2 ? g.sa.i_stride : g.sb.i_stride) +
+                                                             (uint32_t)(kb / PAIR_K) * sstep));
+    sleft = (klen + PAIR_K - 1) / PAIR_K;
+  };
+  // bytes of pairs past the chunk are zeros (2^-127) beside codes that are zeros
+  auto lane_anew = [&]() {            // made again each time: no register is kept for it
+    uint32_t lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+    asm volatile("" : "+v"(lane));
+    return lane;
+  };
+  auto issue_scales = [&](int stage) {
+    const uint32_t lane = lane_anew();
+    const uint32_t base = sleft > 0 ? soff : OOB;
+    load_byte_to_lds(rsrc_s, base + (lane & smask), lds_s + stage * SCALES_STAGE);
+    load_byte_to_lds(rsrc_s, base + ((lane + 64) & smask), lds_s + stage * SCALES_STAGE + 256);
+    soff += sstep;
+    --sleft;
+  };
+  auto packed_scales = [&](int first) {      // of rows or columns first + 32 i + lane % 32, i = 0 .. 3
+    const uint8_t* at = smem + LDS_BYTES + 4 * first + 4 * (lane_anew() & 31);
+    uint32_t v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const uint32_t*>(at + 128 * i);
+    return v[0] | v[1] << 8 | v[2] << 16 | v[3] << 24;
+  };
 
   v16f acc[4][4];   // written by the first K-step of every tile (zero accumulator input), never cleared
   v16f zero16;
@@ -262,16 +308,19 @@ __global__ __launch_bounds__(kThreads) void fp8_gemm_kernel(GemmArgs g) {
       FOG_LOAD_A(j, k0, ST);                                  \
       FOG_LOAD_B(j, k0, ST);                                  \
     }                                                         \
+    if (BLOCKS) issue_scales(ST);                             \
     advance(pa); advance(pb);                                 \
   } while (0)
 #define FOG_RA(i, ST, H) read_frag<A_KM>(smem + (ST) * OPERAND_BYTES, fa_addr, i, H)
 #define FOG_RB(j, ST, H) read_frag<B_KM>(smem + (ST) * OPERAND_BYTES, fb_addr, j, H)
-#define FOG_MFMA(j, FAI_, FB_, i) \
-  acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(FB_[j], FAI_, acc[i][j], FB, FA, 0, 0, 0, 0)
+  // (scale operands 0: the compiler takes the instruction without scales)
+#define FOG_MFMA(j, FAI_, FB_, i) FOG_MFMA_ON(acc[i][j], j, FAI_, FB_, i)
+#define FOG_MFMA_ON(C_, j, FAI_, FB_, i)                                                                                    \
+  acc[i][j] = BLOCKS ? __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(FB_[j], FAI_, C_, FB, FA, j, (int)sb_x, i, (int)sa_x) \
+                     : __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(FB_[j], FAI_, C_, FB, FA, 0, 0, 0, 0)
   // first K-step of a tile: the accumulator input is the constant 0, so the 256 accumulator registers
   // never have to be cleared between tiles
-#define FOG_MFMA_Z(j, FAI_, FB_, i) \
-  acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(FB_[j], FAI_, zero16, FB, FA, 0, 0, 0, 0)
+#define FOG_MFMA_Z(j, FAI_, FB_, i) FOG_MFMA_ON(zero16, j, FAI_, FB_, i)
 #define FOG_FENCE() __builtin_amdgcn_sched_barrier(0)
   // One K-step = 16 MFMAs on the fragments fetched one step earlier, dealt out with the LDS reads
   // of the next step's fragments and (second step of a pair) the 16 direct loads of the pair after
@@ -338,9 +387,17 @@ __global__ __launch_bounds__(kThreads) void fp8_gemm_kernel(GemmArgs g) {
     __syncthreads();                                                                               \
     FOG_STEP_BODY(1 - (ST), 0, FB_IN, FB_CUR, A3_IN, A3_CUR, FOG_L##ST, FOG_MFMA);                           \
     advance(pa); advance(pb);                                                                      \
+    if (BLOCKS) { sa_x = sa_y; sb_x = sb_y; }                                                      \
   } while (0)
-#define FOG_L0(n) do { if ((n) < 8) FOG_LOAD_A((n), k0_, 0); else FOG_LOAD_B((n) - 8, k0_, 0); } while (0)
-#define FOG_L1(n) do { if ((n) < 8) FOG_LOAD_A((n), k0_, 1); else FOG_LOAD_B((n) - 8, k0_, 1); } while (0)
+#define FOG_L0(n) do { if ((n) < 8) FOG_LOAD_A((n), k0_, 0); else FOG_LOAD_B((n) - 8, k0_, 0); FOG_SCALES(n, 0); } while (0)
+#define FOG_L1(n) do { if ((n) < 8) FOG_LOAD_A((n), k0_, 1); else FOG_LOAD_B((n) - 8, k0_, 1); FOG_SCALES(n, 1); } while (0)
+  // scale bytes in the second step of the pair in stage ST: the refill of that stage's, and those of the other stage to registers
+#define FOG_SCALES(n, ST)                                                                   \
+  do {                                                                                      \
+    if (BLOCKS && (n) == 0) issue_scales(ST);                                               \
+    if (BLOCKS && (n) == 6) sa_y = packed_scales((1 - (ST)) * (SCALES_STAGE / 4) + wm);     \
+    if (BLOCKS && (n) == 10) sb_y = packed_scales((1 - (ST)) * (SCALES_STAGE / 4) + 256 + wn);\
+  } while (0)
 
   // The load stream runs ahead of the MFMAs across tile boundaries: during the last four steps of a
   // tile the first two pairs of the workgroup's next tile are already being fetched, so a new tile
@@ -349,11 +406,17 @@ __global__ __launch_bounds__(kThreads) void fp8_gemm_kernel(GemmArgs g) {
   item_range(walk.first);
   LoadPlan pa = A_KM ? plan_km(g.lda, m0, g.M, kb, klen) : plan_kc(g.lda, m0, g.M, kb, klen);
   LoadPlan pb = B_KM ? plan_km(g.ldb, n0, g.N, kb, klen) : plan_kc(g.ldb, n0, g.N, kb, klen);
+  if (BLOCKS) scales_of_tile(m0, n0, kb, klen);
   v8i fa[4], fa3, xb[4], yb[4];   // A fragments (row 3 twice), B fragments twice
   FOG_ISSUE_PAIR(0, 0);
   FOG_ISSUE_PAIR(PAIR_K, 1);
-  __builtin_amdgcn_s_waitcnt(0x4F70);  // vmcnt = 16: the first pair has landed
+  if (BLOCKS) __builtin_amdgcn_s_waitcnt(0x4F72);  // vmcnt = 18: the first pair and its scales have landed
+  else        __builtin_amdgcn_s_waitcnt(0x4F70);  // vmcnt = 16: the first pair has landed
   __syncthreads();
+  if (BLOCKS) {
+    sa_x = packed_scales(wm);
+    sb_x = packed_scales(256 + wn);
+  }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     fa[i] = FOG_RA(i, 0, 0);
@@ -375,7 +438,9 @@ __global__ __launch_bounds__(kThreads) void fp8_gemm_kernel(GemmArgs g) {
         item_range(next);                                                                            \
         pa = A_KM ? plan_km(g.lda, m0, g.M, kb, klen) : plan_kc(g.lda, m0, g.M, kb, klen);           \
         pb = B_KM ? plan_km(g.ldb, n0, g.N, kb, klen) : plan_kc(g.ldb, n0, g.N, kb, klen);           \
+        if (BLOCKS) scales_of_tile(m0, n0, kb, klen);                                                \
       } else {                                                                                       \
+        sleft = 0;                                                                                   \
         pa.off[0] = pa.off[1] = pb.off[0] = pb.off[1] = OOB;                                         \
       }                                                                                              \
     }                                                                                                \
@@ -510,6 +575,7 @@ __global__ __launch_bounds__(kThreads) void fp8_gemm_kernel(GemmArgs g) {
 #undef FOG_RA
 #undef FOG_RB
 #undef FOG_MFMA
+#undef FOG_MFMA_ON
 #undef FOG_MFMA_Z
 #undef FOG_STEP_FIRST_Z
 #undef FOG_FENCE
@@ -519,6 +585,7 @@ __global__ __launch_bounds__(kThreads) void fp8_gemm_kernel(GemmArgs g) {
 #undef FOG_STEP_SECOND
 #undef FOG_L0
 #undef FOG_L1
+#undef FOG_SCALES
 }
 
 // C = 0 for K == 0 (no contraction): bf16 zeros.
@@ -587,7 +654,6 @@ constexpr TileCost kTileCost[] = {
     {128, 128, 2, 2.53, 0.40, 0.70, 0.66, 0.91, 0.29, 0.0, 0.0},     // TILE_128x128_2WG: not split
     {64, 64, 2, 1.40, 0.107, 0.206, 0.33, 0.383, 0.26, 4.3, 13.4},   // TILE_64x64
 };
-struct ProductPlan { int tile, splits, k_chunk; };   // tile: GemmTile, or -1 for the 256 x 256 kernel
 ProductPlan plan_product(fog_layout layout, int64_t M, int64_t N, int64_t K, size_t room, int cus) {
   ProductPlan best{-1, 1, (int)K};
   const int64_t tiles = ((M + BM - 1) / BM) * ((N + BN - 1) / BN);
@@ -638,21 +704,23 @@ ProductPlan plan_product(fog_layout layout, int64_t M, int64_t N, int64_t K, siz
   return best;
 }
 
-template <int LAYOUT, int FA, int FB, bool SPLIT>
+template <int LAYOUT, int FA, int FB, bool SPLIT, bool BLOCKS>
 fog_status launch(const GemmArgs& g, hipStream_t s) {
+  constexpr int LDS = BLOCKS ? LDS_BYTES_BLOCKS : LDS_BYTES;
   static bool configured = false;  // per instantiation; the attribute is sticky for the process
   if (!configured) {
-    if (hipFuncSetAttribute(reinterpret_cast<const void*>(fp8_gemm_kernel<LAYOUT, FA, FB, SPLIT>), hipFuncAttributeMaxDynamicSharedMemorySize, LDS_BYTES) != hipSuccess)
+    if (hipFuncSetAttribute(reinterpret_cast<const void*>(fp8_gemm_kernel<LAYOUT, FA, FB, SPLIT, BLOCKS>), hipFuncAttributeMaxDynamicSharedMemorySize, LDS) != hipSuccess)
       return FOG_ERR_HIP;
     configured = true;
   }
-  fp8_gemm_kernel<LAYOUT, FA, FB, SPLIT><<<persistent_grid((int64_t)g.tiles_m * g.tiles_n * g.splits, fog_compute_units()), kThreads, LDS_BYTES, s>>>(g);
+  fp8_gemm_kernel<LAYOUT, FA, FB, SPLIT, BLOCKS><<<persistent_grid((int64_t)g.tiles_m * g.tiles_n * g.splits, fog_compute_units()), kThreads, LDS, s>>>(g);
   if (SPLIT) gemm_reduce_launch(g, 4, 4, s);
   return fog_launch_status();
 }
 template <int LAYOUT, int FA, int FB>
 fog_status launch(const GemmArgs& g, hipStream_t s) {
-  return g.splits > 1 ? launch<LAYOUT, FA, FB, true>(g, s) : launch<LAYOUT, FA, FB, false>(g, s);
+  if (g.sa.s) return g.splits > 1 ? launch<LAYOUT, FA, FB, true, true>(g, s) : launch<LAYOUT, FA, FB, false, true>(g, s);
+  return g.splits > 1 ? launch<LAYOUT, FA, FB, true, false>(g, s) : launch<LAYOUT, FA, FB, false, false>(g, s);
 }
 
 template <int LAYOUT>
@@ -670,17 +738,10 @@ extern "C" size_t fog_fp8_gemm_workspace(fog_layout, int64_t M, int64_t N, int64
   return split_room(M, N, K, fog_compute_units());
 }
 
-extern "C" fog_status fog_fp8_gemm(fog_layout layout, int64_t M, int64_t N, int64_t K,
-                                   const uint8_t* A, fog_fp8 fmtA, int64_t lda, const float* scale_inv_A,
-                                   const uint8_t* B, fog_fp8 fmtB, int64_t ldb, const float* scale_inv_B,
-                                   void* C_bf16, int64_t ldc, void* workspace, size_t workspace_bytes, void* stream) {
-  if (M < 0 || N < 0 || K < 0) return FOG_ERR_SHAPE;
-  if (layout != FOG_NT && layout != FOG_NN && layout != FOG_TN) return FOG_ERR_UNSUPPORTED;
-  if ((fmtA != FOG_E4M3 && fmtA != FOG_E5M2) || (fmtB != FOG_E4M3 && fmtB != FOG_E5M2)) return FOG_ERR_UNSUPPORTED;
-  if (M == 0 || N == 0) return FOG_OK;
-  if (!C_bf16 || !scale_inv_A || !scale_inv_B) return FOG_ERR_NULL;
-  if (K > 0 && (!A || !B)) return FOG_ERR_NULL;
-  if (M > 0x7FFFFF00 || N > 0x7FFFFF00 || K > 0x7FFFFF00) return FOG_ERR_UNSUPPORTED;
+// A product on arguments of either entry point whose scales are in order (g.sinv_* or g.sa, g.sb are filled in).
+static fog_status run_product(GemmArgs g, fog_layout layout, int64_t M, int64_t N, int64_t K, const uint8_t* A, fog_fp8 fmtA, int64_t lda,
+                              const uint8_t* B, fog_fp8 fmtB, int64_t ldb, void* C_bf16, int64_t ldc, void* workspace, size_t workspace_bytes,
+                              hipStream_t s) {
   // row lengths of the stored operands
   const int64_t a_cols = layout == FOG_TN ? M : K;
   const int64_t b_cols = layout == FOG_NT ? K : N;
@@ -689,9 +750,7 @@ extern "C" fog_status fog_fp8_gemm(fog_layout layout, int64_t M, int64_t N, int6
   if (K > 0 && (a_cols % 16 != 0 || b_cols % 16 != 0)) return FOG_ERR_UNSUPPORTED;
   if (K > 0 && (!aligned(A, 16) || !aligned(B, 16) || lda % 16 != 0 || ldb % 16 != 0)) return FOG_ERR_ALIGN;
   if (!aligned(C_bf16, 2)) return FOG_ERR_ALIGN;
-  GemmArgs g;
   g.A = A; g.B = B; g.C = reinterpret_cast<uint16_t*>(C_bf16);
-  g.sinv_a = scale_inv_A; g.sinv_b = scale_inv_B;
   g.lda = lda; g.ldb = ldb; g.ldc = ldc;
   g.M = (int)M; g.N = (int)N; g.K = (int)K;
   g.tiles_m = (int)((M + BM - 1) / BM);
@@ -705,13 +764,13 @@ extern "C" fog_status fog_fp8_gemm(fog_layout layout, int64_t M, int64_t N, int6
   if (a_span >= 0x7FFFFFFF || b_span >= 0x7FFFFFFF) return FOG_ERR_UNSUPPORTED;  // 32-bit buffer offsets
   g.a_bytes = (uint32_t)a_span; g.b_bytes = (uint32_t)b_span;
   g.splits = 1; g.k_chunk = (int)K; g.partial = nullptr;
-  hipStream_t s = (hipStream_t)stream;
   if (K == 0) {
     int64_t blocks = (M * N + 255) / 256;
     if (blocks > 4096) blocks = 4096;
     gemm_zero_kernel<<<(int)blocks, 256, 0, s>>>(g.C, ldc, g.M, g.N);
     return fog_launch_status();
   }
+  if (g.sa.s && layout == FOG_NT && M <= ROWS_MAX) return gemm_rows_launch(fmtA, fmtB, g, s);
   // the contraction is only split when the caller brought the room that the workspace query names
   size_t room = 0;
   if (workspace && aligned(workspace, 16)) {
@@ -728,6 +787,61 @@ extern "C" fog_status fog_fp8_gemm(fog_layout layout, int64_t M, int64_t N, int6
     case FOG_NN: return launch_fmt<FOG_NN>(g, fmtA, fmtB, s);
     default: return launch_fmt<FOG_TN>(g, fmtA, fmtB, s);
   }
+}
+
+extern "C" fog_status fog_fp8_gemm(fog_layout layout, int64_t M, int64_t N, int64_t K,
+                                   const uint8_t* A, fog_fp8 fmtA, int64_t lda, const float* scale_inv_A,
+                                   const uint8_t* B, fog_fp8 fmtB, int64_t ldb, const float* scale_inv_B,
+                                   void* C_bf16, int64_t ldc, void* workspace, size_t workspace_bytes, void* stream) {
+  if (M < 0 || N < 0 || K < 0) return FOG_ERR_SHAPE;
+  if (layout != FOG_NT && layout != FOG_NN && layout != FOG_TN) return FOG_ERR_UNSUPPORTED;
+  if ((fmtA != FOG_E4M3 && fmtA != FOG_E5M2) || (fmtB != FOG_E4M3 && fmtB != FOG_E5M2)) return FOG_ERR_UNSUPPORTED;
+  if (M == 0 || N == 0) return FOG_OK;
+  if (!C_bf16 || !scale_inv_A || !scale_inv_B) return FOG_ERR_NULL;
+  if (K > 0 && (!A || !B)) return FOG_ERR_NULL;
+  if (M > 0x7FFFFF00 || N > 0x7FFFFF00 || K > 0x7FFFFF00) return FOG_ERR_UNSUPPORTED;
+  GemmArgs g{};
+  g.sinv_a = scale_inv_A; g.sinv_b = scale_inv_B;
+  return run_product(g, layout, M, N, K, A, fmtA, lda, B, fmtB, ldb, C_bf16, ldc, workspace, workspace_bytes, (hipStream_t)stream);
+}
+
+extern "C" size_t fog_fp8_gemm_block_workspace(fog_layout layout, int64_t M, int64_t N, int64_t K) { return fog_fp8_gemm_workspace(layout, M, N, K); }
+
+// Scale bytes of an operand whose element (i, k) is stored at row i (i_is_row) or at row k.  false: the leading dimension is too short.
+static bool block_scales(GemmArgs::BlockScales* out, fog_block block, const uint8_t* s, int64_t lds, int64_t extent, int64_t k_blocks, bool i_is_row,
+                         fog_status* why) {
+  const int64_t tiles = (extent + 127) / 128;
+  const bool tile = block == FOG_BLOCK_TILE;
+  const int64_t row = tile ? (i_is_row ? k_blocks : tiles) : extent, rows = tile && i_is_row ? tiles : k_blocks;
+  if (lds < row) { *why = FOG_ERR_SHAPE; return false; }
+  if ((rows - 1) * lds + row >= 0x7FFFFFFF) { *why = FOG_ERR_UNSUPPORTED; return false; }   // 32-bit buffer offsets
+  out->s = s;
+  out->bytes = (uint32_t)((rows - 1) * lds + row);
+  out->shift = tile ? 7 : 0;
+  out->i_stride = (uint32_t)(tile && i_is_row ? lds : 1);
+  out->k_stride = (uint32_t)(tile && i_is_row ? 1 : lds);
+  return true;
+}
+
+extern "C" fog_status fog_fp8_gemm_block(fog_layout layout, int64_t M, int64_t N, int64_t K,
+                                         const uint8_t* A, fog_fp8 fmtA, int64_t lda, fog_block blockA, const uint8_t* sA, int64_t ldsA,
+                                         const uint8_t* B, fog_fp8 fmtB, int64_t ldb, fog_block blockB, const uint8_t* sB, int64_t ldsB,
+                                         void* C_bf16, int64_t ldc, void* workspace, size_t workspace_bytes, void* stream) {
+  if (M < 0 || N < 0 || K < 0) return FOG_ERR_SHAPE;
+  if (layout != FOG_NT && layout != FOG_NN && layout != FOG_TN) return FOG_ERR_UNSUPPORTED;
+  if ((fmtA != FOG_E4M3 && fmtA != FOG_E5M2) || (fmtB != FOG_E4M3 && fmtB != FOG_E5M2)) return FOG_ERR_UNSUPPORTED;
+  if ((blockA != FOG_BLOCK_VECTOR && blockA != FOG_BLOCK_TILE) || (blockB != FOG_BLOCK_VECTOR && blockB != FOG_BLOCK_TILE)) return FOG_ERR_UNSUPPORTED;
+  if (M == 0 || N == 0) return FOG_OK;
+  if (!C_bf16) return FOG_ERR_NULL;
+  if (K > 0 && (!A || !B || !sA || !sB)) return FOG_ERR_NULL;
+  if (M > 0x7FFFFF00 || N > 0x7FFFFF00 || K > 0x7FFFFF00) return FOG_ERR_UNSUPPORTED;
+  GemmArgs g{};
+  g.k_blocks = (int)((K + PAIR_K - 1) / PAIR_K);
+  fog_status why = FOG_OK;
+  if (K > 0 && (!block_scales(&g.sa, blockA, sA, ldsA, M, g.k_blocks, layout != FOG_TN, &why) ||
+                !block_scales(&g.sb, blockB, sB, ldsB, N, g.k_blocks, layout == FOG_NT, &why)))
+    return why;
+  return run_product(g, layout, M, N, K, A, fmtA, lda, B, fmtB, ldb, C_bf16, ldc, workspace, workspace_bytes, (hipStream_t)stream);
 }
 
 // Host-only helper (include/fog_probe.h): the choice above without a launch.
@@ -754,7 +868,7 @@ extern "C" fog_status fog_probe_gemm_products_only(int64_t M, int64_t N, int64_t
   if (M % BM != 0 || N % BN != 0 || K % 16 != 0 || M > 0x7FFFFF00 || N > 0x7FFFFF00 || K > 0x7FFFFF00) return FOG_ERR_UNSUPPORTED;
   if (lda < K || ldb < K || ldc < N) return FOG_ERR_SHAPE;
   if (!aligned(A, 16) || !aligned(B, 16) || lda % 16 != 0 || ldb % 16 != 0 || !aligned(C_bf16, 16) || ldc % 8 != 0) return FOG_ERR_ALIGN;
-  GemmArgs g;
+  GemmArgs g{};
   g.A = A; g.B = B; g.C = reinterpret_cast<uint16_t*>(C_bf16);
   g.sinv_a = scale_inv_A; g.sinv_b = scale_inv_B;
   g.lda = lda; g.ldb = ldb; g.ldc = ldc;
@@ -768,10 +882,10 @@ extern "C" fog_status fog_probe_gemm_products_only(int64_t M, int64_t N, int64_t
   g.splits = 1; g.k_chunk = (int)K; g.partial = nullptr;
   static bool configured = false;
   if (!configured) {
-    if (hipFuncSetAttribute(reinterpret_cast<const void*>(fp8_gemm_kernel<FOG_NT, 0, 0, false, true>), hipFuncAttributeMaxDynamicSharedMemorySize, LDS_BYTES) != hipSuccess)
+    if (hipFuncSetAttribute(reinterpret_cast<const void*>(fp8_gemm_kernel<FOG_NT, 0, 0, false, false, true>), hipFuncAttributeMaxDynamicSharedMemorySize, LDS_BYTES) != hipSuccess)
       return FOG_ERR_HIP;
     configured = true;
   }
-  fp8_gemm_kernel<FOG_NT, 0, 0, false, true><<<persistent_grid((int64_t)g.tiles_m * g.tiles_n, fog_compute_units()), kThreads, LDS_BYTES, (hipStream_t)stream>>>(g);
+  fp8_gemm_kernel<FOG_NT, 0, 0, false, false, true><<<persistent_grid((int64_t)g.tiles_m * g.tiles_n, fog_compute_units()), kThreads, LDS_BYTES, (hipStream_t)stream>>>(g);
   return fog_launch_status();
 }

@@ -130,13 +130,18 @@ FOG_DEVICE void tile_origin(int logical, int tiles_m, int tiles_n, int bm, int b
 }
 
 // One workgroup of 4 waves (2 x 2) computes one tile of 64 TI x 64 TJ, a wave TI x TJ matrix tiles of 32 x 32.
-template <int LAYOUT, int FA, int FB, int TI, int TJ, int NST, int WPS>
+// BLOCKS: a scale byte for each 128 contraction indices of a row of A or column of B (see gemm_kernels.hip), a stage being one block.
+template <int LAYOUT, int FA, int FB, int TI, int TJ, int NST, int WPS, bool BLOCKS>
 __global__ __launch_bounds__(kThreads, WPS) void fp8_gemm_tile_kernel(GemmArgs g) {
   extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
   constexpr bool A_KM = LAYOUT == FOG_TN, B_KM = LAYOUT != FOG_NT;
   constexpr int A_BYTES = 64 * TI * PAIR_K, B_BYTES = 64 * TJ * PAIR_K;
   constexpr int RING_B = NST * A_BYTES;
-  constexpr int LOADS = 2 * TI + 2 * TJ;          // direct loads per wave and stage
+  constexpr int SCALES = NST * (A_BYTES + B_BYTES);        // block scales behind the ring: per stage a dword a row of A, then a column of B
+  constexpr int SCALES_STAGE = 4 * 64 * (TI + TJ);
+  constexpr int SCALE_LOADS = BLOCKS ? (TI + TJ + 3) / 4 : 0;
+  constexpr int LOADS = 2 * TI + 2 * TJ;          // direct loads of operands per wave and stage
+  constexpr int ALL_LOADS = LOADS + SCALE_LOADS;
   constexpr int NM = TI * TJ, NF = TI + TJ;       // matrix instructions and fragments per K-step
 
   // workgroups are dealt round-robin to the 8 XCDs: each takes one contiguous run of logical tile numbers
@@ -163,7 +168,40 @@ __global__ __launch_bounds__(kThreads, WPS) void fp8_gemm_tile_kernel(GemmArgs g
   Frags<B_KM, TJ> fb;
   fa.init(wm);
   fb.init(wn);
-  const float alpha = (*g.sinv_a) * (*g.sinv_b);
+  const float alpha = BLOCKS ? 1.0f : (*g.sinv_a) * (*g.sinv_b);
+
+  // The stage's TI + TJ groups of 64 scale bytes are dealt to the waves; where they do not come out even, some are fetched twice
+  // (the same bytes to the same place), so that every wave has as many loads in flight.
+  v4i rsrc_s[BLOCKS ? SCALE_LOADS : 1];
+  uint32_t soff[BLOCKS ? SCALE_LOADS : 1], sstep[BLOCKS ? SCALE_LOADS : 1], lds_s[BLOCKS ? SCALE_LOADS : 1];
+  const int sblock0 = kb / PAIR_K, sblock_end = (kb + klen + PAIR_K - 1) / PAIR_K;
+  if (BLOCKS) {
+#pragma unroll
+    for (int u = 0; u < SCALE_LOADS; ++u) {
+      const int group = __builtin_amdgcn_readfirstlane((w + 4 * u) % (TI + TJ));
+      const bool is_a = group < TI;
+      const GemmArgs::BlockScales sc = is_a ? g.sa : g.sb;
+      const int i = (is_a ? m0 + 64 * group : n0 + 64 * (group - TI)) + l;
+      rsrc_s[u] = make_rsrc(sc.s, sc.bytes);
+      soff[u] = i < (is_a ? g.M : g.N) ? (uint32_t)(i >> sc.shift) * sc.i_stride + (uint32_t)sblock0 * sc.k_stride : OOB;
+      sstep[u] = sc.k_stride;
+      lds_s[u] = lds0 + SCALES + 256u * group;
+    }
+  }
+  // scale bytes of stage p to its slot; past the chunk zeros (2^-127) beside codes that are zeros
+  auto load_scales = [&](int p, int slot) {
+#pragma unroll
+    for (int u = 0; u < SCALE_LOADS; ++u)
+      load_byte_to_lds(rsrc_s[u], sblock0 + p < sblock_end ? soff[u] + (uint32_t)p * sstep[u] : OOB,
+                       (uint32_t)__builtin_amdgcn_readfirstlane((int)(lds_s[u] + (uint32_t)slot * SCALES_STAGE)));
+  };
+  auto read_scales = [&](int slot, int* sa, int* sb) {
+    const uint8_t* at = smem + SCALES + slot * SCALES_STAGE + 4 * (l & 31);
+#pragma unroll
+    for (int i = 0; i < TI; ++i) sa[i] = *reinterpret_cast<const int*>(at + 4 * (wm + 32 * i));
+#pragma unroll
+    for (int j = 0; j < TJ; ++j) sb[j] = *reinterpret_cast<const int*>(at + 4 * (64 * TI + wn + 32 * j));
+  };
 
   v16f acc[TI][TJ];
 #pragma unroll
@@ -188,22 +226,25 @@ __global__ __launch_bounds__(kThreads, WPS) void fp8_gemm_tile_kernel(GemmArgs g
   for (int s = 0; s < NST; ++s) {
 #pragma unroll
     for (int t = 0; t < LOADS; ++t) load_piece(t, s * PAIR_K, s);
+    if (BLOCKS) load_scales(s, s);
     la.advance();
     lb.advance();
   }
-  __builtin_amdgcn_s_waitcnt(waitcnt((NST - 1) * LOADS, 15));   // stage 0 has landed
+  __builtin_amdgcn_s_waitcnt(waitcnt((NST - 1) * ALL_LOADS, 15));   // stage 0 has landed
   __syncthreads();
   v8i xa[2 * TI], xb[2 * TJ], ya[2 * TI], yb[2 * TJ];             // fragments of a whole stage (both K-steps), twice
 #pragma unroll
   for (int t = 0; t < 2 * NF; ++t) read_one(t, 0, xa, xb);
+  int xsa[TI], xsb[TJ], ysa[TI], ysb[TJ];                          // and its scale bytes
+  if (BLOCKS) read_scales(0, xsa, xsb);
 
   // Stage p, whose fragments are in ca / cb: the matrix instructions of its two K-steps, dealt out with the LDS reads of
   // the next stage's fragments (which have the rest of the stage to return) and the direct loads that refill its slot.
-  auto stage = [&](auto slot, int p, const v8i* ca, const v8i* cb, v8i* na, v8i* nb) {
+  auto stage = [&](auto slot, int p, const v8i* ca, const v8i* cb, v8i* na, v8i* nb, const int* csa, const int* csb, int* nsa, int* nsb) {
     constexpr int S = decltype(slot)::value, NEXT = (S + 1) % NST;
     // Stage p + 1 has landed (this wave's share: the younger stages may be in flight) and this wave has its fragments of
     // stage p; after the barrier that holds for all four, and the slot of stage p is refilled with stage p + NST (zeros past the end).
-    __builtin_amdgcn_s_waitcnt(waitcnt((NST - 2) * LOADS, 0));
+    __builtin_amdgcn_s_waitcnt(waitcnt((NST - 2) * ALL_LOADS, 0));
     __syncthreads();
     const int k0 = (p + NST) * PAIR_K;
     constexpr int SLOTS = 2 * NM, READS_PER = NM > 1 ? 1 : 2;
@@ -211,13 +252,18 @@ __global__ __launch_bounds__(kThreads, WPS) void fp8_gemm_tile_kernel(GemmArgs g
     for (int n = 0; n < SLOTS; ++n) {
       const int h = n / NM, i = (n % NM) / TJ, j = n % TJ;
       __builtin_amdgcn_sched_barrier(0);
-      acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(cb[h * TJ + j], ca[h * TI + i], acc[i][j], FB, FA, 0, 0, 0, 0);
+      acc[i][j] = BLOCKS ? __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(cb[h * TJ + j], ca[h * TI + i], acc[i][j], FB, FA, 0, csb[j], 0, csa[i])
+                         : __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(cb[h * TJ + j], ca[h * TI + i], acc[i][j], FB, FA, 0, 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int t = n * READS_PER; t < (n + 1) * READS_PER; ++t)
         if (t < 2 * NF) read_one(t, NEXT, na, nb);
 #pragma unroll
       for (int t = n * LOADS / SLOTS; t < (n + 1) * LOADS / SLOTS; ++t) load_piece(t, k0, S);
+      if (BLOCKS && n == 0) {
+        read_scales(NEXT, nsa, nsb);
+        load_scales(p + NST, S);
+      }
     }
     __builtin_amdgcn_sched_barrier(0);
     la.advance();
@@ -228,8 +274,8 @@ __global__ __launch_bounds__(kThreads, WPS) void fp8_gemm_tile_kernel(GemmArgs g
   for (int p = 0; p < nst; p += UNROLL) {
 #define FOG_STAGE(U)                                                                        \
   if (UNROLL > (U) && ((U) == 0 || p + (U) < nst)) {                                        \
-    if ((U) % 2 == 0) stage(Int<(U) % NST>{}, p + (U), xa, xb, ya, yb);                     \
-    else              stage(Int<(U) % NST>{}, p + (U), ya, yb, xa, xb);                     \
+    if ((U) % 2 == 0) stage(Int<(U) % NST>{}, p + (U), xa, xb, ya, yb, xsa, xsb, ysa, ysb); \
+    else              stage(Int<(U) % NST>{}, p + (U), ya, yb, xa, xb, ysa, ysb, xsa, xsb); \
   }
     FOG_STAGE(0) FOG_STAGE(1) FOG_STAGE(2) FOG_STAGE(3) FOG_STAGE(4) FOG_STAGE(5)
 #undef FOG_STAGE
@@ -300,7 +346,7 @@ __global__ __launch_bounds__(kThreads) void gemm_tile_reduce_kernel(GemmArgs g, 
     const float4 v = src[(int64_t)c * ntiles * per_tile * 256];
     acc.x += v.x; acc.y += v.y; acc.z += v.z; acc.w += v.w;
   }
-  const float alpha = (*g.sinv_a) * (*g.sinv_b);
+  const float alpha = g.sinv_a ? (*g.sinv_a) * (*g.sinv_b) : 1.0f;   // block scales are in the partial sums already
   *reinterpret_cast<uint2*>(blk + (l & 31) * STRIDE + 16 * qd + 8 * (l >> 5)) =
       make_uint2(pack_bf16x2(acc.x * alpha, acc.y * alpha), pack_bf16x2(acc.z * alpha, acc.w * alpha));
   __syncthreads();
@@ -310,21 +356,26 @@ __global__ __launch_bounds__(kThreads) void gemm_tile_reduce_kernel(GemmArgs g, 
   }
 }
 
-template <int LAYOUT, int FA, int FB, int TI, int TJ, int NST, int WPS>
+template <int LAYOUT, int FA, int FB, int TI, int TJ, int NST, int WPS, bool BLOCKS>
 fog_status launch(GemmArgs g, hipStream_t s) {
-  constexpr int LDS = NST * 64 * (TI + TJ) * PAIR_K;
+  constexpr int LDS = NST * 64 * (TI + TJ) * (PAIR_K + (BLOCKS ? 4 : 0));
   g.tiles_m = (g.M + 64 * TI - 1) / (64 * TI);
   g.tiles_n = (g.N + 64 * TJ - 1) / (64 * TJ);
   static bool configured = false;  // per instantiation; the attribute is sticky for the process
   if (!configured) {
-    if (hipFuncSetAttribute(reinterpret_cast<const void*>(fp8_gemm_tile_kernel<LAYOUT, FA, FB, TI, TJ, NST, WPS>), hipFuncAttributeMaxDynamicSharedMemorySize, LDS) != hipSuccess)
+    if (hipFuncSetAttribute(reinterpret_cast<const void*>(fp8_gemm_tile_kernel<LAYOUT, FA, FB, TI, TJ, NST, WPS, BLOCKS>), hipFuncAttributeMaxDynamicSharedMemorySize, LDS) != hipSuccess)
       return FOG_ERR_HIP;
     configured = true;
   }
   const int grid = 8 * ((g.tiles_m * g.tiles_n * g.splits + 7) / 8);
-  fp8_gemm_tile_kernel<LAYOUT, FA, FB, TI, TJ, NST, WPS><<<grid, kThreads, LDS, s>>>(g);
+  fp8_gemm_tile_kernel<LAYOUT, FA, FB, TI, TJ, NST, WPS, BLOCKS><<<grid, kThreads, LDS, s>>>(g);
   if (g.splits > 1) gemm_reduce_launch(g, TI, TJ, s);
   return fog_launch_status();
+}
+
+template <int LAYOUT, int FA, int FB, int TI, int TJ, int NST, int WPS>
+fog_status launch(const GemmArgs& g, hipStream_t s) {
+  return g.sa.s ? launch<LAYOUT, FA, FB, TI, TJ, NST, WPS, true>(g, s) : launch<LAYOUT, FA, FB, TI, TJ, NST, WPS, false>(g, s);
 }
 
 template <int LAYOUT, int FA, int FB>

@@ -11,6 +11,8 @@ import torch
 
 E4M3, E5M2 = 0, 1
 NT, NN, TN = 0, 1, 2
+VECTOR, TILE = 0, 1          # fog_block: how an operand's block scales lie
+BF16, F32 = 0, 1             # fog_real
 CAST_BATCH_MAX = 32          # FOG_CAST_BATCH_MAX of the header
 
 _LIB = None
@@ -43,6 +45,16 @@ SIGNATURES = {
     "fog_kurtosis": (_I, [_P, _I64, _I64, _I64, _P, _P, _P]),
     "fog_fp8_gemm": (_I, [_I, _I64, _I64, _I64, _P, _I, _I64, _P, _P, _I, _I64, _P, _P, _I64, _P, _SZ, _P]),
     "fog_fp8_gemm_workspace": (_SZ, [_I, _I64, _I64, _I64]),
+    "fog_quantize_block": (_I, [_P, _I64, _I64, _I64, _I, _I, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _P]),
+    "fog_quantize_tile": (_I, [_P, _I64, _I64, _I64, _I, _I, _P, _I64, _P, _I64, _P]),
+    "fog_fp8_gemm_block": (_I, [_I, _I64, _I64, _I64, _P, _I, _I64, _I, _P, _I64, _P, _I, _I64, _I, _P, _I64, _P, _I64, _P, _SZ, _P]),
+    "fog_fp8_gemm_block_workspace": (_SZ, [_I, _I64, _I64, _I64]),
+    "fog_embed_quantize": (_I, [_P, _I, _I64, _P, _I64, _I64, _I64, _F, _I, _P, _P, _I64, _P, _I64, _P, _P]),
+    "fog_embed_grad": (_I, [_P, _I, _I64, _P, _I64, _I64, _I64, _F, _I, _P, _I64, _I, _P, _SZ, _P]),
+    "fog_embed_grad_workspace": (_SZ, [_I64, _I64, _I64]),
+    "fog_grad_sumsq": (_I, [_P, _I, _P, _P, _SZ, _P]),
+    "fog_grad_sumsq_workspace": (_SZ, [_I]),
+    "fog_grad_clip": (_I, [_P, _I, _P, _F, _P, _P]),
     "fog_fp8_attn_fwd": (_I, [_I, _I, _I, _I, _I, _F, _I, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P]),
     "fog_fp8_attn_bwd": (_I, [_I, _I, _I, _I, _I, _F, _I, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P,
                               _P, _P, _P, _P, _P, _SZ, _P]),
@@ -263,6 +275,126 @@ def fp8_gemm(layout, M, N, K, A, fmt_a, sinv_a, B, fmt_b, sinv_b, C, workspace=N
 
 def fp8_gemm_workspace(layout, M, N, K):
     return load().fog_fp8_gemm_workspace(layout, M, N, K)
+
+
+BLOCK = 128                  # elements of a block scale
+
+
+def _matrix(t, what, rows, cols, size):
+    """Refuses a tensor that the pointer and leading dimension of the call would misdescribe."""
+    if t.dim() != 2 or t.shape[0] < rows or t.shape[1] < cols or t.element_size() != size or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("%s: a [%d, %d] matrix of %d-byte elements with contiguous rows is needed, got %s of %s with strides %s"
+                         % (what, rows, cols, size, tuple(t.shape), t.dtype, t.stride()))
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), cols)
+
+
+def _blocks(n):
+    return (n + BLOCK - 1) // BLOCK
+
+
+def quantize_block(x, fmt, q_row=None, s_row=None, q_col=None, s_col=None, margin=0, stream=None):
+    """Casts with a scale for each block of 128 along the rows (q_row, s_row), along the columns (q_col, s_col), or both in one pass."""
+    rows, cols = x.shape
+    ldx = _matrix(x, "x", rows, cols, 2)
+    ld = [0, 0, 0, 0]
+    if q_row is not None:
+        ld[0] = _matrix(q_row, "q_row", rows, cols, 1)
+    if s_row is not None:
+        ld[1] = _matrix(s_row, "s_row", _blocks(cols), rows, 1)
+    if q_col is not None:
+        ld[2] = _matrix(q_col, "q_col", rows, cols, 1)
+    if s_col is not None:
+        ld[3] = _matrix(s_col, "s_col", _blocks(rows), cols, 1)
+    _check(load().fog_quantize_block(_ptr(x), rows, cols, ldx, fmt, margin, _ptr(q_row), ld[0], _ptr(s_row), ld[1],
+                                     _ptr(q_col), ld[2], _ptr(s_col), ld[3], _stream(stream)), "fog_quantize_block")
+
+
+def quantize_tile(x, fmt, q, s, margin=0, stream=None):
+    """The cast with a scale for each tile of 128 x 128."""
+    rows, cols = x.shape
+    _check(load().fog_quantize_tile(_ptr(x), rows, cols, _matrix(x, "x", rows, cols, 2), fmt, margin, _ptr(q), _matrix(q, "q", rows, cols, 1),
+                                    _ptr(s), _matrix(s, "s", _blocks(rows), _blocks(cols), 1), _stream(stream)), "fog_quantize_tile")
+
+
+def fp8_gemm_block(layout, M, N, K, A, fmt_a, block_a, s_a, B, fmt_b, block_b, s_b, C, workspace=None, stream=None):
+    """fp8_gemm on operands with a scale for each block of 128 contraction indices; block_a, block_b: VECTOR or TILE."""
+    a_rows, a_cols = (K, M) if layout == TN else (M, K)
+    b_rows, b_cols = (N, K) if layout == NT else (K, N)
+    lda, ldb = _matrix(A, "A", a_rows, a_cols, 1), _matrix(B, "B", b_rows, b_cols, 1)
+    lds_a = _matrix(s_a, "s_a", *((_blocks(a_rows), _blocks(a_cols)) if block_a == TILE else (_blocks(K), M)), 1)
+    lds_b = _matrix(s_b, "s_b", *((_blocks(b_rows), _blocks(b_cols)) if block_b == TILE else (_blocks(K), N)), 1)
+    ws = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    _check(load().fog_fp8_gemm_block(layout, M, N, K, _ptr(A), fmt_a, lda, block_a, _ptr(s_a), lds_a, _ptr(B), fmt_b, ldb, block_b, _ptr(s_b), lds_b,
+                                     _ptr(C), _matrix(C, "C", M, N, 2), _ptr(workspace), ws, _stream(stream)), "fog_fp8_gemm_block")
+
+
+def fp8_gemm_block_workspace(layout, M, N, K):
+    return load().fog_fp8_gemm_block_workspace(layout, M, N, K)
+
+
+def _ids(tokens):
+    """Tokens as the calls take them: a contiguous vector of 4- or 8-byte integers."""
+    if tokens.dtype not in (torch.int32, torch.int64) or not tokens.is_contiguous():
+        raise ValueError("tokens: contiguous int32 or int64 ids are needed, got %s with strides %s" % (tokens.dtype, tokens.stride()))
+    return tokens.data_ptr(), tokens.element_size(), tokens.numel()
+
+
+def embed_quantize(tokens, table, factor, fmt, scale_t, x, q=None, amax_out=None, stream=None):
+    """x = bf16(factor * table[tokens]) with its FP8 cast and abs-max; tokens outside the table give rows of zeros."""
+    ids, size, count = _ids(tokens)
+    vocab, cols = table.shape
+    _check(load().fog_embed_quantize(ids, size, count, _ptr(table), vocab, cols, _matrix(table, "table", vocab, cols, 2), factor, fmt, _ptr(scale_t),
+                                     _ptr(x), _matrix(x, "x", count, cols, 2), _ptr(q), _matrix(q, "q", count, cols, 1) if q is not None else 0,
+                                     _ptr(amax_out), _stream(stream)), "fog_embed_quantize")
+
+
+def embed_grad(tokens, dx, factor, dE, workspace, accumulate=False, stream=None):
+    """dE[v] = factor * sum of dx[t] over the tokens t with id v (binary32 or bf16 dE, overwritten or added to)."""
+    ids, size, count = _ids(tokens)
+    vocab, cols = dE.shape
+    kind = F32 if dE.dtype == torch.float32 else BF16
+    _check(load().fog_embed_grad(ids, size, count, _ptr(dx), _matrix(dx, "dx", count, cols, 2), vocab, cols, factor, kind, _ptr(dE),
+                                 _matrix(dE, "dE", vocab, cols, 4 if kind == F32 else 2), int(accumulate),
+                                 _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)), "fog_embed_grad")
+
+
+def embed_grad_workspace(count, vocab, cols):
+    return load().fog_embed_grad_workspace(count, vocab, cols)
+
+
+class GradJob(ctypes.Structure):
+    """Mirror of fog_grad_job."""
+    _fields_ = [("g", _P), ("out", _P), ("n", _I64), ("type", _I)]
+
+
+def make_grad_jobs(items):
+    """items: gradients, or (gradient, clipped gradient) pairs, contiguous and in binary32 or 2-byte bfloat16 -> ctypes array for grad_sumsq
+    and grad_clip (built once, reused while the tensors stay in place).  A gradient by itself is clipped in place."""
+    arr = (GradJob * len(items))()
+    for job, item in zip(arr, items):
+        g, out = item if isinstance(item, (tuple, list)) else (item, item)
+        for t in (g, out):
+            if not t.is_contiguous() or t.dtype not in (torch.float32, torch.bfloat16, torch.int16) or t.dtype != g.dtype or t.numel() != g.numel():
+                raise ValueError("contiguous float32 or bfloat16 gradients are needed, with results of their size and type")
+        job.g, job.out, job.n, job.type = _ptr(g), _ptr(out), g.numel(), F32 if g.dtype == torch.float32 else BF16
+    return arr
+
+
+def grad_sumsq(jobs, sumsq, workspace, stream=None):
+    """sumsq (one float64): the sum of the squares of all gradients."""
+    if sumsq.dtype != torch.float64:
+        raise ValueError("sumsq: a float64 tensor is needed, got %s" % sumsq.dtype)
+    _check(load().fog_grad_sumsq(jobs, len(jobs), _ptr(sumsq), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)),
+           "fog_grad_sumsq")
+
+
+def grad_sumsq_workspace(count):
+    return load().fog_grad_sumsq_workspace(count)
+
+
+def grad_clip(jobs, sumsq, max_norm, norm=None, stream=None):
+    """out = g * min(1, max_norm / sqrt(sumsq)) for every job; norm: receives sqrt(sumsq)."""
+    _check(load().fog_grad_clip(jobs, len(jobs), _ptr(sumsq), max_norm, _ptr(norm), _stream(stream)), "fog_grad_clip")
 
 
 def fp8_attn_fwd(B, H, S, D, softmax_scale, causal, Q, K, V, sinv_q, sinv_k, sinv_v, scale_p, O, lse,
