@@ -6,13 +6,16 @@
 // Gradient: dE[v] = factor sum over the tokens t with id v of dx[t], in binary32 and in the order of the tokens.  The tokens are
 // sorted by id first, so that every sum is a run of the sorted order and no two writers meet: no atomics on sums, the same result on
 // every run.
-//   1. sort_tiles: a workgroup sorts 1024 tokens by (id, position) in LDS.
-//   2. merge_ranks: a token's place in the whole order is its place in its tile plus, for every other tile, the number of that tile's
-//      tokens before it (a binary search); stable, because earlier tiles count their equal ids and later ones do not.
-//   3. sum_runs: a wave adds `chunk` consecutive tokens of the order on 512 columns and writes each run that begins and ends in
-//      the chunk; what a run has in a chunk that it does not begin and end in goes to the workspace.  Other waves of the same
-//      launch write zeros to the rows of absent ids.
-//   4. join_runs: adds the pieces of the runs that cross chunks, in order.
+//   1. rank_tokens: up to RANK_MOST tokens.  A token's place is the number of tokens before it in the order, counted by comparing it with
+//      all of them; every workgroup places a few tokens, so that the whole chip counts.
+//      sort_tiles and merge_ranks: more tokens.  A workgroup sorts 1024 tokens by (id, position) in LDS; then a token's place is its
+//      place in its tile plus, for every other tile, the number of that tile's tokens before it (a binary search); stable, because earlier
+//      tiles count their equal ids and later ones do not.
+//      Further workgroups of these launches write zeros to the whole table's gradient, which is most of the work where the table has many
+//      more rows than there are tokens; looking up the rows that need none costs more than it saves (see fill_zeros).
+//   2. sum_runs: a wave adds `chunk` consecutive tokens of the order on 512 columns and writes each run that begins and ends in
+//      the chunk; what a run has in a chunk that it does not begin and end in goes to the workspace.
+//   3. join_runs: adds the pieces of the runs that cross chunks, in order.
 #include "common.h"
 #include "launch.h"
 
@@ -40,6 +43,22 @@ struct EmbedArgs {
   int lanes;    // threads of a row, a power of two
 };
 
+// Eight elements of a row of the table times the factor, rounded to bf16.
+FOG_DEVICE uint4 scaled_piece(uint4 v, float f) {
+  return make_uint4(pack_bf16x2(bf16lo(v.x) * f, bf16hi(v.x) * f), pack_bf16x2(bf16lo(v.y) * f, bf16hi(v.y) * f),
+                    pack_bf16x2(bf16lo(v.z) * f, bf16hi(v.z) * f), pack_bf16x2(bf16lo(v.w) * f, bf16hi(v.w) * f));
+}
+// Stores them with their codes; returns the running maximum.
+template <int FMT>
+FOG_DEVICE uint32_t store_piece(const EmbedArgs& a, int64_t r, int64_t c, uint4 v, float rho, uint32_t m) {
+  m = pkmax_abs_bf16(m, v.x); m = pkmax_abs_bf16(m, v.y); m = pkmax_abs_bf16(m, v.z); m = pkmax_abs_bf16(m, v.w);
+  st_nt16(a.x + r * a.ldx + c, v);
+  if (a.q)
+    st_nt8(a.q + r * a.ldq + c, make_uint2(cvt4_fp8_nan<FMT>(bf16lo(v.x) * rho, bf16hi(v.x) * rho, bf16lo(v.y) * rho, bf16hi(v.y) * rho),
+                                           cvt4_fp8_nan<FMT>(bf16lo(v.z) * rho, bf16hi(v.z) * rho, bf16lo(v.w) * rho, bf16hi(v.w) * rho)));
+  return m;
+}
+
 // VEC: rows of the table, of x and of q in pieces of eight elements.
 template <int FMT, bool VEC>
 __global__ __launch_bounds__(kThreads) void embed_kernel(EmbedArgs a) {
@@ -52,17 +71,7 @@ __global__ __launch_bounds__(kThreads) void embed_kernel(EmbedArgs a) {
     const uint16_t* e = a.table + (in ? id : 0) * a.ld_table;
     if (VEC) {
       for (int64_t c = 8 * (int64_t)lane; c < a.cols; c += 8 * (int64_t)a.lanes) {
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (in) {
-          v = *reinterpret_cast<const uint4*>(e + c);
-          v = make_uint4(pack_bf16x2(bf16lo(v.x) * a.factor, bf16hi(v.x) * a.factor), pack_bf16x2(bf16lo(v.y) * a.factor, bf16hi(v.y) * a.factor),
-                         pack_bf16x2(bf16lo(v.z) * a.factor, bf16hi(v.z) * a.factor), pack_bf16x2(bf16lo(v.w) * a.factor, bf16hi(v.w) * a.factor));
-        }
-        m = pkmax_abs_bf16(m, v.x); m = pkmax_abs_bf16(m, v.y); m = pkmax_abs_bf16(m, v.z); m = pkmax_abs_bf16(m, v.w);
-        st_nt16(a.x + r * a.ldx + c, v);
-        if (a.q)
-          st_nt8(a.q + r * a.ldq + c, make_uint2(cvt4_fp8_nan<FMT>(bf16lo(v.x) * rho, bf16hi(v.x) * rho, bf16lo(v.y) * rho, bf16hi(v.y) * rho),
-                                                 cvt4_fp8_nan<FMT>(bf16lo(v.z) * rho, bf16hi(v.z) * rho, bf16lo(v.w) * rho, bf16hi(v.w) * rho)));
+        m = store_piece<FMT>(a, r, c, in ? scaled_piece(*reinterpret_cast<const uint4*>(e + c), a.factor) : make_uint4(0, 0, 0, 0), rho, m);
       }
     } else {
       for (int64_t c = lane; c < a.cols; c += a.lanes) {
@@ -83,6 +92,46 @@ __global__ __launch_bounds__(kThreads) void embed_kernel(EmbedArgs a) {
   }
 }
 
+// Up to SMALL pieces of eight elements (a decoding step's tokens), with an abs-max: one workgroup, so that the abs-max needs no word that
+// a launch before has cleared.  All ids, then all pieces, are asked for before the first is used.
+constexpr int SMALL_THREADS = 1024, SMALL_PER = 8, SMALL = SMALL_THREADS * SMALL_PER;
+template <int FMT>
+__global__ __launch_bounds__(SMALL_THREADS) void embed_small_kernel(EmbedArgs a) {
+  const float rho = a.q ? *a.scale : 0.0f;
+  const int per_row = (int)(a.cols / 8), pieces = (int)a.count * per_row;
+  int row[SMALL_PER], at[SMALL_PER];
+  int64_t id[SMALL_PER];
+#pragma unroll
+  for (int u = 0; u < SMALL_PER; ++u) {
+    const int p = threadIdx.x + u * SMALL_THREADS;
+    row[u] = p / per_row;
+    at[u] = 8 * (p - row[u] * per_row);
+    id[u] = p < pieces ? token_at(a.tokens, a.wide, row[u]) : -1;
+  }
+  uint4 v[SMALL_PER];
+#pragma unroll
+  for (int u = 0; u < SMALL_PER; ++u) {
+    v[u] = make_uint4(0, 0, 0, 0);
+    if (id[u] >= 0 && id[u] < a.vocab) v[u] = *reinterpret_cast<const uint4*>(a.table + id[u] * a.ld_table + at[u]);
+    else                               id[u] = -1;
+  }
+  uint32_t m = 0u;
+#pragma unroll
+  for (int u = 0; u < SMALL_PER; ++u) {
+    if ((int)threadIdx.x + u * SMALL_THREADS >= pieces) break;
+    if (id[u] >= 0) v[u] = scaled_piece(v[u], a.factor);
+    m = store_piece<FMT>(a, row[u], at[u], v[u], rho, m);
+  }
+  m = wave_max_u32(max_of_pair(m));
+  __shared__ uint32_t part[SMALL_THREADS / 64];
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < SMALL_THREADS / 64; ++w) m = m > part[w] ? m : part[w];
+    *a.amax_out = m << 16;
+  }
+}
+
 // ---------------------------------------------------------------- gradient: order of the tokens
 constexpr int SORT_TILE = 1024;
 constexpr int POS_BITS = 10;
@@ -96,70 +145,163 @@ FOG_DEVICE uint32_t sort_key(const void* tokens, int wide, int64_t count, int64_
   return (uint32_t)((id >= 0 && id < vocab ? id : vocab) << POS_BITS) | (uint32_t)local;
 }
 
-// keys: tiles * SORT_TILE words.  With one tile the order is final: ids and positions are written instead.
-__global__ __launch_bounds__(SORT_TILE / 2) void sort_tiles_kernel(const void* tokens, int wide, int64_t count, int64_t vocab, uint32_t* keys, uint32_t* ids,
-                                                                  uint32_t* positions) {
-  __shared__ uint32_t k[SORT_TILE];
+// Zeros for the rows of dE, 4 KB a workgroup; contiguous rows count as one.
+struct Fill {
+  uint8_t* p;
+  int64_t row_bytes, ld_bytes;
+  int64_t first, units;       // units of 4 KB that this launch writes
+  uint32_t per_row;           // units of a row
+  int one_row, vec, size;
+};
+constexpr int FILL_UNIT = 16 * kThreads;
+// Small workgroups that each write 16 bytes a thread and end: 2.1 GB take 313 us this way, 356 with four stores a thread, 343 and 377
+// with workgroups of 1024 threads and one or two.  As one launch with the sums, which looked up what rows to leave out, the
+// zeros took 358 to 420, the whole call 433 to 469 us.
+FOG_DEVICE void fill_zeros(const Fill& f, int64_t group, int64_t groups) {
   const int t = threadIdx.x;
+  for (int64_t u = f.first + group; u < f.first + f.units; u += groups) {
+    int64_t row = 0, at = u * FILL_UNIT;
+    if (!f.one_row) {
+      row = (int64_t)((uint32_t)u / f.per_row);
+      at = (int64_t)((uint32_t)u - (uint32_t)row * f.per_row) * FILL_UNIT;
+    }
+    uint8_t* p = f.p + row * f.ld_bytes;
+    if (f.vec) {
+      if (at + 16 * t < f.row_bytes) *reinterpret_cast<uint4*>(p + at + 16 * t) = make_uint4(0, 0, 0, 0);
+    } else {
+      for (int i = t * f.size; i < FILL_UNIT; i += kThreads * f.size) {
+        if (at + i >= f.row_bytes) break;
+        if (f.size == 4) *reinterpret_cast<uint32_t*>(p + at + i) = 0u;
+        else             *reinterpret_cast<uint16_t*>(p + at + i) = 0;
+      }
+    }
+  }
+}
+
+// Places RANK_TOKENS tokens a workgroup.  The other tokens pass through LDS, RANK_BLOCK at a time; a quad of them is compared with a token
+// by one of the 16 lanes that share that token, and the lanes' counts are added at the end.
+constexpr int RANK_TOKENS = 16, RANK_BLOCK = 4096, RANK_MOST = 8192;
+__global__ __launch_bounds__(kThreads) void rank_tokens_kernel(const void* tokens, int wide, int count, int64_t vocab, uint32_t* ids, uint32_t* positions,
+                                                              int work, Fill fill) {
+  if ((int)blockIdx.x >= work) return fill_zeros(fill, (int)blockIdx.x - work, (int)gridDim.x - work);
+  __shared__ uint4 other[RANK_BLOCK / 4];
+  __shared__ int places[RANK_TOKENS];
+  constexpr int GROUPS = kThreads / RANK_TOKENS;
+  const int t = threadIdx.x, first = blockIdx.x * RANK_TOKENS, mine = first + t % RANK_TOKENS;
+  auto id_of = [&](int i) -> uint32_t {
+    if (i >= count) return 0xFFFFFFFFu;
+    const int64_t id = token_at(tokens, wide, i);
+    return (uint32_t)(id >= 0 && id < vocab ? id : vocab);
+  };
+  const uint32_t id = id_of(mine);
+  if (t < RANK_TOKENS) places[t] = 0;
+  int n = 0;
+  for (int base = 0; base < count; base += RANK_BLOCK) {
+    const int quads = min(RANK_BLOCK, count - base + 3) / 4;
+    __syncthreads();
+#pragma unroll 4
+    for (int i = t; i < 4 * quads; i += kThreads) reinterpret_cast<uint32_t*>(other)[i] = id_of(base + i);
+    __syncthreads();
+    for (int q = t / RANK_TOKENS; q < quads; q += GROUPS) {
+      const uint4 o = other[q];
+      const int at = base + 4 * q;
+      if ((unsigned)(at - first) < (unsigned)RANK_TOKENS) {   // among this workgroup's own tokens: by id, then by position
+        n += o.x < id || (o.x == id && at < mine);
+        n += o.y < id || (o.y == id && at + 1 < mine);
+        n += o.z < id || (o.z == id && at + 2 < mine);
+        n += o.w < id || (o.w == id && at + 3 < mine);
+      } else {
+        const uint32_t limit = id + (at < first ? 1u : 0u);    // tokens before these with the same id come first
+        n += o.x < limit;
+        n += o.y < limit;
+        n += o.z < limit;
+        n += o.w < limit;
+      }
+    }
+  }
+  atomicAdd(&places[t % RANK_TOKENS], n);
+  __syncthreads();
+  if (t < RANK_TOKENS && mine < count) {
+    ids[places[t]] = id;
+    positions[places[t]] = (uint32_t)mine;
+  }
+}
+
+// keys: tiles * SORT_TILE words.
+__global__ __launch_bounds__(kThreads) void sort_tiles_kernel(const void* tokens, int wide, int64_t count, int64_t vocab, uint32_t* keys, int work, Fill fill) {
+  if ((int)blockIdx.x >= work) return fill_zeros(fill, (int)blockIdx.x - work, (int)gridDim.x - work);
+  __shared__ uint32_t k[SORT_TILE];
   const int64_t base = (int64_t)blockIdx.x * SORT_TILE;
-  for (int i = t; i < SORT_TILE; i += SORT_TILE / 2) k[i] = sort_key(tokens, wide, count, vocab, base + i, i);
+  for (int i = threadIdx.x; i < SORT_TILE; i += kThreads) k[i] = sort_key(tokens, wide, count, vocab, base + i, i);
   for (int size = 2; size <= SORT_TILE; size *= 2)
     for (int stride = size / 2; stride > 0; stride /= 2) {
-      __syncthreads();
-      const int i = 2 * t - (t & (stride - 1)), j = i + stride;
-      const uint32_t x = k[i], y = k[j];
-      const bool up = (i & size) == 0;
-      if ((x > y) == up) {
-        k[i] = y;
-        k[j] = x;
+      // the pairs of 64 neighbouring t lie within 128 keys up to a stride of 64: a wave waits for the others only before and behind longer ones
+      if (stride >= 128 || (stride == 64 && size >= 256) || size == 2) __syncthreads();
+      else                                                             asm volatile("" ::: "memory");   // LDS serves a wave in order
+#pragma unroll
+      for (int t = threadIdx.x; t < SORT_TILE / 2; t += kThreads) {
+        const int i = 2 * t - (t & (stride - 1)), j = i + stride;
+        const uint32_t x = k[i], y = k[j];
+        const bool up = (i & size) == 0, turn = (x > y) == up;
+        k[i] = turn ? y : x;
+        k[j] = turn ? x : y;
       }
     }
   __syncthreads();
-  for (int i = t; i < SORT_TILE; i += SORT_TILE / 2) {
-    if (gridDim.x > 1) {
-      keys[base + i] = k[i];
-    } else if (i < count) {
-      ids[i] = k[i] >> POS_BITS;
-      positions[i] = k[i] & (SORT_TILE - 1);
-    }
-  }
+  for (int i = threadIdx.x; i < SORT_TILE; i += kThreads) keys[base + i] = k[i];
 }
 
-// Number of a sorted tile's keys below `limit`.
-FOG_DEVICE int keys_below(const uint32_t* tile, uint32_t limit) {
-  int at = 0;
+// Numbers of four sorted tiles' keys below `limit` (four searches at a time: each step of one waits for LDS).
+FOG_DEVICE int keys_below(const uint32_t (*tiles)[SORT_TILE], const uint32_t* limit) {
+  int at[4] = {0, 0, 0, 0};
 #pragma unroll
   for (int step = SORT_TILE / 2; step > 0; step /= 2)
-    if (tile[at + step - 1] < limit) at += step;
-  return at + (tile[at] < limit ? 1 : 0);
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (tiles[u][at[u] + step - 1] < limit[u]) at[u] += step;
+  int n = 0;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) n += at[u] + (tiles[u][at[u]] < limit[u] ? 1 : 0);
+  return n;
 }
 
-constexpr int MERGE_TILES = 16;    // tiles in LDS at a time
-__global__ __launch_bounds__(SORT_TILE) void merge_ranks_kernel(const uint32_t* __restrict__ keys, int64_t count, int tiles, uint32_t* __restrict__ ids,
-                                                                uint32_t* __restrict__ positions) {
-  __shared__ uint32_t k[MERGE_TILES][SORT_TILE];
-  const int mine = blockIdx.x, t = threadIdx.x;
-  const uint32_t key = keys[(int64_t)mine * SORT_TILE + t], id = key >> POS_BITS;
-  int64_t rank = t;
+// A workgroup for each quarter of a tile.
+constexpr int MERGE_TILES = 4;     // tiles in LDS at a time (16 KB: the workgroups that write zeros beside these are to fill the compute units)
+constexpr int MERGE_PARTS = SORT_TILE / kThreads;
+__global__ __launch_bounds__(kThreads) void merge_ranks_kernel(const uint32_t* __restrict__ keys, int64_t count, int tiles, uint32_t* __restrict__ ids,
+                                                              uint32_t* __restrict__ positions, int work, Fill fill) {
+  if ((int)blockIdx.x >= work) return fill_zeros(fill, (int)blockIdx.x - work, (int)gridDim.x - work);
+  __shared__ __attribute__((aligned(16))) uint32_t k[MERGE_TILES][SORT_TILE];
+  const int mine = blockIdx.x / MERGE_PARTS, in_tile = threadIdx.x + kThreads * (blockIdx.x % MERGE_PARTS);
+  const uint32_t key = keys[(int64_t)mine * SORT_TILE + in_tile], id = key >> POS_BITS;
+  int64_t rank = in_tile;
   for (int base = 0; base < tiles; base += MERGE_TILES) {
     const int n = min(MERGE_TILES, tiles - base);
     __syncthreads();
-    for (int b = 0; b < n; ++b) k[b][t] = keys[(int64_t)(base + b) * SORT_TILE + t];
+#pragma unroll 4
+    for (int i = threadIdx.x; i < n * (SORT_TILE / 4); i += kThreads)
+      reinterpret_cast<uint4*>(&k[0][0])[i] = reinterpret_cast<const uint4*>(keys + (int64_t)base * SORT_TILE)[i];
     __syncthreads();
-    for (int b = 0; b < n; ++b) {
-      const int tile = base + b;
-      if (tile == mine) continue;
-      // a key of an earlier tile with the same id comes first; one of a later tile does not (id + 1 of a token
-      // fits its bits; the padding behind the last tile's tokens sorts behind all of them and takes no place)
-      rank += keys_below(k[b], (tile < mine ? id + 1u : id) << POS_BITS);
+    for (int b = 0; b < n; b += 4) {
+      uint32_t limit[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int tile = base + b + u;
+        // a key of an earlier tile with the same id comes first; one of a later tile does not (id + 1 of a token fits its bits; the
+        // padding behind the last tile's tokens sorts behind all of them and takes no place).  No key of its own tile, or behind the
+        // last, lies below 0.
+        limit[u] = tile == mine || tile >= tiles ? 0u : (tile < mine ? id + 1u : id) << POS_BITS;
+      }
+      rank += keys_below(k + b, limit);
     }
   }
-  const int64_t pos = (int64_t)mine * SORT_TILE + (key & (SORT_TILE - 1));
   if (key != 0xFFFFFFFFu) {
     ids[rank] = id;
-    positions[rank] = (uint32_t)pos;
+    positions[rank] = (uint32_t)((int64_t)mine * SORT_TILE + (key & (SORT_TILE - 1)));
   }
 }
+
+__global__ __launch_bounds__(kThreads) void fill_kernel(Fill fill) { fill_zeros(fill, blockIdx.x, gridDim.x); }
 
 // ---------------------------------------------------------------- gradient: sums
 constexpr int SLAB = 512;    // columns of a wave
@@ -175,7 +317,7 @@ struct GradArgs {
   int chunk;                // tokens of a wave, a power of two up to 64
   int slabs;                // ceil(cols / SLAB)
   int64_t chunks;
-  int64_t units;            // waves of sums: chunks * slabs; waves behind them write zeros
+  int64_t units;            // waves: chunks * slabs
 };
 
 template <bool F32, bool VEC>
@@ -246,49 +388,11 @@ struct Row {
   }
 };
 
-// Is id among the sorted ids?
-FOG_DEVICE bool present(const uint32_t* ids, int64_t count, uint32_t id) {
-  int64_t lo = 0, hi = count;
-  while (lo < hi) {
-    const int64_t mid = (lo + hi) >> 1;
-    if (ids[mid] < id) lo = mid + 1;
-    else hi = mid;
-  }
-  return lo < count && ids[lo] == id;
-}
-
-constexpr int ZERO_ROWS = 16;    // rows of the table a wave looks up and clears
-
-template <bool F32, bool VEC>
-FOG_DEVICE void zero_rows(const GradArgs& a, int64_t group, int l) {
-  const int64_t first = group * ZERO_ROWS;
-  if (first >= a.vocab) return;
-  const int64_t row = first + (l & (ZERO_ROWS - 1));
-  const uint64_t there = __ballot(row >= a.vocab || present(a.ids, a.count, (uint32_t)row));
-  for (int i = 0; i < ZERO_ROWS; ++i) {
-    if (there >> i & 1) continue;
-    const int64_t at = (first + i) * a.ld_dE;
-    if (VEC) {
-      constexpr int E = F32 ? 4 : 8;
-      uint8_t* p = reinterpret_cast<uint8_t*>(a.dE) + at * (F32 ? 4 : 2);
-      for (int64_t c = (int64_t)E * l; c < a.cols; c += E * 64) st_nt16(p + c * (F32 ? 4 : 2), make_uint4(0, 0, 0, 0));
-    } else {
-      for (int64_t c = l; c < a.cols; c += 64) {
-        if (F32) reinterpret_cast<float*>(a.dE)[at + c] = 0.0f;
-        else     reinterpret_cast<uint16_t*>(a.dE)[at + c] = 0;
-      }
-    }
-  }
-}
-
 template <bool F32, bool VEC>
 __global__ __launch_bounds__(kThreads) void sum_runs_kernel(GradArgs a) {
   const int l = threadIdx.x & 63;
   const int64_t unit = (int64_t)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (unit >= a.units) {
-    if (!a.accumulate) zero_rows<F32, VEC>(a, unit - a.units, l);
-    return;
-  }
+  if (unit >= a.units) return;
   const int64_t c = unit / a.slabs, p0 = c * a.chunk;
   const int64_t col = (unit - c * a.slabs) * SLAB + 8 * l;
   const int n = a.cols - col >= 8 ? 8 : a.cols > col ? (int)(a.cols - col) : 0;
@@ -343,18 +447,18 @@ __global__ __launch_bounds__(kThreads) void join_runs_kernel(GradArgs a) {
   const uint32_t id = a.ids[next];
   if (id >= (uint32_t)a.vocab || a.ids[next - 1] != id) return;
   if (c * a.chunk > 0 && a.ids[c * a.chunk] == id && a.ids[c * a.chunk - 1] == id) return;      // begun before this chunk
-  // end of the run: first token behind it
-  int64_t lo = next, hi = a.count;
-  while (lo < hi) {
-    const int64_t mid = (lo + hi) >> 1;
-    if (a.ids[mid] <= id) lo = mid + 1;
-    else hi = mid;
+  // chunks c + 1 .. c + m begin with a token of the run and have a piece of it: 64 of them are looked at together
+  int64_t m = 0;
+  for (;;) {
+    const int64_t at = (c + 1 + m + (threadIdx.x & 63)) * a.chunk;
+    const uint64_t out = __ballot(at >= a.count || a.ids[at < a.count ? at : 0] != id);
+    m += out ? __builtin_ctzll(out) : 64;
+    if (out) break;
   }
-  const int64_t last = (lo - 1) / a.chunk, m = last - c;   // chunks c + 1 .. last have a head of this run
   const int w = threadIdx.x >> 6, l = threadIdx.x & 63;
   const int64_t col = ((int64_t)blockIdx.x - c * a.slabs) * SLAB + 8 * l;
   const int n = a.cols - col >= 8 ? 8 : a.cols > col ? (int)(a.cols - col) : 0;
-  const int64_t per = (m + 3) / 4, b = c + 1 + w * per, e = b + per < last + 1 ? b + per : last + 1;
+  const int64_t per = (m + 3) / 4, b = c + 1 + w * per, e = b + per < c + m + 1 ? b + per : c + m + 1;
   Row<F32, VEC> sum;
   sum.clear();
   if (w == 0) sum.add_floats(a.tail + c * a.cols + col, n);
@@ -388,12 +492,14 @@ GradRoom room_of(int64_t count, int64_t cols) {
   GradRoom r;
   const int64_t tiles = (count + SORT_TILE - 1) / SORT_TILE;
   const int chunk = chunk_of(count, cols);
-  r.keys = (size_t)tiles * SORT_TILE * 4;
+  r.keys = count > RANK_MOST ? (size_t)tiles * SORT_TILE * 4 : 0;
   r.order = ((size_t)count * 4 + 15) / 16 * 16;
   r.pieces = ((size_t)((count + chunk - 1) / chunk) * (size_t)cols * 4 + 15) / 16 * 16;
   r.total = r.keys + 2 * r.order + 2 * r.pieces;
   return r;
 }
+
+constexpr int64_t GROUPS_MAX = 1 << 23;    // workgroups of a launch: grids are counted in threads of 32 bits
 
 inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
@@ -413,12 +519,17 @@ extern "C" fog_status fog_embed_quantize(const void* tokens, int token_bytes, in
     if (!aligned(tokens, token_bytes) || !aligned(table_bf16, 2) || !aligned(x_bf16, 2)) return FOG_ERR_ALIGN;
   }
   hipStream_t s = (hipStream_t)stream;
-  if (amax_out) zero_u32e<<<1, 1, 0, s>>>(reinterpret_cast<uint32_t*>(amax_out));
-  if (!any) return amax_out ? fog_launch_status() : FOG_OK;
   EmbedArgs a{tokens, token_bytes == 8, count, vocab, cols, ld_table, ldx, ldq, reinterpret_cast<const uint16_t*>(table_bf16), factor, scale,
               reinterpret_cast<uint16_t*>(x_bf16), q, reinterpret_cast<uint32_t*>(amax_out), kThreads};
   const bool vec = cols % 8 == 0 && ld_table % 8 == 0 && ldx % 8 == 0 && aligned(table_bf16, 16) && aligned(x_bf16, 16) &&
                    (!q || (ldq % 8 == 0 && aligned(q, 8)));
+  if (any && amax_out && vec && cols <= 8 * SMALL && count * (cols / 8) <= SMALL) {
+    if (fmt == FOG_E4M3) embed_small_kernel<FOG_E4M3><<<1, SMALL_THREADS, 0, s>>>(a);
+    else                 embed_small_kernel<FOG_E5M2><<<1, SMALL_THREADS, 0, s>>>(a);
+    return fog_launch_status();
+  }
+  if (amax_out) zero_u32e<<<1, 1, 0, s>>>(reinterpret_cast<uint32_t*>(amax_out));
+  if (!any) return amax_out ? fog_launch_status() : FOG_OK;
   const int64_t pieces = vec ? cols / 8 : cols;
   while (a.lanes > 16 && a.lanes / 2 >= pieces) a.lanes /= 2;
   const int64_t per_wg = kThreads / a.lanes;
@@ -455,22 +566,14 @@ extern "C" fog_status fog_embed_grad(const void* tokens, int token_bytes, int64_
     if (!workspace || workspace_bytes < room.total) return FOG_ERR_WORKSPACE;
     if (!aligned(workspace, 16)) return FOG_ERR_ALIGN;
   }
-  hipStream_t s = (hipStream_t)stream;
   uint8_t* ws = reinterpret_cast<uint8_t*>(workspace);
   uint32_t *keys = reinterpret_cast<uint32_t*>(ws), *ids = reinterpret_cast<uint32_t*>(ws + room.keys);
   uint32_t* positions = reinterpret_cast<uint32_t*>(ws + room.keys + room.order);
-  float* head = reinterpret_cast<float*>(ws + room.keys + 2 * room.order);
-  const int wide = token_bytes == 8;
-  if (count > 0) {
-    const int tiles = (int)((count + SORT_TILE - 1) / SORT_TILE);
-    sort_tiles_kernel<<<tiles, SORT_TILE / 2, 0, s>>>(tokens, wide, count, vocab, keys, ids, positions);
-    if (tiles > 1) merge_ranks_kernel<<<tiles, SORT_TILE, 0, s>>>(keys, count, tiles, ids, positions);
-  }
   GradArgs a{};
   a.ids = ids; a.positions = positions;
   a.dx = reinterpret_cast<const uint16_t*>(dx_bf16);
   a.dE = dE;
-  a.head = head;
+  a.head = reinterpret_cast<float*>(ws + room.keys + 2 * room.order);
   a.tail = reinterpret_cast<float*>(ws + room.keys + 2 * room.order + room.pieces);
   a.count = count; a.vocab = vocab; a.cols = cols; a.ld_dx = ld_dx; a.ld_dE = ld_dE;
   a.factor = factor;
@@ -479,13 +582,43 @@ extern "C" fog_status fog_embed_grad(const void* tokens, int token_bytes, int64_
   a.slabs = (int)((cols + SLAB - 1) / SLAB);
   a.chunks = (count + a.chunk - 1) / a.chunk;
   a.units = a.chunks * a.slabs;
-  const int64_t waves = a.units + (accumulate ? 0 : (vocab + ZERO_ROWS - 1) / ZERO_ROWS);
-  const int64_t groups = (waves + kThreads / 64 - 1) / (kThreads / 64);
-  if (groups > 0x7FFFFFFF || a.units > 0x7FFFFFFF) return FOG_ERR_UNSUPPORTED;
+  if (a.units > GROUPS_MAX) return FOG_ERR_UNSUPPORTED;
   const bool vec = cols % 8 == 0 && ld_dE % 8 == 0 && aligned(dE, 16) && (count == 0 || (ld_dx % 8 == 0 && aligned(dx_bf16, 16)));
+  Fill fill{reinterpret_cast<uint8_t*>(dE), cols * size, ld_dE * size, 0, 0, (uint32_t)((cols * size + FILL_UNIT - 1) / FILL_UNIT), ld_dE == cols, vec, size};
+  int64_t units = accumulate ? 0 : vocab * fill.per_row;
+  if (fill.one_row) {
+    fill.row_bytes = vocab * cols * size;
+    units = accumulate ? 0 : (fill.row_bytes + FILL_UNIT - 1) / FILL_UNIT;
+  } else if (units > 0xFFFFFFFFll) {
+    return FOG_ERR_UNSUPPORTED;
+  }
+  hipStream_t s = (hipStream_t)stream;
+  const int wide = token_bytes == 8;
+  // the launches that put the tokens in order share the zeros
+  auto share = [&](int64_t first, int64_t n) {
+    fill.first = first;
+    fill.units = n;
+    return (int)(n < GROUPS_MAX ? n : GROUPS_MAX);
+  };
+  if (count == 0) {
+    const int groups = share(0, units);
+    fill_kernel<<<groups, kThreads, 0, s>>>(fill);
+    return fog_launch_status();
+  }
+  if (count <= RANK_MOST) {
+    const int work = (int)((count + RANK_TOKENS - 1) / RANK_TOKENS), groups = work + share(0, units);
+    rank_tokens_kernel<<<groups, kThreads, 0, s>>>(tokens, wide, (int)count, vocab, ids, positions, work, fill);
+  } else {
+    const int tiles = (int)((count + SORT_TILE - 1) / SORT_TILE);
+    int groups = tiles + share(0, units / 2);
+    sort_tiles_kernel<<<groups, kThreads, 0, s>>>(tokens, wide, count, vocab, keys, tiles, fill);
+    groups = tiles * MERGE_PARTS + share(units / 2, units - units / 2);
+    merge_ranks_kernel<<<groups, kThreads, 0, s>>>(keys, count, tiles, ids, positions, tiles * MERGE_PARTS, fill);
+  }
+  const int groups = (int)((a.units + kThreads / 64 - 1) / (kThreads / 64));
 #define FOG_EG(F, V)                                                                            \
   do {                                                                                          \
-    sum_runs_kernel<F, V><<<(int)groups, kThreads, 0, s>>>(a);                                  \
+    sum_runs_kernel<F, V><<<groups, kThreads, 0, s>>>(a);                                       \
     if (a.chunks > 1) join_runs_kernel<F, V><<<(int)a.units, kThreads, 0, s>>>(a);              \
   } while (0)
   if (type == FOG_F32) { if (vec) FOG_EG(true, true); else FOG_EG(true, false); }
