@@ -178,45 +178,48 @@ FOG_DEVICE void fill_zeros(const Fill& f, int64_t group, int64_t groups) {
   }
 }
 
-// Places RANK_TOKENS tokens a workgroup.  The other tokens pass through LDS, RANK_BLOCK at a time; a quad of them is compared with a token
-// by one of the 16 lanes that share that token, and the lanes' counts are added at the end.
-constexpr int RANK_TOKENS = 16, RANK_BLOCK = 4096, RANK_MOST = 8192;
+// Places RANK_TOKENS tokens a workgroup.  All tokens are in LDS; a quad of them is compared with a token by one of the 16 lanes that share
+// that token, and the lanes' counts are added at the end.  One launch, where sorting takes two, but work that grows with the square of the
+// tokens: whole calls on 512 columns by ranking and by sorting, us: 1024 tokens 16.1 and 19.0, 2048 18.1 and 19.1, 3000 20.6 and 19.6.
+constexpr int RANK_TOKENS = 16, RANK_MOST = 2048;
 __global__ __launch_bounds__(kThreads) void rank_tokens_kernel(const void* tokens, int wide, int count, int64_t vocab, uint32_t* ids, uint32_t* positions,
                                                               int work, Fill fill) {
   if ((int)blockIdx.x >= work) return fill_zeros(fill, (int)blockIdx.x - work, (int)gridDim.x - work);
-  __shared__ uint4 other[RANK_BLOCK / 4];
+  __shared__ uint4 other[RANK_MOST / 4];
   __shared__ int places[RANK_TOKENS];
-  constexpr int GROUPS = kThreads / RANK_TOKENS;
-  const int t = threadIdx.x, first = blockIdx.x * RANK_TOKENS, mine = first + t % RANK_TOKENS;
-  auto id_of = [&](int i) -> uint32_t {
-    if (i >= count) return 0xFFFFFFFFu;
-    const int64_t id = token_at(tokens, wide, i);
-    return (uint32_t)(id >= 0 && id < vocab ? id : vocab);
-  };
-  const uint32_t id = id_of(mine);
+  constexpr int GROUPS = kThreads / RANK_TOKENS, PER = RANK_MOST / kThreads;
+  const int t = threadIdx.x, first = blockIdx.x * RANK_TOKENS, mine = first + t % RANK_TOKENS, quads = (count + 3) / 4;
+  uint32_t staged[PER];
+#pragma unroll
+  for (int u = 0; u < PER; ++u) {
+    const int i = t + u * kThreads;
+    staged[u] = 0xFFFFFFFFu;
+    if (i < count) {
+      const int64_t id = token_at(tokens, wide, i);
+      staged[u] = (uint32_t)(id >= 0 && id < vocab ? id : vocab);
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < PER; ++u) reinterpret_cast<uint32_t*>(other)[t + u * kThreads] = staged[u];
   if (t < RANK_TOKENS) places[t] = 0;
+  __syncthreads();
+  const uint32_t id = mine < RANK_MOST ? reinterpret_cast<const uint32_t*>(other)[mine] : 0xFFFFFFFFu;
   int n = 0;
-  for (int base = 0; base < count; base += RANK_BLOCK) {
-    const int quads = min(RANK_BLOCK, count - base + 3) / 4;
-    __syncthreads();
 #pragma unroll 4
-    for (int i = t; i < 4 * quads; i += kThreads) reinterpret_cast<uint32_t*>(other)[i] = id_of(base + i);
-    __syncthreads();
-    for (int q = t / RANK_TOKENS; q < quads; q += GROUPS) {
-      const uint4 o = other[q];
-      const int at = base + 4 * q;
-      if ((unsigned)(at - first) < (unsigned)RANK_TOKENS) {   // among this workgroup's own tokens: by id, then by position
-        n += o.x < id || (o.x == id && at < mine);
-        n += o.y < id || (o.y == id && at + 1 < mine);
-        n += o.z < id || (o.z == id && at + 2 < mine);
-        n += o.w < id || (o.w == id && at + 3 < mine);
-      } else {
-        const uint32_t limit = id + (at < first ? 1u : 0u);    // tokens before these with the same id come first
-        n += o.x < limit;
-        n += o.y < limit;
-        n += o.z < limit;
-        n += o.w < limit;
-      }
+  for (int q = t / RANK_TOKENS; q < quads; q += GROUPS) {
+    const uint4 o = other[q];
+    const int at = 4 * q;
+    if ((unsigned)(at - first) < (unsigned)RANK_TOKENS) {   // among this workgroup's own tokens: by id, then by position
+      n += o.x < id || (o.x == id && at < mine);
+      n += o.y < id || (o.y == id && at + 1 < mine);
+      n += o.z < id || (o.z == id && at + 2 < mine);
+      n += o.w < id || (o.w == id && at + 3 < mine);
+    } else {
+      const uint32_t limit = id + (at < first ? 1u : 0u);    // tokens before these with the same id come first
+      n += o.x < limit;
+      n += o.y < limit;
+      n += o.z < limit;
+      n += o.w < limit;
     }
   }
   atomicAdd(&places[t % RANK_TOKENS], n);
@@ -227,28 +230,65 @@ __global__ __launch_bounds__(kThreads) void rank_tokens_kernel(const void* token
   }
 }
 
-// keys: tiles * SORT_TILE words.
+// The value of lane l ^ MASK.
+template <int MASK>
+FOG_DEVICE uint32_t of_lane_xor(uint32_t v) {
+  if (MASK == 1) return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xF, 0xF, true);     // quads 1, 0, 3, 2
+  if (MASK == 2) return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xF, 0xF, true);     // quads 2, 3, 0, 1
+  if (MASK == 4) return (uint32_t)__builtin_amdgcn_mov_dpp(__builtin_amdgcn_mov_dpp((int)v, 0x141, 0xF, 0xF, true), 0x1B, 0xF, 0xF, true);   // xor 7, xor 3
+  if (MASK == 8) return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x128, 0xF, 0xF, true);    // rows of 16 turned by 8
+  return (uint32_t)__shfl_xor((int)v, MASK, 64);
+}
+
+// One step of the bitonic sort on key number 4 t + r of the tile: keys STRIDE apart, runs of SIZE in alternating order.
+template <int SIZE, int STRIDE>
+FOG_DEVICE void sort_step(uint32_t* v, uint4* lds) {
+  const int t = threadIdx.x;
+  if (STRIDE < 4) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      if (r & STRIDE) continue;
+      const bool up = ((4 * t + r) & SIZE) == 0;
+      const uint32_t lo = min(v[r], v[r + STRIDE]), hi = max(v[r], v[r + STRIDE]);
+      v[r] = up ? lo : hi;
+      v[r + STRIDE] = up ? hi : lo;
+    }
+    return;
+  }
+  const bool smaller = ((4 * t & SIZE) == 0) == ((4 * t & STRIDE) == 0);
+  uint32_t o[4];
+  if (STRIDE < 256) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) o[r] = of_lane_xor<STRIDE / 4>(v[r]);
+  } else {                                          // keys of another wave
+    __syncthreads();
+    lds[t] = make_uint4(v[0], v[1], v[2], v[3]);
+    __syncthreads();
+    const uint4 x = lds[t ^ (STRIDE / 4)];
+    o[0] = x.x; o[1] = x.y; o[2] = x.z; o[3] = x.w;
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r) v[r] = smaller ? min(v[r], o[r]) : max(v[r], o[r]);
+}
+template <int SIZE, int STRIDE>
+FOG_DEVICE void sort_from(uint32_t* v, uint4* lds) {
+  sort_step<SIZE, STRIDE>(v, lds);
+  if constexpr (STRIDE > 1) sort_from<SIZE, STRIDE / 2>(v, lds);
+  else if constexpr (SIZE < SORT_TILE) sort_from<2 * SIZE, SIZE>(v, lds);
+}
+
+// keys: tiles * SORT_TILE words.  A thread keeps four neighbouring keys; of the 55 steps 19 stay within a thread and 33 within a wave (a
+// step on all keys in LDS took the tile 14.5 us, this one 3).
 __global__ __launch_bounds__(kThreads) void sort_tiles_kernel(const void* tokens, int wide, int64_t count, int64_t vocab, uint32_t* keys, int work, Fill fill) {
   if ((int)blockIdx.x >= work) return fill_zeros(fill, (int)blockIdx.x - work, (int)gridDim.x - work);
-  __shared__ uint32_t k[SORT_TILE];
+  static_assert(SORT_TILE == 4 * kThreads, "four keys a thread");
+  __shared__ uint4 lds[kThreads];
   const int64_t base = (int64_t)blockIdx.x * SORT_TILE;
-  for (int i = threadIdx.x; i < SORT_TILE; i += kThreads) k[i] = sort_key(tokens, wide, count, vocab, base + i, i);
-  for (int size = 2; size <= SORT_TILE; size *= 2)
-    for (int stride = size / 2; stride > 0; stride /= 2) {
-      // the pairs of 64 neighbouring t lie within 128 keys up to a stride of 64: a wave waits for the others only before and behind longer ones
-      if (stride >= 128 || (stride == 64 && size >= 256) || size == 2) __syncthreads();
-      else                                                             asm volatile("" ::: "memory");   // LDS serves a wave in order
+  uint32_t v[4];
 #pragma unroll
-      for (int t = threadIdx.x; t < SORT_TILE / 2; t += kThreads) {
-        const int i = 2 * t - (t & (stride - 1)), j = i + stride;
-        const uint32_t x = k[i], y = k[j];
-        const bool up = (i & size) == 0, turn = (x > y) == up;
-        k[i] = turn ? y : x;
-        k[j] = turn ? x : y;
-      }
-    }
-  __syncthreads();
-  for (int i = threadIdx.x; i < SORT_TILE; i += kThreads) keys[base + i] = k[i];
+  for (int r = 0; r < 4; ++r) v[r] = sort_key(tokens, wide, count, vocab, base + 4 * threadIdx.x + r, 4 * threadIdx.x + r);
+  sort_from<2, 1>(v, lds);
+  reinterpret_cast<uint4*>(keys + base)[threadIdx.x] = make_uint4(v[0], v[1], v[2], v[3]);
 }
 
 // Numbers of four sorted tiles' keys below `limit` (four searches at a time: each step of one waits for LDS).
@@ -275,13 +315,25 @@ __global__ __launch_bounds__(kThreads) void merge_ranks_kernel(const uint32_t* _
   const int mine = blockIdx.x / MERGE_PARTS, in_tile = threadIdx.x + kThreads * (blockIdx.x % MERGE_PARTS);
   const uint32_t key = keys[(int64_t)mine * SORT_TILE + in_tile], id = key >> POS_BITS;
   int64_t rank = in_tile;
+  const uint4* all = reinterpret_cast<const uint4*>(keys);
+  constexpr int PER = MERGE_TILES * SORT_TILE / 4 / kThreads;     // 16-byte pieces a thread brings in
+  uint4 next[PER];
+  const int64_t pieces = (int64_t)tiles * (SORT_TILE / 4);
+  auto fetch = [&](int base) {
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+      const int64_t i = (int64_t)base * (SORT_TILE / 4) + threadIdx.x + u * kThreads;
+      next[u] = i < pieces ? all[i] : make_uint4(0, 0, 0, 0);
+    }
+  };
+  fetch(0);
   for (int base = 0; base < tiles; base += MERGE_TILES) {
     const int n = min(MERGE_TILES, tiles - base);
     __syncthreads();
-#pragma unroll 4
-    for (int i = threadIdx.x; i < n * (SORT_TILE / 4); i += kThreads)
-      reinterpret_cast<uint4*>(&k[0][0])[i] = reinterpret_cast<const uint4*>(keys + (int64_t)base * SORT_TILE)[i];
+#pragma unroll
+    for (int u = 0; u < PER; ++u) reinterpret_cast<uint4*>(&k[0][0])[threadIdx.x + u * kThreads] = next[u];
     __syncthreads();
+    fetch(base + MERGE_TILES);
     for (int b = 0; b < n; b += 4) {
       uint32_t limit[4];
 #pragma unroll
@@ -340,15 +392,36 @@ struct Row {
     v[0] += bf16lo(x.x); v[1] += bf16hi(x.x); v[2] += bf16lo(x.y); v[3] += bf16hi(x.y);
     v[4] += bf16lo(x.z); v[5] += bf16hi(x.z); v[6] += bf16lo(x.w); v[7] += bf16hi(x.w);
   }
-  __device__ __forceinline__ void add_floats(const float* p, int n) {
+  // n floats of a piece in the workspace, zeros behind them
+  static __device__ __forceinline__ void load_floats(float* x, const float* p, int n) {
+    if (VEC) {
+      float4 lo = make_float4(0.0f, 0.0f, 0.0f, 0.0f), hi = lo;
+      if (n > 0) {
+        lo = *reinterpret_cast<const float4*>(p);
+        hi = *reinterpret_cast<const float4*>(p + 4);
+      }
+      x[0] = lo.x; x[1] = lo.y; x[2] = lo.z; x[3] = lo.w; x[4] = hi.x; x[5] = hi.y; x[6] = hi.z; x[7] = hi.w;
+    } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < n) v[i] += p[i];
+      for (int i = 0; i < 8; ++i) x[i] = i < n ? p[i] : 0.0f;
+    }
+  }
+  __device__ __forceinline__ void add_floats(const float* p, int n) {
+    float x[8];
+    load_floats(x, p, n);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += x[i];
   }
   __device__ __forceinline__ void put_floats(float* p, int n) const {
+    if (VEC) {
+      if (n <= 0) return;
+      *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+      *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
+    } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < n) p[i] = v[i];
+      for (int i = 0; i < 8; ++i)
+        if (i < n) p[i] = v[i];
+    }
   }
   // the finished sum times the factor (added to what is there) to the table's gradient
   __device__ __forceinline__ void finish(const GradArgs& a, int64_t id, int64_t col, int n) const {
@@ -437,10 +510,11 @@ __global__ __launch_bounds__(kThreads) void sum_runs_kernel(GradArgs a) {
   else                   sum.finish(a, cur, col, n);
 }
 
-// A workgroup for each chunk and slab; those whose chunk ends inside a run that it began add up the run's pieces: the four waves a
-// quarter of the chunks each, then the four sums in order.
+// A workgroup for each chunk and slab; those whose chunk ends inside a run that it began add up the run's pieces: the eight waves an eighth
+// of the chunks each, then the eight sums in order.
+constexpr int JOIN_WAVES = 8;
 template <bool F32, bool VEC>
-__global__ __launch_bounds__(kThreads) void join_runs_kernel(GradArgs a) {
+__global__ __launch_bounds__(64 * JOIN_WAVES) void join_runs_kernel(GradArgs a) {
   const int64_t c = (int64_t)blockIdx.x / a.slabs;
   const int64_t next = (c + 1) * a.chunk;              // first token of the next chunk
   if (next >= a.count) return;
@@ -458,20 +532,29 @@ __global__ __launch_bounds__(kThreads) void join_runs_kernel(GradArgs a) {
   const int w = threadIdx.x >> 6, l = threadIdx.x & 63;
   const int64_t col = ((int64_t)blockIdx.x - c * a.slabs) * SLAB + 8 * l;
   const int n = a.cols - col >= 8 ? 8 : a.cols > col ? (int)(a.cols - col) : 0;
-  const int64_t per = (m + 3) / 4, b = c + 1 + w * per, e = b + per < c + m + 1 ? b + per : c + m + 1;
+  const int64_t per = (m + JOIN_WAVES - 1) / JOIN_WAVES, b = c + 1 + w * per, e = b + per < c + m + 1 ? b + per : c + m + 1;
   Row<F32, VEC> sum;
   sum.clear();
   if (w == 0) sum.add_floats(a.tail + c * a.cols + col, n);
-#pragma unroll 4
-  for (int64_t i = b; i < e; ++i) sum.add_floats(a.head + i * a.cols + col, n);
-  __shared__ float part[3][8][64];
+  constexpr int AHEAD = 8;
+  for (int64_t i = b; i < e; i += AHEAD) {
+    float v[AHEAD][8];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) Row<F32, VEC>::load_floats(v[u], a.head + (i + u) * a.cols + col, i + u < e ? n : 0);
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) sum.v[k] += v[u][k];
+  }
+  __shared__ float part[JOIN_WAVES - 1][8][64];
   if (w > 0) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) part[w - 1][i][l] = sum.v[i];
   }
   __syncthreads();
   if (w > 0) return;
-  for (int k = 0; k < 3; ++k)
+#pragma unroll
+  for (int k = 0; k < JOIN_WAVES - 1; ++k)
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum.v[i] += part[k][i][l];
   sum.finish(a, id, col, n);
@@ -499,7 +582,7 @@ GradRoom room_of(int64_t count, int64_t cols) {
   return r;
 }
 
-constexpr int64_t GROUPS_MAX = 1 << 23;    // workgroups of a launch: grids are counted in threads of 32 bits
+constexpr int64_t GROUPS_MAX = 1 << 22;    // workgroups of a launch (up to 512 threads each): grids are counted in threads of 32 bits
 
 inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
@@ -619,7 +702,7 @@ extern "C" fog_status fog_embed_grad(const void* tokens, int token_bytes, int64_
 #define FOG_EG(F, V)                                                                            \
   do {                                                                                          \
     sum_runs_kernel<F, V><<<groups, kThreads, 0, s>>>(a);                                       \
-    if (a.chunks > 1) join_runs_kernel<F, V><<<(int)a.units, kThreads, 0, s>>>(a);              \
+    if (a.chunks > 1) join_runs_kernel<F, V><<<(int)a.units, 64 * JOIN_WAVES, 0, s>>>(a);       \
   } while (0)
   if (type == FOG_F32) { if (vec) FOG_EG(true, true); else FOG_EG(true, false); }
   else                 { if (vec) FOG_EG(false, true); else FOG_EG(false, false); }

@@ -117,7 +117,7 @@ def check_gradient(got, want, mag, n, dtype, start=None):
 
 
 GRADS = [(1, 5, 8), (2, 3, 264), (7, 100, 2064), (63, 1, 512), (64, 40, 520), (65, 33, 131), (777, 1000, 264), (1023, 17, 72), (1024, 5000, 64),
-         (1025, 200, 1032), (3000, 3, 1544), (20000, 900, 40), (40001, 50000, 16)]
+         (1025, 200, 1032), (2047, 300, 72), (2048, 5, 264), (2049, 4000, 24), (3000, 3, 1544), (20000, 900, 40), (40001, 50000, 16)]
 
 
 @pytest.mark.parametrize("T,V,H", GRADS)
