@@ -429,7 +429,7 @@ fog_status fog_embed_quantize(const void* tokens, int token_bytes, int64_t count
  *   dx_bf16 : [count, cols], leading dimension ld_dx.   type : of dE, [vocab, cols] with leading dimension ld_dE.
  *   workspace : fog_embed_grad_workspace(count, vocab, cols) bytes, 16-byte aligned; contents on entry do not matter.  Calls that may
  *            overlap in time need a workspace each.
- * Limits: count and cols below 2^31, vocab up to 4194302, count * cols up to 2^37.  The tokens are sorted in tiles of 1024 that are
+ * Limits: count and cols below 2^31, vocab up to 4194302, count * max(cols, 512) up to 2^37.  The tokens are sorted in tiles of 1024 that are
  * merged by searching every tile for every token, which grows with count^2 / 1024 and stays below the sums up to about 10^5 tokens.
  * Errors: NULL, SHAPE, ALIGN, WORKSPACE, UNSUPPORTED (token_bytes, type, factor, limits).
  */

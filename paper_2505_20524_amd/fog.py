@@ -281,11 +281,15 @@ BLOCK = 128                  # elements of a block scale
 
 
 def _matrix(t, what, rows, cols, size):
-    """Refuses a tensor that the pointer and leading dimension of the call would misdescribe."""
-    if t.dim() != 2 or t.shape[0] < rows or t.shape[1] < cols or t.element_size() != size or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError("%s: a [%d, %d] matrix of %d-byte elements with contiguous rows is needed, got %s of %s with strides %s"
-                         % (what, rows, cols, size, tuple(t.shape), t.dtype, t.stride()))
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), cols)
+    """The leading dimension of a matrix of at least rows x cols; refuses a tensor that the pointer and leading dimension of the call would
+    misdescribe.  (Half a microsecond: calls that take five have up to five matrices.)"""
+    if t.dim() == 2:
+        r, c = t.shape
+        ld, step = t.stride()
+        if r >= rows and c >= cols and (step == 1 or c == 1) and t.element_size() == size:
+            return ld if ld >= cols or r > 1 else cols
+    raise ValueError("%s: a [%d, %d] matrix of %d-byte elements with contiguous rows is needed, got %s of %s with strides %s"
+                     % (what, rows, cols, size, tuple(t.shape), t.dtype, t.stride()))
 
 
 def _blocks(n):
@@ -321,8 +325,8 @@ def fp8_gemm_block(layout, M, N, K, A, fmt_a, block_a, s_a, B, fmt_b, block_b, s
     a_rows, a_cols = (K, M) if layout == TN else (M, K)
     b_rows, b_cols = (N, K) if layout == NT else (K, N)
     lda, ldb = _matrix(A, "A", a_rows, a_cols, 1), _matrix(B, "B", b_rows, b_cols, 1)
-    lds_a = _matrix(s_a, "s_a", *((_blocks(a_rows), _blocks(a_cols)) if block_a == TILE else (_blocks(K), M)), 1)
-    lds_b = _matrix(s_b, "s_b", *((_blocks(b_rows), _blocks(b_cols)) if block_b == TILE else (_blocks(K), N)), 1)
+    lds_a = _matrix(s_a, "s_a", _blocks(a_rows), _blocks(a_cols), 1) if block_a == TILE else _matrix(s_a, "s_a", _blocks(K), M, 1)
+    lds_b = _matrix(s_b, "s_b", _blocks(b_rows), _blocks(b_cols), 1) if block_b == TILE else _matrix(s_b, "s_b", _blocks(K), N, 1)
     ws = workspace.numel() * workspace.element_size() if workspace is not None else 0
     _check(load().fog_fp8_gemm_block(layout, M, N, K, _ptr(A), fmt_a, lda, block_a, _ptr(s_a), lds_a, _ptr(B), fmt_b, ldb, block_b, _ptr(s_b), lds_b,
                                      _ptr(C), _matrix(C, "C", M, N, 2), _ptr(workspace), ws, _stream(stream)), "fog_fp8_gemm_block")
