@@ -395,7 +395,7 @@ fog_status fog_quantize_tile(const void* x_bf16, int64_t rows, int64_t cols, int
  *                       way the product contracts it
  *   Bytes 1 .. 254 (byte 255 gives NaN).  Any alignment.
  *   workspace : NULL, or fog_fp8_gemm_block_workspace(layout, M, N, K) bytes, as for fog_fp8_gemm.
- * NT products of up to 64 rows (the tokens of a decoding step) read B once, straight into the matrix instruction.
+ * NT products of up to 32 rows (the tokens of a decoding step) have a kernel of their own that streams B.
  * Layouts, other arguments, requirements and errors as for fog_fp8_gemm.
  */
 typedef enum { FOG_BLOCK_VECTOR = 0, FOG_BLOCK_TILE = 1 } fog_block;

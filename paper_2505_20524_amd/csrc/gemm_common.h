@@ -36,8 +36,8 @@ struct ProductPlan { int tile, splits, k_chunk; };
 // Launches one of the small-tile kernels (gemm_tile_kernels.hip) on checked arguments; with g.sa.s set its block-scaled form.
 enum GemmTile { TILE_256x128, TILE_128x128, TILE_128x128_2WG, TILE_64x64 };
 __attribute__((visibility("hidden"))) fog_status gemm_tile_launch(GemmTile tile, fog_layout layout, fog_fp8 fmt_a, fog_fp8 fmt_b, GemmArgs g, hipStream_t s);
-// Launches the kernel of block-scaled NT products with up to ROWS_MAX rows (gemm_rows_kernel.hip).
-constexpr int ROWS_MAX = 64;
+// Whether the kernel of block-scaled NT products of few rows (gemm_rows_kernel.hip) takes a product, and its launch.
+__attribute__((visibility("hidden"))) bool gemm_rows_takes(int64_t M, int64_t N, int64_t K, int cus);
 __attribute__((visibility("hidden"))) fog_status gemm_rows_launch(fog_fp8 fmt_a, fog_fp8 fmt_b, GemmArgs g, hipStream_t s);
 // Adds up the partial tiles of a split product whose tiles are 64 ti x 64 tj.
 __attribute__((visibility("hidden"))) void gemm_reduce_launch(const GemmArgs& g, int ti, int tj, hipStream_t s);

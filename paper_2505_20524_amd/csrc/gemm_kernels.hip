@@ -777,7 +777,7 @@ static fog_status run_product(GemmArgs g, fog_layout layout, int64_t M, int64_t 
     gemm_zero_kernel<<<(int)blocks, 256, 0, s>>>(g.C, ldc, g.M, g.N);
     return fog_launch_status();
   }
-  if (g.sa.s && layout == FOG_NT && M <= ROWS_MAX) return gemm_rows_launch(fmtA, fmtB, g, s);
+  if (g.sa.s && layout == FOG_NT && gemm_rows_takes(M, N, K, fog_compute_units())) return gemm_rows_launch(fmtA, fmtB, g, s);
   // the contraction is only split when the caller brought the room that the workspace query names
   size_t room = 0;
   if (workspace && aligned(workspace, 16)) {
