@@ -4,19 +4,20 @@
 // 127 - k of its reciprocal.  Multiplying by it is exact, so that the one rounding of an element is the cast's own, and the matrix
 // instruction takes the byte as it is.  The price is up to one binary place of the format's range, not of its precision.
 //
-// One workgroup of 256 threads reads a tile of 128 x 128 elements once, 16 bytes a lane, 16 lanes a row, and keeps it in registers (32
+// One workgroup of 512 threads reads a tile of 128 x 128 elements once, 16 bytes a lane, 16 lanes a row, and keeps it in registers (16
 // a thread): the maxima along rows are a reduction over 16 lanes, those along columns one over a thread's rows, the wave's four lanes
-// of a column group and, through LDS, the four waves.  Both forms of codes then come from the same registers: a tensor that a step
+// of a column group and, through LDS, the waves.  Both forms of codes then come from the same registers: a tensor that a step
 // multiplies along its rows and along its columns is read once for the two casts.  Bound by memory: 2 bytes read and 1 written (2 for
-// both forms) per element.
+// both forms) per element.  us (at 4.8 TB/s, the rate of a large copy): 8192 x 14336 rows 60 (73), both 85 (98), tiles 60 (73);
+// 1777 x 2064 rows 6.1 (2.3), both 7.7 (3.1).  Workgroups of 256 and of 1024 threads: 8192 x 14336 both 88 and 89, 1777 x 2064 both 8.5 and
+// 7.6, 24 x 4096 rows 3.7 and 3.0 where these take 3.1.
 #include "common.h"
 #include "launch.h"
 
 namespace {
 
-constexpr int kThreads = 256;
 constexpr int BLK = 128;
-constexpr int PASSES = BLK * BLK / 8 / kThreads;    // row groups of 16 that a thread holds: 8
+constexpr int kThreads = 512;
 
 struct BlockCastArgs {
   const uint16_t* x;
@@ -25,6 +26,7 @@ struct BlockCastArgs {
   int64_t rows, cols;
   int64_t tiles_c;
   int margin;
+  int stream;      // read past the caches
 };
 
 // k of the block's scale from the magnitude pattern of its abs-max (bf16 without sign; 0x7F80 and above: not finite)
@@ -65,10 +67,13 @@ FOG_DEVICE uint2 cast8(uint4 v, const float* f) {
   return make_uint2(cvt4_fp8<FMT>(a, b, c, d), cvt4_fp8<FMT>(e, g, h, i));
 }
 
+// Codes are written through: the product that reads them next finds them in the memory-side cache, and nothing is left to write back
+// while it runs (stored past the caches: a layer of 8192 x 2048 x 2048 forward and backward 152 us instead of 136, of 4096 x 4096 x 4096
+// 217 and 205; the cast of 8192 x 12288 both ways by itself 72 and 75).
 template <bool VEC>
 FOG_DEVICE void store8(uint8_t* q, int64_t at, uint2 v, int n) {
   if (VEC) {
-    st_nt8(q + at, v);
+    st_through8(q + at, v);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
@@ -79,13 +84,15 @@ FOG_DEVICE void store8(uint8_t* q, int64_t at, uint2 v, int n) {
 // VEC: x in 16-byte pieces, codes in 8-byte pieces (leading dimensions and cols multiples of 8, aligned pointers).
 template <int FMT, bool ROW, bool COL, bool TILE, bool VEC>
 __global__ __launch_bounds__(kThreads) void block_cast_kernel(BlockCastArgs a) {
-  __shared__ uint32_t colmax[4][64];      // per wave: 128 columns' maxima in pairs
-  __shared__ uint8_t rowbyte[BLK];
+  constexpr int GROUP = kThreads / 16, PASSES = BLK / GROUP, WAVES = kThreads / 64;    // rows of a pass; pieces that a thread holds
+  __shared__ uint32_t colmax[COL || TILE ? WAVES : 1][64];      // per wave: 128 columns' maxima in pairs
+  __shared__ float colscale[COL ? BLK : 1];
+  __shared__ uint8_t rowbyte[ROW ? BLK : 1];
   const int t = threadIdx.x, l = t & 63, w = t >> 6;
   const int64_t tr = (int64_t)blockIdx.x / a.tiles_c, tc = (int64_t)blockIdx.x - tr * a.tiles_c;
   const int64_t r0 = tr * BLK, c0 = tc * BLK;
   const int nrows = (int)(a.rows - r0 < BLK ? a.rows - r0 : BLK), ncols = (int)(a.cols - c0 < BLK ? a.cols - c0 : BLK);
-  const int rr = t >> 4, cc = 8 * (t & 15);      // row of pass p: 16 p + rr
+  const int rr = t >> 4, cc = 8 * (t & 15);      // row of pass p: GROUP p + rr
   const int n = ncols - cc < 0 ? 0 : ncols - cc < 8 ? ncols - cc : 8;
   const uint16_t* x = a.x + (r0 + rr) * a.ldx + c0 + cc;
 
@@ -93,78 +100,78 @@ __global__ __launch_bounds__(kThreads) void block_cast_kernel(BlockCastArgs a) {
 #pragma unroll
   for (int p = 0; p < PASSES; ++p) {
     v[p] = make_uint4(0, 0, 0, 0);
-    if (16 * p + rr < nrows) {
+    if (GROUP * p + rr < nrows) {
       if (VEC) {
-        if (n > 0) v[p] = ld_nt16(x + 16 * p * a.ldx);
+        if (n > 0) v[p] = a.stream ? ld_nt16(x + GROUP * p * a.ldx) : *reinterpret_cast<const uint4*>(x + GROUP * p * a.ldx);
       } else {
         uint32_t wv[4] = {0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          if (i < n) wv[i >> 1] |= (uint32_t)x[16 * p * a.ldx + i] << (16 * (i & 1));
+          if (i < n) wv[i >> 1] |= (uint32_t)x[GROUP * p * a.ldx + i] << (16 * (i & 1));
         v[p] = make_uint4(wv[0], wv[1], wv[2], wv[3]);
       }
     }
   }
-  // maxima: of each row over the 16 lanes that hold it, of each column over this thread's rows
-  uint32_t rowmax[PASSES];
-  uint32_t cm[4] = {0, 0, 0, 0};
+  // maxima of the columns: over a thread's rows, over the wave's four lanes of a column group, and through LDS over the waves
+  if (COL || TILE) {
+    uint32_t cm[4] = {0, 0, 0, 0};
 #pragma unroll
-  for (int p = 0; p < PASSES; ++p) {
-    if (ROW) rowmax[p] = max_of_pair(max_over_16(pkmax_abs_bf16(pkmax_abs_bf16(pkmax_abs_bf16(pkmax_abs_bf16(0u, v[p].x), v[p].y), v[p].z), v[p].w)));
-    if (COL || TILE) {
+    for (int p = 0; p < PASSES; ++p) {
       cm[0] = pkmax_abs_bf16(cm[0], v[p].x);
       cm[1] = pkmax_abs_bf16(cm[1], v[p].y);
       cm[2] = pkmax_abs_bf16(cm[2], v[p].z);
       cm[3] = pkmax_abs_bf16(cm[3], v[p].w);
     }
-  }
-  if (ROW) {
-#pragma unroll
-    for (int p = 0; p < PASSES; ++p) {
-      const int k = block_exponent<FMT>(rowmax[p], a.margin);
-      const float f1 = pow2(k);
-      const float f[8] = {f1, f1, f1, f1, f1, f1, f1, f1};
-      const int r = 16 * p + rr;
-      if ((t & 15) == 0) rowbyte[r] = (uint8_t)(127 - k);
-      if (r < nrows && n > 0) {
-        const uint2 o = __builtin_expect(rowmax[p] >= 0x7F80u, 0) ? cast8<FMT, true>(v[p], f) : cast8<FMT, false>(v[p], f);
-        store8<VEC>(a.q_row, (r0 + r) * a.ldq_row + c0 + cc, o, n);
-      }
-    }
-  }
-  if (COL || TILE) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       cm[i] = pkmax(cm[i], (uint32_t)__shfl_xor((int)cm[i], 16, 64));
       cm[i] = pkmax(cm[i], (uint32_t)__shfl_xor((int)cm[i], 32, 64));
     }
-    if (l < 16) {
+    if (l < 16) *reinterpret_cast<uint4*>(&colmax[w][4 * l]) = make_uint4(cm[0], cm[1], cm[2], cm[3]);
+    __syncthreads();
+  }
+  int odd = 0;      // a column of the tile is not finite
+  if (COL && t < 64) {
+    uint32_t m = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) colmax[w][4 * l + i] = cm[i];
+    for (int i = 0; i < WAVES; ++i) m = pkmax(m, colmax[i][t]);
+    const int k0 = block_exponent<FMT>(m & 0xFFFFu, a.margin), k1 = block_exponent<FMT>(m >> 16, a.margin);
+    // a scale with its sign bit set marks a column that is not finite
+    colscale[2 * t] = (m & 0xFFFFu) >= 0x7F80u ? -1.0f : pow2(k0);
+    colscale[2 * t + 1] = (m >> 16) >= 0x7F80u ? -1.0f : pow2(k1);
+    uint8_t* s = a.s_col + tr * a.lds_col + c0 + 2 * t;
+    if (2 * t < ncols) s[0] = (uint8_t)(127 - k0);
+    if (2 * t + 1 < ncols) s[1] = (uint8_t)(127 - k1);
+  }
+  // rows: maxima over the 16 lanes that hold one
+  if (ROW) {
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+      const uint32_t rowmax = max_of_pair(max_over_16(pkmax_abs_bf16(pkmax_abs_bf16(pkmax_abs_bf16(pkmax_abs_bf16(0u, v[p].x), v[p].y), v[p].z), v[p].w)));
+      const int k = block_exponent<FMT>(rowmax, a.margin);
+      const float f1 = pow2(k);
+      const float f[8] = {f1, f1, f1, f1, f1, f1, f1, f1};
+      const int r = GROUP * p + rr;
+      if ((t & 15) == 0) rowbyte[r] = (uint8_t)(127 - k);
+      if (r < nrows && n > 0) {
+        const uint2 o = __builtin_expect(rowmax >= 0x7F80u, 0) ? cast8<FMT, true>(v[p], f) : cast8<FMT, false>(v[p], f);
+        store8<VEC>(a.q_row, (r0 + r) * a.ldq_row + c0 + cc, o, n);
+      }
     }
   }
-  __syncthreads();
+  if (ROW || COL) __syncthreads();
   if (ROW && t < nrows) a.s_row[tc * a.lds_row + r0 + t] = rowbyte[t];
   if (COL) {
-    float f[8];
-    bool odd = false;
+    const float4 lo = *reinterpret_cast<const float4*>(&colscale[cc]), hi = *reinterpret_cast<const float4*>(&colscale[cc + 4]);
+    float f[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int at = 4 * (t & 15) + i;
-      const uint32_t m = pkmax(pkmax(colmax[0][at], colmax[1][at]), pkmax(colmax[2][at], colmax[3][at]));
-      const int k0 = block_exponent<FMT>(m & 0xFFFFu, a.margin), k1 = block_exponent<FMT>(m >> 16, a.margin);
-      f[2 * i] = pow2(k0);
-      f[2 * i + 1] = pow2(k1);
-      odd = odd || max_of_pair(m) >= 0x7F80u;
-      if (t < 16) {
-        uint8_t* s = a.s_col + tr * a.lds_col + c0 + cc + 2 * i;
-        if (2 * i < n) s[0] = (uint8_t)(127 - k0);
-        if (2 * i + 1 < n) s[1] = (uint8_t)(127 - k1);
-      }
+    for (int i = 0; i < 8; ++i) {
+      odd |= f[i] < 0.0f;
+      f[i] = fabsf(f[i]);
     }
 #pragma unroll
     for (int p = 0; p < PASSES; ++p) {
-      const int r = 16 * p + rr;
+      const int r = GROUP * p + rr;
       if (r < nrows && n > 0) {
         const uint2 o = __builtin_expect(odd, 0) ? cast8<FMT, true>(v[p], f) : cast8<FMT, false>(v[p], f);
         store8<VEC>(a.q_col, (r0 + r) * a.ldq_col + c0 + cc, o, n);
@@ -172,7 +179,9 @@ __global__ __launch_bounds__(kThreads) void block_cast_kernel(BlockCastArgs a) {
     }
   }
   if (TILE) {
-    uint32_t m = pkmax(pkmax(colmax[0][l], colmax[1][l]), pkmax(colmax[2][l], colmax[3][l]));
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) m = pkmax(m, colmax[i][l]);
     m = wave_max_u32(max_of_pair(m));
     const int k = block_exponent<FMT>(m, a.margin);
     const float f1 = pow2(k);
@@ -180,7 +189,7 @@ __global__ __launch_bounds__(kThreads) void block_cast_kernel(BlockCastArgs a) {
     if (t == 0) a.s_row[tr * a.lds_row + tc] = (uint8_t)(127 - k);
 #pragma unroll
     for (int p = 0; p < PASSES; ++p) {
-      const int r = 16 * p + rr;
+      const int r = GROUP * p + rr;
       if (r < nrows && n > 0) {
         const uint2 o = __builtin_expect(m >= 0x7F80u, 0) ? cast8<FMT, true>(v[p], f) : cast8<FMT, false>(v[p], f);
         store8<VEC>(a.q_row, (r0 + r) * a.ldq_row + c0 + cc, o, n);
@@ -195,6 +204,9 @@ template <bool ROW, bool COL, bool TILE>
 fog_status launch(BlockCastArgs a, fog_fp8 fmt, hipStream_t s) {
   a.tiles_c = (a.cols + BLK - 1) / BLK;
   const int64_t tiles = a.tiles_c * ((a.rows + BLK - 1) / BLK);
+  // what the kernel before has left in the caches is worth finding up to about 16 M elements (past the caches and as ordinary loads: the layer of
+  // 1777 x 3088 x 2064 86.0 and 81.5 us, 4096 x 8192 x 2048 forward 76.9 and 74.8, 4096 x 4096 x 4096 205 and 207, 8192 x 4096 x 14336 1180 and 1210)
+  a.stream = a.rows * a.cols > ((int64_t)16 << 20);
   if (tiles > 0x7FFFFFFF) return FOG_ERR_UNSUPPORTED;
   const bool vec = a.cols % 8 == 0 && a.ldx % 8 == 0 && aligned(a.x, 16) && (!(ROW || TILE) || (aligned(a.q_row, 8) && a.ldq_row % 8 == 0)) &&
                    (!COL || (aligned(a.q_col, 8) && a.ldq_col % 8 == 0));
@@ -217,7 +229,7 @@ extern "C" fog_status fog_quantize_block(const void* x_bf16, int64_t rows, int64
   if (!x_bf16 || (!q_row && !q_col) || (!q_row) != (!s_row) || (!q_col) != (!s_col)) return FOG_ERR_NULL;
   if (ldx < cols || (q_row && (ldq_row < cols || lds_row < rows)) || (q_col && (ldq_col < cols || lds_col < cols))) return FOG_ERR_SHAPE;
   if (!aligned(x_bf16, 2)) return FOG_ERR_ALIGN;
-  const BlockCastArgs a{reinterpret_cast<const uint16_t*>(x_bf16), q_row, s_row, q_col, s_col, ldx, ldq_row, lds_row, ldq_col, lds_col, rows, cols, 0, margin};
+  const BlockCastArgs a{reinterpret_cast<const uint16_t*>(x_bf16), q_row, s_row, q_col, s_col, ldx, ldq_row, lds_row, ldq_col, lds_col, rows, cols, 0, margin, 0};
   hipStream_t s = (hipStream_t)stream;
   if (q_row && q_col) return launch<true, true, false>(a, fmt, s);
   return q_row ? launch<true, false, false>(a, fmt, s) : launch<false, true, false>(a, fmt, s);
@@ -231,6 +243,6 @@ extern "C" fog_status fog_quantize_tile(const void* x_bf16, int64_t rows, int64_
   if (!x_bf16 || !q || !s) return FOG_ERR_NULL;
   if (ldx < cols || ldq < cols || lds < (cols + BLK - 1) / BLK) return FOG_ERR_SHAPE;
   if (!aligned(x_bf16, 2)) return FOG_ERR_ALIGN;
-  const BlockCastArgs a{reinterpret_cast<const uint16_t*>(x_bf16), q, s, nullptr, nullptr, ldx, ldq, lds, 0, 0, rows, cols, 0, margin};
+  const BlockCastArgs a{reinterpret_cast<const uint16_t*>(x_bf16), q, s, nullptr, nullptr, ldx, ldq, lds, 0, 0, rows, cols, 0, margin, 0};
   return launch<false, false, true>(a, fmt, (hipStream_t)stream);
 }
