@@ -280,16 +280,41 @@ def fp8_gemm_workspace(layout, M, N, K):
 BLOCK = 128                  # elements of a block scale
 
 
-def _matrix(t, what, rows, cols, size):
+# what a tensor may be that the calls read or write as codes and scale bytes, as bfloat16, as binary32
+_CODES = (torch.uint8, torch.float8_e4m3fn, torch.float8_e5m2, torch.int8)
+_HALVES = (torch.bfloat16, torch.int16)
+_WORDS = (torch.float32,)
+
+
+def _matrix(t, what, rows, cols, types):
     """The leading dimension of a matrix of at least rows x cols; refuses a tensor that the pointer and leading dimension of the call would
     misdescribe.  (Half a microsecond: calls that take five have up to five matrices.)"""
     if t.dim() == 2:
         r, c = t.shape
         ld, step = t.stride()
-        if r >= rows and c >= cols and (step == 1 or c == 1) and t.element_size() == size:
+        if r >= rows and c >= cols and (step == 1 or c == 1) and t.dtype in types:
             return ld if ld >= cols or r > 1 else cols
-    raise ValueError("%s: a [%d, %d] matrix of %d-byte elements with contiguous rows is needed, got %s of %s with strides %s"
-                     % (what, rows, cols, size, tuple(t.shape), t.dtype, t.stride()))
+    raise ValueError("%s: a [%d, %d] matrix of one of %s with contiguous rows is needed, got %s of %s with strides %s"
+                     % (what, rows, cols, types, tuple(t.shape), t.dtype, t.stride()))
+
+
+def _floats(t, what, dtype=torch.float32):
+    if t is not None and (t.dtype != dtype or t.numel() < 1):
+        raise ValueError("%s: a %s tensor is needed, got %s of %s" % (what, dtype, tuple(t.shape), t.dtype))
+
+
+def _here(stream, *tensors):
+    """The handle of the stream, after a look at where the tensors are: a kernel is launched on the current device and would fault on
+    host memory or on another device's."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError("a tensor on %s: the call runs on the current device, cuda:%d" % (t.device, dev))
+    if stream is None:
+        return _raw_stream(dev) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
+    if stream.device_index != dev:
+        raise ValueError("a stream of cuda:%d: the call runs on the current device, cuda:%d" % (stream.device_index, dev))
+    return stream.cuda_stream
 
 
 def _blocks(n):
@@ -299,37 +324,37 @@ def _blocks(n):
 def quantize_block(x, fmt, q_row=None, s_row=None, q_col=None, s_col=None, margin=0, stream=None):
     """Casts with a scale for each block of 128 along the rows (q_row, s_row), along the columns (q_col, s_col), or both in one pass."""
     rows, cols = x.shape
-    ldx = _matrix(x, "x", rows, cols, 2)
+    ldx = _matrix(x, "x", rows, cols, _HALVES)
     ld = [0, 0, 0, 0]
     if q_row is not None:
-        ld[0] = _matrix(q_row, "q_row", rows, cols, 1)
+        ld[0] = _matrix(q_row, "q_row", rows, cols, _CODES)
     if s_row is not None:
-        ld[1] = _matrix(s_row, "s_row", _blocks(cols), rows, 1)
+        ld[1] = _matrix(s_row, "s_row", _blocks(cols), rows, _CODES)
     if q_col is not None:
-        ld[2] = _matrix(q_col, "q_col", rows, cols, 1)
+        ld[2] = _matrix(q_col, "q_col", rows, cols, _CODES)
     if s_col is not None:
-        ld[3] = _matrix(s_col, "s_col", _blocks(rows), cols, 1)
+        ld[3] = _matrix(s_col, "s_col", _blocks(rows), cols, _CODES)
     _check(load().fog_quantize_block(_ptr(x), rows, cols, ldx, fmt, margin, _ptr(q_row), ld[0], _ptr(s_row), ld[1],
-                                     _ptr(q_col), ld[2], _ptr(s_col), ld[3], _stream(stream)), "fog_quantize_block")
+                                     _ptr(q_col), ld[2], _ptr(s_col), ld[3], _here(stream, x, q_row, s_row, q_col, s_col)), "fog_quantize_block")
 
 
 def quantize_tile(x, fmt, q, s, margin=0, stream=None):
     """The cast with a scale for each tile of 128 x 128."""
     rows, cols = x.shape
-    _check(load().fog_quantize_tile(_ptr(x), rows, cols, _matrix(x, "x", rows, cols, 2), fmt, margin, _ptr(q), _matrix(q, "q", rows, cols, 1),
-                                    _ptr(s), _matrix(s, "s", _blocks(rows), _blocks(cols), 1), _stream(stream)), "fog_quantize_tile")
+    _check(load().fog_quantize_tile(_ptr(x), rows, cols, _matrix(x, "x", rows, cols, _HALVES), fmt, margin, _ptr(q), _matrix(q, "q", rows, cols, _CODES),
+                                    _ptr(s), _matrix(s, "s", _blocks(rows), _blocks(cols), _CODES), _here(stream, x, q, s)), "fog_quantize_tile")
 
 
 def fp8_gemm_block(layout, M, N, K, A, fmt_a, block_a, s_a, B, fmt_b, block_b, s_b, C, workspace=None, stream=None):
     """fp8_gemm on operands with a scale for each block of 128 contraction indices; block_a, block_b: VECTOR or TILE."""
     a_rows, a_cols = (K, M) if layout == TN else (M, K)
     b_rows, b_cols = (N, K) if layout == NT else (K, N)
-    lda, ldb = _matrix(A, "A", a_rows, a_cols, 1), _matrix(B, "B", b_rows, b_cols, 1)
-    lds_a = _matrix(s_a, "s_a", _blocks(a_rows), _blocks(a_cols), 1) if block_a == TILE else _matrix(s_a, "s_a", _blocks(K), M, 1)
-    lds_b = _matrix(s_b, "s_b", _blocks(b_rows), _blocks(b_cols), 1) if block_b == TILE else _matrix(s_b, "s_b", _blocks(K), N, 1)
+    lda, ldb = _matrix(A, "A", a_rows, a_cols, _CODES), _matrix(B, "B", b_rows, b_cols, _CODES)
+    lds_a = _matrix(s_a, "s_a", _blocks(a_rows), _blocks(a_cols), _CODES) if block_a == TILE else _matrix(s_a, "s_a", _blocks(K), M, _CODES)
+    lds_b = _matrix(s_b, "s_b", _blocks(b_rows), _blocks(b_cols), _CODES) if block_b == TILE else _matrix(s_b, "s_b", _blocks(K), N, _CODES)
     ws = workspace.numel() * workspace.element_size() if workspace is not None else 0
     _check(load().fog_fp8_gemm_block(layout, M, N, K, _ptr(A), fmt_a, lda, block_a, _ptr(s_a), lds_a, _ptr(B), fmt_b, ldb, block_b, _ptr(s_b), lds_b,
-                                     _ptr(C), _matrix(C, "C", M, N, 2), _ptr(workspace), ws, _stream(stream)), "fog_fp8_gemm_block")
+                                     _ptr(C), _matrix(C, "C", M, N, _HALVES), _ptr(workspace), ws, _here(stream, A, s_a, B, s_b, C, workspace)), "fog_fp8_gemm_block")
 
 
 def fp8_gemm_block_workspace(layout, M, N, K):
@@ -347,9 +372,11 @@ def embed_quantize(tokens, table, factor, fmt, scale_t, x, q=None, amax_out=None
     """x = bf16(factor * table[tokens]) with its FP8 cast and abs-max; tokens outside the table give rows of zeros."""
     ids, size, count = _ids(tokens)
     vocab, cols = table.shape
-    _check(load().fog_embed_quantize(ids, size, count, _ptr(table), vocab, cols, _matrix(table, "table", vocab, cols, 2), factor, fmt, _ptr(scale_t),
-                                     _ptr(x), _matrix(x, "x", count, cols, 2), _ptr(q), _matrix(q, "q", count, cols, 1) if q is not None else 0,
-                                     _ptr(amax_out), _stream(stream)), "fog_embed_quantize")
+    _floats(scale_t, "scale_t")
+    _floats(amax_out, "amax_out")
+    _check(load().fog_embed_quantize(ids, size, count, _ptr(table), vocab, cols, _matrix(table, "table", vocab, cols, _HALVES), factor, fmt, _ptr(scale_t),
+                                     _ptr(x), _matrix(x, "x", count, cols, _HALVES), _ptr(q), _matrix(q, "q", count, cols, _CODES) if q is not None else 0,
+                                     _ptr(amax_out), _here(stream, tokens, table, scale_t, x, q, amax_out)), "fog_embed_quantize")
 
 
 def embed_grad(tokens, dx, factor, dE, workspace, accumulate=False, stream=None):
@@ -357,9 +384,9 @@ def embed_grad(tokens, dx, factor, dE, workspace, accumulate=False, stream=None)
     ids, size, count = _ids(tokens)
     vocab, cols = dE.shape
     kind = F32 if dE.dtype == torch.float32 else BF16
-    _check(load().fog_embed_grad(ids, size, count, _ptr(dx), _matrix(dx, "dx", count, cols, 2), vocab, cols, factor, kind, _ptr(dE),
-                                 _matrix(dE, "dE", vocab, cols, 4 if kind == F32 else 2), int(accumulate),
-                                 _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)), "fog_embed_grad")
+    _check(load().fog_embed_grad(ids, size, count, _ptr(dx), _matrix(dx, "dx", count, cols, _HALVES), vocab, cols, factor, kind, _ptr(dE),
+                                 _matrix(dE, "dE", vocab, cols, _WORDS if kind == F32 else _HALVES), int(accumulate),
+                                 _ptr(workspace), workspace.numel() * workspace.element_size(), _here(stream, tokens, dx, dE, workspace)), "fog_embed_grad")
 
 
 def embed_grad_workspace(count, vocab, cols):
@@ -375,21 +402,30 @@ def make_grad_jobs(items):
     """items: gradients, or (gradient, clipped gradient) pairs, contiguous and in binary32 or 2-byte bfloat16 -> ctypes array for grad_sumsq
     and grad_clip (built once, reused while the tensors stay in place).  A gradient by itself is clipped in place."""
     arr = (GradJob * len(items))()
+    arr.tensors = []           # the array keeps them alive
     for job, item in zip(arr, items):
         g, out = item if isinstance(item, (tuple, list)) else (item, item)
         for t in (g, out):
-            if not t.is_contiguous() or t.dtype not in (torch.float32, torch.bfloat16, torch.int16) or t.dtype != g.dtype or t.numel() != g.numel():
+            if not t.is_contiguous() or t.dtype not in _WORDS + _HALVES or t.dtype != g.dtype or t.numel() != g.numel():
                 raise ValueError("contiguous float32 or bfloat16 gradients are needed, with results of their size and type")
         job.g, job.out, job.n, job.type = _ptr(g), _ptr(out), g.numel(), F32 if g.dtype == torch.float32 else BF16
+        arr.tensors += [g, out]
+    arr.devices = {t.get_device() for t in arr.tensors}
     return arr
+
+
+def _jobs_here(jobs):
+    if jobs.devices - {torch.cuda.current_device()}:
+        raise ValueError("gradients on devices %s (-1: the host): the call runs on the current device, cuda:%d"
+                         % (sorted(jobs.devices), torch.cuda.current_device()))
 
 
 def grad_sumsq(jobs, sumsq, workspace, stream=None):
     """sumsq (one float64): the sum of the squares of all gradients."""
-    if sumsq.dtype != torch.float64:
-        raise ValueError("sumsq: a float64 tensor is needed, got %s" % sumsq.dtype)
-    _check(load().fog_grad_sumsq(jobs, len(jobs), _ptr(sumsq), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)),
-           "fog_grad_sumsq")
+    _floats(sumsq, "sumsq", torch.float64)
+    _jobs_here(jobs)
+    _check(load().fog_grad_sumsq(jobs, len(jobs), _ptr(sumsq), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                 _here(stream, sumsq, workspace)), "fog_grad_sumsq")
 
 
 def grad_sumsq_workspace(count):
@@ -398,7 +434,10 @@ def grad_sumsq_workspace(count):
 
 def grad_clip(jobs, sumsq, max_norm, norm=None, stream=None):
     """out = g * min(1, max_norm / sqrt(sumsq)) for every job; norm: receives sqrt(sumsq)."""
-    _check(load().fog_grad_clip(jobs, len(jobs), _ptr(sumsq), max_norm, _ptr(norm), _stream(stream)), "fog_grad_clip")
+    _floats(sumsq, "sumsq", torch.float64)
+    _floats(norm, "norm")
+    _jobs_here(jobs)
+    _check(load().fog_grad_clip(jobs, len(jobs), _ptr(sumsq), max_norm, _ptr(norm), _here(stream, sumsq, norm)), "fog_grad_clip")
 
 
 def fp8_attn_fwd(B, H, S, D, softmax_scale, causal, Q, K, V, sinv_q, sinv_k, sinv_v, scale_p, O, lse,

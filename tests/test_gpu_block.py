@@ -245,3 +245,20 @@ def test_empty_products():
     torch.cuda.synchronize()
     assert bool((C == 0).all())
     fog.quantize_block(none.view(torch.int16), fog.E4M3, q_row=none[:, :8], s_row=torch.empty((1, 0), dtype=torch.uint8, device="cuda"))
+
+
+def test_a_cast_beyond_32_bit_offsets():
+    """The last rows of a tensor of more than 2^31 elements, against the same rows cast by themselves."""
+    rows, cols, last = 65536 + 40, 33000, 40
+    x = torch.zeros((rows, cols), dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    x[-last:] = torch.randn((last, cols), device="cuda", generator=g)
+    q, s = torch.full((rows, cols), 0xA5, dtype=torch.uint8, device="cuda"), torch.empty((-(-cols // 128), rows), dtype=torch.uint8, device="cuda")
+    fog.quantize_block(x, fog.E4M3, q_row=q, s_row=s)
+    q1, s1 = torch.empty((last, cols), dtype=torch.uint8, device="cuda"), torch.empty((-(-cols // 128), last), dtype=torch.uint8, device="cuda")
+    fog.quantize_block(x[-last:], fog.E4M3, q_row=q1, s_row=s1)
+    assert torch.equal(q[-last:], q1) and torch.equal(s[:, -last:], s1)
+    assert int(torch.count_nonzero(q[:-last])) == 0 and bool((s[:, :-last] == 127).all())
+    fog.quantize_tile(x, fog.E4M3, q, torch.empty((-(-rows // 128), -(-cols // 128)), dtype=torch.uint8, device="cuda"))
+    assert int(torch.count_nonzero(q[:-last])) == 0 and int(torch.count_nonzero(q[-last:])) > last * cols // 2

@@ -137,3 +137,15 @@ def test_sums_of_shards_add_up_to_the_whole_norm():
     fog.grad_clip(fog.make_grad_jobs(halves[1]), total, 1e-2, norm)
     assert abs(norm.item() - want) <= 2.0 ** -23 * want
     assert len(np.unique(norm.cpu().numpy())) == 1
+
+
+def test_a_gradient_of_more_than_2_to_the_31_elements():
+    n = (1 << 31) + 12345
+    g = torch.full((n,), 2.0 ** -10, dtype=torch.bfloat16, device="cuda")
+    g[-1] = 3.0
+    _, sumsq = norm_of([g])
+    assert sumsq.item() == (n - 1) * 2.0 ** -20 + 9.0          # every partial sum is a multiple of 2^-20 below 2^33: exact
+    norm = torch.zeros(1, device="cuda")
+    fog.grad_clip(fog.make_grad_jobs([g]), sumsq, math.sqrt(sumsq.item()) / 2, norm)
+    # the factor is a half within a rounding or two: the products round to the exact halves
+    assert bool((g[:-1] == 2.0 ** -11).all()) and g[-1].item() == 1.5
