@@ -373,9 +373,10 @@ size_t fog_fp8_gemm_workspace(fog_layout layout, int64_t M, int64_t N, int64_t K
  *            both pairs (one pass over x); a pair that is not wanted is NULL.
  *   s_row  : [ceil(cols / 128)][rows] bytes, leading dimension lds_row >= rows;  s_col : [ceil(rows / 128)][cols] bytes,
  *            lds_col >= cols;  s : [ceil(rows / 128)][ceil(cols / 128)] bytes, lds >= ceil(cols / 128).  Any alignment.
- * NaN and infinities as in fog_quantize.  The fast path needs cols and ldx multiples of 8 and 16-byte aligned x, codes 8-byte aligned with
- * leading dimensions that are multiples of 8; other shapes go element by element with identical results.
- * Errors: NULL (also half of a pair), SHAPE (negative sizes, leading dimensions, margin), ALIGN (odd x), UNSUPPORTED (format).
+ * NaN and infinities as in fog_quantize.  Rows of any length, alignment and leading dimension; 16-byte aligned rows of x and 8-byte
+ * aligned rows of codes (cols and leading dimensions multiples of 8) are written twice as fast.
+ * Errors: NULL (also half of a pair), SHAPE (negative sizes, leading dimensions, margin), ALIGN (odd x), UNSUPPORTED (format; 2^23 tiles
+ * of 128 x 128 or more).
  */
 fog_status fog_quantize_block(const void* x_bf16, int64_t rows, int64_t cols, int64_t ldx, fog_fp8 fmt, int margin,
                               uint8_t* q_row, int64_t ldq_row, uint8_t* s_row, int64_t lds_row,
@@ -414,8 +415,8 @@ size_t fog_fp8_gemm_block_workspace(fog_layout layout, int64_t M, int64_t N, int
  *   factor : finite.   scale : one float; may be NULL without q.
  *   x_bf16 : [count, cols], leading dimension ldx.   q : NULL or [count, cols] bytes, leading dimension ldq.
  *   amax_out : NULL or one float, overwritten.
- * The fast path needs cols and leading dimensions multiples of 8, table and x 16-byte and q 8-byte aligned.
- * Errors: NULL, SHAPE, ALIGN, UNSUPPORTED (token_bytes, format, factor).
+ * Rows of any length, alignment and leading dimension; 16-byte aligned rows are the fastest.
+ * Errors: NULL, SHAPE, ALIGN, UNSUPPORTED (token_bytes, format, factor, cols above 2^33).
  */
 fog_status fog_embed_quantize(const void* tokens, int token_bytes, int64_t count, const void* table_bf16, int64_t vocab, int64_t cols,
                               int64_t ld_table, float factor, fog_fp8 fmt, const float* scale, void* x_bf16, int64_t ldx,
@@ -430,7 +431,7 @@ fog_status fog_embed_quantize(const void* tokens, int token_bytes, int64_t count
  *   workspace : fog_embed_grad_workspace(count, vocab, cols) bytes, 16-byte aligned; contents on entry do not matter.  Calls that may
  *            overlap in time need a workspace each.
  * Limits: count and cols below 2^31, vocab up to 4194302, count * max(cols, 512) up to 2^37.  The tokens are sorted in tiles of 1024 that are
- * merged by searching every tile for every token, which grows with count^2 / 1024 and stays below the sums up to about 10^5 tokens.
+ * merged by searching every tile for every token, which grows with count^2 / 1024: 20 us at 65536 tokens, 200 at 300000.
  * Errors: NULL, SHAPE, ALIGN, WORKSPACE, UNSUPPORTED (token_bytes, type, factor, limits).
  */
 typedef enum { FOG_BF16 = 0, FOG_F32 = 1 } fog_real;
@@ -446,7 +447,7 @@ size_t fog_embed_grad_workspace(int64_t count, int64_t vocab, int64_t cols);
  * Two calls, so that a job over several GPUs can add up the ranks' sums in between (one 8-byte all-reduce).  c is a binary32 number: below
  * 2^-126 it loses places.  A norm that is not finite leaves the gradients as they are and shows in `norm`: skip that step.
  *   jobs  : HOST array of `count` descriptions, read before the call returns; any number of tensors, 120 to a launch.
- *   g, out : n contiguous elements of `type`, aligned to their size (16-byte aligned ones are faster); out may be g (nothing is
+ *   g, out : n contiguous elements of `type`, aligned to their size; out may be g (nothing is
  *            written then where c is 1) and must not overlap any other gradient; fog_grad_sumsq does not look at it.
  *   sumsq : one double, overwritten by fog_grad_sumsq, 8-byte aligned.   norm : NULL or one float, overwritten
  *            (with FLT_MAX for a finite norm beyond it).

@@ -26,7 +26,6 @@ struct BlockCastArgs {
   int64_t rows, cols;
   int64_t tiles_c;
   int margin;
-  int stream;      // read past the caches
 };
 
 // k of the block's scale from the magnitude pattern of its abs-max (bf16 without sign; 0x7F80 and above: not finite)
@@ -70,19 +69,14 @@ FOG_DEVICE uint2 cast8(uint4 v, const float* f) {
 // Codes are written through: the product that reads them next finds them in the memory-side cache, and nothing is left to write back
 // while it runs (stored past the caches: a layer of 8192 x 2048 x 2048 forward and backward 152 us instead of 136, of 4096 x 4096 x 4096
 // 217 and 205; the cast of 8192 x 12288 both ways by itself 72 and 75).
-template <bool VEC>
-FOG_DEVICE void store8(uint8_t* q, int64_t at, uint2 v, int n) {
-  if (VEC) {
-    st_through8(q + at, v);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < n) q[at + i] = (uint8_t)((i < 4 ? v.x : v.y) >> (8 * (i & 3)));
-  }
+template <bool RAGGED>
+FOG_DEVICE void store8(uint8_t* q, uint2 v, int n) {
+  if (!RAGGED || n == 8) st_through8(q, v);
+  else                   st_upto8(q, v, n);
 }
 
-// VEC: x in 16-byte pieces, codes in 8-byte pieces (leading dimensions and cols multiples of 8, aligned pointers).
-template <int FMT, bool ROW, bool COL, bool TILE, bool VEC>
+// RAGGED: 8 does not divide the columns, and the last thread of a row takes its elements one by one.  STREAM: reads past the caches.
+template <int FMT, bool ROW, bool COL, bool TILE, bool RAGGED, bool STREAM>
 __global__ __launch_bounds__(kThreads) void block_cast_kernel(BlockCastArgs a) {
   constexpr int GROUP = kThreads / 16, PASSES = BLK / GROUP, WAVES = kThreads / 64;    // rows of a pass; pieces that a thread holds
   __shared__ uint32_t colmax[COL || TILE ? WAVES : 1][64];      // per wave: 128 columns' maxima in pairs
@@ -101,15 +95,9 @@ __global__ __launch_bounds__(kThreads) void block_cast_kernel(BlockCastArgs a) {
   for (int p = 0; p < PASSES; ++p) {
     v[p] = make_uint4(0, 0, 0, 0);
     if (GROUP * p + rr < nrows) {
-      if (VEC) {
-        if (n > 0) v[p] = a.stream ? ld_nt16(x + GROUP * p * a.ldx) : *reinterpret_cast<const uint4*>(x + GROUP * p * a.ldx);
-      } else {
-        uint32_t wv[4] = {0, 0, 0, 0};
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (i < n) wv[i >> 1] |= (uint32_t)x[GROUP * p * a.ldx + i] << (16 * (i & 1));
-        v[p] = make_uint4(wv[0], wv[1], wv[2], wv[3]);
-      }
+      const uint16_t* from = x + GROUP * p * a.ldx;
+      if (RAGGED && n < 8) v[p] = ld_upto8(from, n);
+      else if (n > 0)      v[p] = STREAM ? ld_any_nt16(from) : ld_any16(from);
     }
   }
   // maxima of the columns: over a thread's rows, over the wave's four lanes of a column group, and through LDS over the waves
@@ -155,7 +143,7 @@ __global__ __launch_bounds__(kThreads) void block_cast_kernel(BlockCastArgs a) {
       if ((t & 15) == 0) rowbyte[r] = (uint8_t)(127 - k);
       if (r < nrows && n > 0) {
         const uint2 o = __builtin_expect(rowmax >= 0x7F80u, 0) ? cast8<FMT, true>(v[p], f) : cast8<FMT, false>(v[p], f);
-        store8<VEC>(a.q_row, (r0 + r) * a.ldq_row + c0 + cc, o, n);
+        store8<RAGGED>(a.q_row + (r0 + r) * a.ldq_row + c0 + cc, o, n);
       }
     }
   }
@@ -174,7 +162,7 @@ __global__ __launch_bounds__(kThreads) void block_cast_kernel(BlockCastArgs a) {
       const int r = GROUP * p + rr;
       if (r < nrows && n > 0) {
         const uint2 o = __builtin_expect(odd, 0) ? cast8<FMT, true>(v[p], f) : cast8<FMT, false>(v[p], f);
-        store8<VEC>(a.q_col, (r0 + r) * a.ldq_col + c0 + cc, o, n);
+        store8<RAGGED>(a.q_col + (r0 + r) * a.ldq_col + c0 + cc, o, n);
       }
     }
   }
@@ -192,7 +180,7 @@ __global__ __launch_bounds__(kThreads) void block_cast_kernel(BlockCastArgs a) {
       const int r = GROUP * p + rr;
       if (r < nrows && n > 0) {
         const uint2 o = __builtin_expect(m >= 0x7F80u, 0) ? cast8<FMT, true>(v[p], f) : cast8<FMT, false>(v[p], f);
-        store8<VEC>(a.q_row, (r0 + r) * a.ldq_row + c0 + cc, o, n);
+        store8<RAGGED>(a.q_row + (r0 + r) * a.ldq_row + c0 + cc, o, n);
       }
     }
   }
@@ -206,14 +194,19 @@ fog_status launch(BlockCastArgs a, fog_fp8 fmt, hipStream_t s) {
   const int64_t tiles = a.tiles_c * ((a.rows + BLK - 1) / BLK);
   // what the kernel before has left in the caches is worth finding up to about 16 M elements (past the caches and as ordinary loads: the layer of
   // 1777 x 3088 x 2064 86.0 and 81.5 us, 4096 x 8192 x 2048 forward 76.9 and 74.8, 4096 x 4096 x 4096 205 and 207, 8192 x 4096 x 14336 1180 and 1210)
-  a.stream = a.rows * a.cols > ((int64_t)16 << 20);
-  if (tiles > 0x7FFFFFFF) return FOG_ERR_UNSUPPORTED;
-  const bool vec = a.cols % 8 == 0 && a.ldx % 8 == 0 && aligned(a.x, 16) && (!(ROW || TILE) || (aligned(a.q_row, 8) && a.ldq_row % 8 == 0)) &&
-                   (!COL || (aligned(a.q_col, 8) && a.ldq_col % 8 == 0));
-  const int grid = (int)tiles;
-#define FOG_BC(F, V) block_cast_kernel<F, ROW, COL, TILE, V><<<grid, kThreads, 0, s>>>(a)
-  if (fmt == FOG_E4M3) { if (vec) FOG_BC(FOG_E4M3, true); else FOG_BC(FOG_E4M3, false); }
-  else                 { if (vec) FOG_BC(FOG_E5M2, true); else FOG_BC(FOG_E5M2, false); }
+  // (rows that begin inside a line share it with the row before: 4096 x 4097 both ways 24 us past the caches, 19.5 without)
+  const bool ragged = a.cols % 8 != 0, stream = !ragged && a.rows * a.cols > ((int64_t)16 << 20);
+  if (tiles >= (1 << 23)) return FOG_ERR_UNSUPPORTED;      // grids are counted in threads of 32 bits
+#define FOG_BC(F, R, S) block_cast_kernel<F, ROW, COL, TILE, R, S><<<(int)tiles, kThreads, 0, s>>>(a)
+#define FOG_BR(F)                                       \
+  do {                                                  \
+    if (ragged)      FOG_BC(F, true, false);            \
+    else if (stream) FOG_BC(F, false, true);            \
+    else             FOG_BC(F, false, false);           \
+  } while (0)
+  if (fmt == FOG_E4M3) FOG_BR(FOG_E4M3);
+  else                 FOG_BR(FOG_E5M2);
+#undef FOG_BR
 #undef FOG_BC
   return fog_launch_status();
 }
@@ -229,7 +222,7 @@ extern "C" fog_status fog_quantize_block(const void* x_bf16, int64_t rows, int64
   if (!x_bf16 || (!q_row && !q_col) || (!q_row) != (!s_row) || (!q_col) != (!s_col)) return FOG_ERR_NULL;
   if (ldx < cols || (q_row && (ldq_row < cols || lds_row < rows)) || (q_col && (ldq_col < cols || lds_col < cols))) return FOG_ERR_SHAPE;
   if (!aligned(x_bf16, 2)) return FOG_ERR_ALIGN;
-  const BlockCastArgs a{reinterpret_cast<const uint16_t*>(x_bf16), q_row, s_row, q_col, s_col, ldx, ldq_row, lds_row, ldq_col, lds_col, rows, cols, 0, margin, 0};
+  const BlockCastArgs a{reinterpret_cast<const uint16_t*>(x_bf16), q_row, s_row, q_col, s_col, ldx, ldq_row, lds_row, ldq_col, lds_col, rows, cols, 0, margin};
   hipStream_t s = (hipStream_t)stream;
   if (q_row && q_col) return launch<true, true, false>(a, fmt, s);
   return q_row ? launch<true, false, false>(a, fmt, s) : launch<false, true, false>(a, fmt, s);
@@ -243,6 +236,6 @@ extern "C" fog_status fog_quantize_tile(const void* x_bf16, int64_t rows, int64_
   if (!x_bf16 || !q || !s) return FOG_ERR_NULL;
   if (ldx < cols || ldq < cols || lds < (cols + BLK - 1) / BLK) return FOG_ERR_SHAPE;
   if (!aligned(x_bf16, 2)) return FOG_ERR_ALIGN;
-  const BlockCastArgs a{reinterpret_cast<const uint16_t*>(x_bf16), q, s, nullptr, nullptr, ldx, ldq, lds, 0, 0, rows, cols, 0, margin, 0};
+  const BlockCastArgs a{reinterpret_cast<const uint16_t*>(x_bf16), q, s, nullptr, nullptr, ldx, ldq, lds, 0, 0, rows, cols, 0, margin};
   return launch<false, false, true>(a, fmt, (hipStream_t)stream);
 }

@@ -147,6 +147,46 @@ FOG_DEVICE void st_nt8(void* p, uint2 v) {
   __builtin_nontemporal_store(w, reinterpret_cast<u32x2*>(p));
 }
 
+// The same for data that is aligned to its element only (rows of any length): the memory instructions of this part take any address, the
+// types tell the compiler that they may.  An aligned address costs nothing more.
+typedef u32x4 __attribute__((aligned(2))) u32x4_any;
+FOG_DEVICE uint4 ld_any16(const void* p) {
+  const u32x4 v = *reinterpret_cast<const u32x4_any*>(p);
+  return make_uint4(v[0], v[1], v[2], v[3]);
+}
+FOG_DEVICE uint4 ld_any_nt16(const void* p) {
+  const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const u32x4_any*>(p));
+  return make_uint4(v[0], v[1], v[2], v[3]);
+}
+FOG_DEVICE void st_any16(void* p, uint4 v) {
+  u32x4 w = {v.x, v.y, v.z, v.w};
+  *reinterpret_cast<u32x4_any*>(p) = w;
+}
+FOG_DEVICE void st_any_nt16(void* p, uint4 v) {
+  u32x4 w = {v.x, v.y, v.z, v.w};
+  __builtin_nontemporal_store(w, reinterpret_cast<u32x4_any*>(p));
+}
+// Eight 16-bit elements from p on of which n are there; zeros behind them.
+FOG_DEVICE uint4 ld_upto8(const uint16_t* p, int n) {
+  uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (i < n) w[i >> 1] |= (uint32_t)p[i] << (16 * (i & 1));
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// The first n (< 8) of eight 16-bit elements, and of eight codes.
+FOG_DEVICE void st_upto8(uint16_t* p, uint4 v, int n) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (i < n) p[i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
+}
+FOG_DEVICE void st_upto8(uint8_t* p, uint2 v, int n) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (i < n) p[i] = (uint8_t)((i < 4 ? v.x : v.y) >> (8 * (i & 3)));
+}
+
 // Stores written through: the lines stay in the caches for the next kernel, but clean, so that nothing is left to write back when the
 // kernel ends or while the next one runs.  (The two wait states cover the rule that the data registers of a store of more than 8 bytes
 // must not be written by the next two vector instructions; the compiler, which keeps it for its own stores, does not see the one inside

@@ -33,103 +33,99 @@ FOG_DEVICE int64_t token_at(const void* tokens, int wide, int64_t i) {
 struct EmbedArgs {
   const void* tokens;
   int wide;
-  int64_t count, vocab, cols, ld_table, ldx, ldq;
+  int64_t vocab, cols, ld_table, ldx, ldq;
   const uint16_t* table;
   float factor;
   const float* scale;
   uint16_t* x;
   uint8_t* q;
   uint32_t* amax_out;
-  int lanes;    // threads of a row, a power of two
+  uint32_t pieces, per_row;    // pieces of eight elements of all rows, of a row
 };
 
-// Eight elements of a row of the table times the factor, rounded to bf16.
-FOG_DEVICE uint4 scaled_piece(uint4 v, float f) {
-  return make_uint4(pack_bf16x2(bf16lo(v.x) * f, bf16hi(v.x) * f), pack_bf16x2(bf16lo(v.y) * f, bf16hi(v.y) * f),
-                    pack_bf16x2(bf16lo(v.z) * f, bf16hi(v.z) * f), pack_bf16x2(bf16lo(v.w) * f, bf16hi(v.w) * f));
-}
-// Stores them with their codes; returns the running maximum.
-template <int FMT>
-FOG_DEVICE uint32_t store_piece(const EmbedArgs& a, int64_t r, int64_t c, uint4 v, float rho, uint32_t m) {
-  m = pkmax_abs_bf16(m, v.x); m = pkmax_abs_bf16(m, v.y); m = pkmax_abs_bf16(m, v.z); m = pkmax_abs_bf16(m, v.w);
-  st_nt16(a.x + r * a.ldx + c, v);
-  if (a.q)
-    st_nt8(a.q + r * a.ldq + c, make_uint2(cvt4_fp8_nan<FMT>(bf16lo(v.x) * rho, bf16hi(v.x) * rho, bf16lo(v.y) * rho, bf16hi(v.y) * rho),
-                                           cvt4_fp8_nan<FMT>(bf16lo(v.z) * rho, bf16hi(v.z) * rho, bf16lo(v.w) * rho, bf16hi(v.w) * rho)));
-  return m;
-}
-
-// VEC: rows of the table, of x and of q in pieces of eight elements.
-template <int FMT, bool VEC>
-__global__ __launch_bounds__(kThreads) void embed_kernel(EmbedArgs a) {
+// A workgroup takes the pieces first, first + step, ... four at a time: all four ids, then all four pieces, are asked for before the first
+// is used.  RAGGED: 8 does not divide the columns, the last piece of a row goes element by element.  Returns the thread's largest magnitude in
+// packed pairs.
+template <int FMT, bool RAGGED>
+FOG_DEVICE uint32_t embed_pieces(const EmbedArgs& a, uint32_t first, uint32_t step) {
+  constexpr int AHEAD = 4;
   const float rho = a.q ? *a.scale : 0.0f;
-  const int per_wg = kThreads / a.lanes, lane = threadIdx.x & (a.lanes - 1);
   uint32_t m = 0u;
-  for (int64_t r = (int64_t)blockIdx.x * per_wg + threadIdx.x / a.lanes; r < a.count; r += (int64_t)gridDim.x * per_wg) {
-    const int64_t id = token_at(a.tokens, a.wide, r);
-    const bool in = id >= 0 && id < a.vocab;
-    const uint16_t* e = a.table + (in ? id : 0) * a.ld_table;
-    if (VEC) {
-      for (int64_t c = 8 * (int64_t)lane; c < a.cols; c += 8 * (int64_t)a.lanes) {
-        m = store_piece<FMT>(a, r, c, in ? scaled_piece(*reinterpret_cast<const uint4*>(e + c), a.factor) : make_uint4(0, 0, 0, 0), rho, m);
-      }
-    } else {
-      for (int64_t c = lane; c < a.cols; c += a.lanes) {
-        const uint32_t b = in ? f32_to_bf16(bf16lo(e[c]) * a.factor) : 0u;
-        const uint32_t mag = b & 0x7FFFu;
-        m = max_of_pair(m) > mag ? max_of_pair(m) : mag;
-        a.x[r * a.ldx + c] = (uint16_t)b;
-        if (a.q) {
-          const float t = bf16lo(b) * rho;
-          a.q[r * a.ldq + c] = (uint8_t)(cvt4_fp8_nan<FMT>(t, t, t, t) & 0xFFu);
-        }
+  for (uint64_t base = first; base < a.pieces; base += (uint64_t)AHEAD * step) {
+    uint32_t row[AHEAD], col[AHEAD];
+    int64_t id[AHEAD];
+    uint4 v[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const uint64_t p = base + (uint64_t)u * step;
+      row[u] = (uint32_t)p / a.per_row;
+      col[u] = 8u * ((uint32_t)p - row[u] * a.per_row);
+      id[u] = p < a.pieces ? token_at(a.tokens, a.wide, row[u]) : -1;
+      if (id[u] >= a.vocab) id[u] = -1;
+    }
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      v[u] = make_uint4(0, 0, 0, 0);
+      if (id[u] < 0) continue;
+      const uint16_t* e = a.table + id[u] * a.ld_table + col[u];
+      if (!RAGGED || col[u] + 8 <= a.cols) v[u] = ld_any16(e);
+      else                                 v[u] = ld_upto8(e, (int)(a.cols - col[u]));
+    }
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      if (base + (uint64_t)u * step >= a.pieces) break;
+      const float f = a.factor;
+      uint4 o = v[u];
+      if (id[u] >= 0)
+        o = make_uint4(pack_bf16x2(bf16lo(o.x) * f, bf16hi(o.x) * f), pack_bf16x2(bf16lo(o.y) * f, bf16hi(o.y) * f),
+                       pack_bf16x2(bf16lo(o.z) * f, bf16hi(o.z) * f), pack_bf16x2(bf16lo(o.w) * f, bf16hi(o.w) * f));
+      const int n = !RAGGED || col[u] + 8 <= a.cols ? 8 : (int)(a.cols - col[u]);
+      m = pkmax_abs_bf16(m, o.x); m = pkmax_abs_bf16(m, o.y); m = pkmax_abs_bf16(m, o.z); m = pkmax_abs_bf16(m, o.w);
+      if (n < 8) st_upto8(a.x + row[u] * a.ldx + col[u], o, n);
+      else       st_through16(a.x + row[u] * a.ldx + col[u], o);
+      if (a.q) {
+        const uint2 c = make_uint2(cvt4_fp8_nan<FMT>(bf16lo(o.x) * rho, bf16hi(o.x) * rho, bf16lo(o.y) * rho, bf16hi(o.y) * rho),
+                                   cvt4_fp8_nan<FMT>(bf16lo(o.z) * rho, bf16hi(o.z) * rho, bf16lo(o.w) * rho, bf16hi(o.w) * rho));
+        if (n < 8) st_upto8(a.q + row[u] * a.ldq + col[u], c, n);
+        else       st_through8(a.q + row[u] * a.ldq + col[u], c);
       }
     }
   }
-  if (a.amax_out) {
-    const uint32_t top = wave_max_u32(max_of_pair(m)) << 16;     // the float with that bf16 pattern
-    if ((threadIdx.x & 63) == 0 && top > __hip_atomic_load(a.amax_out, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(a.amax_out, top);
-  }
+  return m;
 }
 
-// Up to SMALL pieces of eight elements (a decoding step's tokens), with an abs-max: one workgroup, so that the abs-max needs no word that
-// a launch before has cleared.  All ids, then all pieces, are asked for before the first is used.
-constexpr int SMALL_THREADS = 1024, SMALL_PER = 8, SMALL = SMALL_THREADS * SMALL_PER;
-template <int FMT>
-__global__ __launch_bounds__(SMALL_THREADS) void embed_small_kernel(EmbedArgs a) {
-  const float rho = a.q ? *a.scale : 0.0f;
-  const int per_row = (int)(a.cols / 8), pieces = (int)a.count * per_row;
-  int row[SMALL_PER], at[SMALL_PER];
-  int64_t id[SMALL_PER];
-#pragma unroll
-  for (int u = 0; u < SMALL_PER; ++u) {
-    const int p = threadIdx.x + u * SMALL_THREADS;
-    row[u] = p / per_row;
-    at[u] = 8 * (p - row[u] * per_row);
-    id[u] = p < pieces ? token_at(a.tokens, a.wide, row[u]) : -1;
-  }
-  uint4 v[SMALL_PER];
-#pragma unroll
-  for (int u = 0; u < SMALL_PER; ++u) {
-    v[u] = make_uint4(0, 0, 0, 0);
-    if (id[u] >= 0 && id[u] < a.vocab) v[u] = *reinterpret_cast<const uint4*>(a.table + id[u] * a.ld_table + at[u]);
-    else                               id[u] = -1;
-  }
-  uint32_t m = 0u;
-#pragma unroll
-  for (int u = 0; u < SMALL_PER; ++u) {
-    if ((int)threadIdx.x + u * SMALL_THREADS >= pieces) break;
-    if (id[u] >= 0) v[u] = scaled_piece(v[u], a.factor);
-    m = store_piece<FMT>(a, row[u], at[u], v[u], rho, m);
-  }
+// The workgroup's largest magnitude as the bits of a float, in thread 0.
+constexpr int EMBED_THREADS = 1024;
+FOG_DEVICE uint32_t group_amax(uint32_t m) {
+  __shared__ uint32_t part[EMBED_THREADS / 64];
   m = wave_max_u32(max_of_pair(m));
-  __shared__ uint32_t part[SMALL_THREADS / 64];
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
   __syncthreads();
   if (threadIdx.x == 0) {
-    for (int w = 1; w < SMALL_THREADS / 64; ++w) m = m > part[w] ? m : part[w];
-    *a.amax_out = m << 16;
+#pragma unroll
+    for (int w = 1; w < EMBED_THREADS / 64; ++w) m = m > part[w] ? m : part[w];
   }
+  return m << 16;      // the float with that bf16 pattern
+}
+
+// With an abs-max one workgroup a compute unit, which ends with one atomic at most: an atomic of each wave of 1112 rows of 3568, all at the
+// same time, took 30 us where the rows take 8.  Rows and codes are written through, for the cast or the product that reads them next:
+// 8192 x 4096 with codes 26 us (floor at 4.8 TB/s, every row from memory: 35); followed by the block cast 44 us, and 47 with stores past the caches.
+template <int FMT, bool RAGGED>
+__global__ __launch_bounds__(EMBED_THREADS) void embed_kernel(EmbedArgs a) {
+  const uint32_t m = embed_pieces<FMT, RAGGED>(a, blockIdx.x * EMBED_THREADS + threadIdx.x, gridDim.x * EMBED_THREADS);
+  if (!a.amax_out) return;
+  const uint32_t top = group_amax(m);
+  if (threadIdx.x == 0 && top > __hip_atomic_load(a.amax_out, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(a.amax_out, top);
+}
+
+// Up to SMALL pieces (a decoding step's tokens) with an abs-max: one workgroup, so that the abs-max needs no word that a launch before has
+// cleared.
+constexpr uint32_t SMALL = 8 * EMBED_THREADS;
+template <int FMT, bool RAGGED>
+__global__ __launch_bounds__(EMBED_THREADS) void embed_small_kernel(EmbedArgs a) {
+  const uint32_t top = group_amax(embed_pieces<FMT, RAGGED>(a, threadIdx.x, EMBED_THREADS));
+  if (threadIdx.x == 0) *a.amax_out = top;
 }
 
 // ---------------------------------------------------------------- gradient: order of the tokens
@@ -151,7 +147,7 @@ struct Fill {
   int64_t row_bytes, ld_bytes;
   int64_t first, units;       // units of 4 KB that this launch writes
   uint32_t per_row;           // units of a row
-  int one_row, vec, size;
+  int one_row;
 };
 constexpr int FILL_UNIT = 16 * kThreads;
 // Small workgroups that each write 16 bytes a thread and end: 2.1 GB take 313 us this way, 356 with four stores a thread, 343 and 377
@@ -166,14 +162,11 @@ FOG_DEVICE void fill_zeros(const Fill& f, int64_t group, int64_t groups) {
       at = (int64_t)((uint32_t)u - (uint32_t)row * f.per_row) * FILL_UNIT;
     }
     uint8_t* p = f.p + row * f.ld_bytes;
-    if (f.vec) {
-      if (at + 16 * t < f.row_bytes) *reinterpret_cast<uint4*>(p + at + 16 * t) = make_uint4(0, 0, 0, 0);
+    at += 16 * t;
+    if (at + 16 <= f.row_bytes) {
+      st_any16(p + at, make_uint4(0, 0, 0, 0));
     } else {
-      for (int i = t * f.size; i < FILL_UNIT; i += kThreads * f.size) {
-        if (at + i >= f.row_bytes) break;
-        if (f.size == 4) *reinterpret_cast<uint32_t*>(p + at + i) = 0u;
-        else             *reinterpret_cast<uint16_t*>(p + at + i) = 0;
-      }
+      for (; at < f.row_bytes; at += 2) *reinterpret_cast<uint16_t*>(p + at) = 0;
     }
   }
 }
@@ -372,21 +365,18 @@ struct GradArgs {
   int64_t units;            // waves: chunks * slabs
 };
 
-template <bool F32, bool VEC>
+// RAGGED: 8 does not divide the columns, the last lane of a row takes its elements one by one.
+template <bool F32, bool RAGGED>
 struct Row {
   float v[8];
   __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = 0.0f;
   }
-  // + the row of dx at p (n of its elements are inside)
+  // eight elements of dx of which n are inside the row
   static __device__ __forceinline__ uint4 load(const uint16_t* p, int n) {
-    if (VEC) return n > 0 ? ld_nt16(p) : make_uint4(0, 0, 0, 0);
-    uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < n) w[i >> 1] |= (uint32_t)p[i] << (16 * (i & 1));
-    return make_uint4(w[0], w[1], w[2], w[3]);
+    if (RAGGED && n < 8) return ld_upto8(p, n);
+    return n > 0 ? ld_any_nt16(p) : make_uint4(0, 0, 0, 0);
   }
   __device__ __forceinline__ void add(uint4 x) {
     v[0] += bf16lo(x.x); v[1] += bf16hi(x.x); v[2] += bf16lo(x.y); v[3] += bf16hi(x.y);
@@ -394,16 +384,17 @@ struct Row {
   }
   // n floats of a piece in the workspace, zeros behind them
   static __device__ __forceinline__ void load_floats(float* x, const float* p, int n) {
-    if (VEC) {
-      float4 lo = make_float4(0.0f, 0.0f, 0.0f, 0.0f), hi = lo;
-      if (n > 0) {
-        lo = *reinterpret_cast<const float4*>(p);
-        hi = *reinterpret_cast<const float4*>(p + 4);
-      }
-      x[0] = lo.x; x[1] = lo.y; x[2] = lo.z; x[3] = lo.w; x[4] = hi.x; x[5] = hi.y; x[6] = hi.z; x[7] = hi.w;
-    } else {
+    if (RAGGED && n < 8) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] = i < n ? p[i] : 0.0f;
+    } else {
+      uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
+      if (n > 0) {
+        lo = ld_any16(p);
+        hi = ld_any16(p + 4);
+      }
+      x[0] = __uint_as_float(lo.x); x[1] = __uint_as_float(lo.y); x[2] = __uint_as_float(lo.z); x[3] = __uint_as_float(lo.w);
+      x[4] = __uint_as_float(hi.x); x[5] = __uint_as_float(hi.y); x[6] = __uint_as_float(hi.z); x[7] = __uint_as_float(hi.w);
     }
   }
   __device__ __forceinline__ void add_floats(const float* p, int n) {
@@ -412,15 +403,17 @@ struct Row {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] += x[i];
   }
+  static __device__ __forceinline__ uint4 bits(const float* x) {
+    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+  }
   __device__ __forceinline__ void put_floats(float* p, int n) const {
-    if (VEC) {
-      if (n <= 0) return;
-      *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-      *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
-    } else {
+    if (RAGGED && n < 8) {
 #pragma unroll
       for (int i = 0; i < 8; ++i)
         if (i < n) p[i] = v[i];
+    } else if (n > 0) {
+      st_any16(p, bits(v));
+      st_any16(p + 4, bits(v + 4));
     }
   }
   // the finished sum times the factor (added to what is there) to the table's gradient
@@ -431,37 +424,35 @@ struct Row {
     for (int i = 0; i < 8; ++i) r[i] = v[i] * a.factor;
     if (F32) {
       float* p = reinterpret_cast<float*>(a.dE) + id * a.ld_dE + col;
-      if (VEC) {
-        if (a.accumulate) {
-          const float4 x = *reinterpret_cast<const float4*>(p), y = *reinterpret_cast<const float4*>(p + 4);
-          r[0] += x.x; r[1] += x.y; r[2] += x.z; r[3] += x.w; r[4] += y.x; r[5] += y.y; r[6] += y.z; r[7] += y.w;
-        }
-        st_nt16(p, make_uint4(__float_as_uint(r[0]), __float_as_uint(r[1]), __float_as_uint(r[2]), __float_as_uint(r[3])));
-        st_nt16(p + 4, make_uint4(__float_as_uint(r[4]), __float_as_uint(r[5]), __float_as_uint(r[6]), __float_as_uint(r[7])));
-      } else {
+      if (a.accumulate) {
+        float x[8];
+        load_floats(x, p, n);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r[i] += x[i];
+      }
+      if (RAGGED && n < 8) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          if (i < n) p[i] = a.accumulate ? p[i] + r[i] : r[i];
+          if (i < n) p[i] = r[i];
+      } else {
+        st_any_nt16(p, bits(r));
+        st_any_nt16(p + 4, bits(r + 4));
       }
     } else {
       uint16_t* p = reinterpret_cast<uint16_t*>(a.dE) + id * a.ld_dE + col;
-      if (VEC) {
-        if (a.accumulate) {
-          const uint4 x = *reinterpret_cast<const uint4*>(p);
-          r[0] += bf16lo(x.x); r[1] += bf16hi(x.x); r[2] += bf16lo(x.y); r[3] += bf16hi(x.y);
-          r[4] += bf16lo(x.z); r[5] += bf16hi(x.z); r[6] += bf16lo(x.w); r[7] += bf16hi(x.w);
-        }
-        st_nt16(p, make_uint4(pack_bf16x2(r[0], r[1]), pack_bf16x2(r[2], r[3]), pack_bf16x2(r[4], r[5]), pack_bf16x2(r[6], r[7])));
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (i < n) p[i] = (uint16_t)f32_to_bf16(a.accumulate ? bf16lo(p[i]) + r[i] : r[i]);
+      if (a.accumulate) {
+        const uint4 x = RAGGED && n < 8 ? ld_upto8(p, n) : ld_any16(p);
+        r[0] += bf16lo(x.x); r[1] += bf16hi(x.x); r[2] += bf16lo(x.y); r[3] += bf16hi(x.y);
+        r[4] += bf16lo(x.z); r[5] += bf16hi(x.z); r[6] += bf16lo(x.w); r[7] += bf16hi(x.w);
       }
+      const uint4 o = make_uint4(pack_bf16x2(r[0], r[1]), pack_bf16x2(r[2], r[3]), pack_bf16x2(r[4], r[5]), pack_bf16x2(r[6], r[7]));
+      if (RAGGED && n < 8) st_upto8(p, o, n);
+      else                 st_any_nt16(p, o);
     }
   }
 };
 
-template <bool F32, bool VEC>
+template <bool F32, bool RAGGED>
 __global__ __launch_bounds__(kThreads) void sum_runs_kernel(GradArgs a) {
   const int l = threadIdx.x & 63;
   const int64_t unit = (int64_t)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -476,7 +467,7 @@ __global__ __launch_bounds__(kThreads) void sum_runs_kernel(GradArgs a) {
   const uint32_t before = p0 > 0 ? a.ids[p0 - 1] : 0xFFFFFFFFu;
   const uint32_t after = p0 + len < a.count ? a.ids[p0 + len] : 0xFFFFFFFFu;
   constexpr int AHEAD = 8;
-  Row<F32, VEC> sum;
+  Row<F32, RAGGED> sum;
   sum.clear();
   uint32_t cur = (uint32_t)__builtin_amdgcn_readlane((int)id_l, 0);
   bool began = cur != before;       // the current run begins in this chunk
@@ -489,7 +480,7 @@ __global__ __launch_bounds__(kThreads) void sum_runs_kernel(GradArgs a) {
       id[u] = (uint32_t)__builtin_amdgcn_readlane((int)id_l, i);
       const uint32_t pos = (uint32_t)__builtin_amdgcn_readlane((int)pos_l, i);
       v[u] = make_uint4(0, 0, 0, 0);
-      if (i0 + u < len && id[u] < (uint32_t)a.vocab) v[u] = Row<F32, VEC>::load(a.dx + (int64_t)pos * a.ld_dx + col, n);
+      if (i0 + u < len && id[u] < (uint32_t)a.vocab) v[u] = Row<F32, RAGGED>::load(a.dx + (int64_t)pos * a.ld_dx + col, n);
     }
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
@@ -513,7 +504,7 @@ __global__ __launch_bounds__(kThreads) void sum_runs_kernel(GradArgs a) {
 // A workgroup for each chunk and slab; those whose chunk ends inside a run that it began add up the run's pieces: the eight waves an eighth
 // of the chunks each, then the eight sums in order.
 constexpr int JOIN_WAVES = 8;
-template <bool F32, bool VEC>
+template <bool F32, bool RAGGED>
 __global__ __launch_bounds__(64 * JOIN_WAVES) void join_runs_kernel(GradArgs a) {
   const int64_t c = (int64_t)blockIdx.x / a.slabs;
   const int64_t next = (c + 1) * a.chunk;              // first token of the next chunk
@@ -533,14 +524,14 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void join_runs_kernel(GradArgs a) 
   const int64_t col = ((int64_t)blockIdx.x - c * a.slabs) * SLAB + 8 * l;
   const int n = a.cols - col >= 8 ? 8 : a.cols > col ? (int)(a.cols - col) : 0;
   const int64_t per = (m + JOIN_WAVES - 1) / JOIN_WAVES, b = c + 1 + w * per, e = b + per < c + m + 1 ? b + per : c + m + 1;
-  Row<F32, VEC> sum;
+  Row<F32, RAGGED> sum;
   sum.clear();
   if (w == 0) sum.add_floats(a.tail + c * a.cols + col, n);
   constexpr int AHEAD = 8;
   for (int64_t i = b; i < e; i += AHEAD) {
     float v[AHEAD][8];
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u) Row<F32, VEC>::load_floats(v[u], a.head + (i + u) * a.cols + col, i + u < e ? n : 0);
+    for (int u = 0; u < AHEAD; ++u) Row<F32, RAGGED>::load_floats(v[u], a.head + (i + u) * a.cols + col, i + u < e ? n : 0);
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u)
 #pragma unroll
@@ -584,6 +575,8 @@ GradRoom room_of(int64_t count, int64_t cols) {
 
 constexpr int64_t GROUPS_MAX = 1 << 22;    // workgroups of a launch (up to 512 threads each): grids are counted in threads of 32 bits
 
+constexpr int64_t PIECES_MAX = 1 << 30;    // pieces of a launch of the forward
+
 inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
 }  // namespace
@@ -602,27 +595,40 @@ extern "C" fog_status fog_embed_quantize(const void* tokens, int token_bytes, in
     if (!aligned(tokens, token_bytes) || !aligned(table_bf16, 2) || !aligned(x_bf16, 2)) return FOG_ERR_ALIGN;
   }
   hipStream_t s = (hipStream_t)stream;
-  EmbedArgs a{tokens, token_bytes == 8, count, vocab, cols, ld_table, ldx, ldq, reinterpret_cast<const uint16_t*>(table_bf16), factor, scale,
-              reinterpret_cast<uint16_t*>(x_bf16), q, reinterpret_cast<uint32_t*>(amax_out), kThreads};
-  const bool vec = cols % 8 == 0 && ld_table % 8 == 0 && ldx % 8 == 0 && aligned(table_bf16, 16) && aligned(x_bf16, 16) &&
-                   (!q || (ldq % 8 == 0 && aligned(q, 8)));
-  if (any && amax_out && vec && cols <= 8 * SMALL && count * (cols / 8) <= SMALL) {
-    if (fmt == FOG_E4M3) embed_small_kernel<FOG_E4M3><<<1, SMALL_THREADS, 0, s>>>(a);
-    else                 embed_small_kernel<FOG_E5M2><<<1, SMALL_THREADS, 0, s>>>(a);
+  EmbedArgs a{tokens, token_bytes == 8, vocab, cols, ld_table, ldx, ldq, reinterpret_cast<const uint16_t*>(table_bf16), factor, scale,
+              reinterpret_cast<uint16_t*>(x_bf16), q, reinterpret_cast<uint32_t*>(amax_out), 0, 0};
+  const int64_t per_row = (cols + 7) / 8;
+  const bool ragged = cols % 8 != 0;
+  if (per_row > PIECES_MAX) return FOG_ERR_UNSUPPORTED;
+  if (any && amax_out && per_row <= SMALL && count * per_row <= SMALL) {
+    a.per_row = (uint32_t)per_row;
+    a.pieces = (uint32_t)(count * per_row);
+#define FOG_EM(F, R) embed_small_kernel<F, R><<<1, EMBED_THREADS, 0, s>>>(a)
+    if (fmt == FOG_E4M3) { if (ragged) FOG_EM(FOG_E4M3, true); else FOG_EM(FOG_E4M3, false); }
+    else                 { if (ragged) FOG_EM(FOG_E5M2, true); else FOG_EM(FOG_E5M2, false); }
+#undef FOG_EM
     return fog_launch_status();
   }
   if (amax_out) zero_u32e<<<1, 1, 0, s>>>(reinterpret_cast<uint32_t*>(amax_out));
   if (!any) return amax_out ? fog_launch_status() : FOG_OK;
-  const int64_t pieces = vec ? cols / 8 : cols;
-  while (a.lanes > 16 && a.lanes / 2 >= pieces) a.lanes /= 2;
-  const int64_t per_wg = kThreads / a.lanes;
-  int64_t blocks = (count + per_wg - 1) / per_wg;
-  const int64_t most = 8 * (int64_t)fog_compute_units();
-  if (blocks > most) blocks = most;
-#define FOG_EM(F, V) embed_kernel<F, V><<<(int)blocks, kThreads, 0, s>>>(a)
-  if (fmt == FOG_E4M3) { if (vec) FOG_EM(FOG_E4M3, true); else FOG_EM(FOG_E4M3, false); }
-  else                 { if (vec) FOG_EM(FOG_E5M2, true); else FOG_EM(FOG_E5M2, false); }
+  // pieces are counted in 32 bits: as many rows a launch as that allows
+  const int64_t rows = PIECES_MAX / per_row;
+  for (int64_t r = 0; r < count; r += rows) {
+    const int64_t n = count - r < rows ? count - r : rows;
+    EmbedArgs b = a;
+    b.tokens = reinterpret_cast<const uint8_t*>(tokens) + r * token_bytes;
+    b.x = a.x + r * ldx;
+    b.q = a.q ? a.q + r * ldq : nullptr;
+    b.per_row = (uint32_t)per_row;
+    b.pieces = (uint32_t)(n * per_row);
+    int64_t groups = (n * per_row + EMBED_THREADS - 1) / EMBED_THREADS;
+    const int64_t most = (amax_out ? 1 : 4) * (int64_t)fog_compute_units();
+    if (groups > most) groups = most;
+#define FOG_EM(F, R) embed_kernel<F, R><<<(int)groups, EMBED_THREADS, 0, s>>>(b)
+    if (fmt == FOG_E4M3) { if (ragged) FOG_EM(FOG_E4M3, true); else FOG_EM(FOG_E4M3, false); }
+    else                 { if (ragged) FOG_EM(FOG_E5M2, true); else FOG_EM(FOG_E5M2, false); }
 #undef FOG_EM
+  }
   return fog_launch_status();
 }
 
@@ -666,8 +672,7 @@ extern "C" fog_status fog_embed_grad(const void* tokens, int token_bytes, int64_
   a.chunks = (count + a.chunk - 1) / a.chunk;
   a.units = a.chunks * a.slabs;
   if (a.units > GROUPS_MAX) return FOG_ERR_UNSUPPORTED;
-  const bool vec = cols % 8 == 0 && ld_dE % 8 == 0 && aligned(dE, 16) && (count == 0 || (ld_dx % 8 == 0 && aligned(dx_bf16, 16)));
-  Fill fill{reinterpret_cast<uint8_t*>(dE), cols * size, ld_dE * size, 0, 0, (uint32_t)((cols * size + FILL_UNIT - 1) / FILL_UNIT), ld_dE == cols, vec, size};
+  Fill fill{reinterpret_cast<uint8_t*>(dE), cols * size, ld_dE * size, 0, 0, (uint32_t)((cols * size + FILL_UNIT - 1) / FILL_UNIT), ld_dE == cols};
   int64_t units = accumulate ? 0 : vocab * fill.per_row;
   if (fill.one_row) {
     fill.row_bytes = vocab * cols * size;
@@ -699,13 +704,14 @@ extern "C" fog_status fog_embed_grad(const void* tokens, int token_bytes, int64_
     merge_ranks_kernel<<<groups, kThreads, 0, s>>>(keys, count, tiles, ids, positions, tiles * MERGE_PARTS, fill);
   }
   const int groups = (int)((a.units + kThreads / 64 - 1) / (kThreads / 64));
-#define FOG_EG(F, V)                                                                            \
-  do {                                                                                          \
-    sum_runs_kernel<F, V><<<groups, kThreads, 0, s>>>(a);                                       \
-    if (a.chunks > 1) join_runs_kernel<F, V><<<(int)a.units, 64 * JOIN_WAVES, 0, s>>>(a);       \
+#define FOG_EG(F, R)                                                                         \
+  do {                                                                                       \
+    sum_runs_kernel<F, R><<<groups, kThreads, 0, s>>>(a);                                    \
+    if (a.chunks > 1) join_runs_kernel<F, R><<<(int)a.units, 64 * JOIN_WAVES, 0, s>>>(a);    \
   } while (0)
-  if (type == FOG_F32) { if (vec) FOG_EG(true, true); else FOG_EG(true, false); }
-  else                 { if (vec) FOG_EG(false, true); else FOG_EG(false, false); }
+  const bool ragged = cols % 8 != 0;
+  if (type == FOG_F32) { if (ragged) FOG_EG(true, true); else FOG_EG(true, false); }
+  else                 { if (ragged) FOG_EG(false, true); else FOG_EG(false, false); }
 #undef FOG_EG
   return fog_launch_status();
 }

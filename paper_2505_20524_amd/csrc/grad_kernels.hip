@@ -57,28 +57,24 @@ __global__ __launch_bounds__(kThreads) void sumsq_kernel(GradBatch b, double* __
     const int n = (int)(b.n[j] - at < PIECE ? b.n[j] - at : PIECE);
     const bool f32 = b.f32[j] != 0;
     const uint8_t* base = reinterpret_cast<const uint8_t*>(b.g[j]) + at * (f32 ? 4 : 2);
-    int done = 0;
-    if ((reinterpret_cast<uintptr_t>(base) & 15) == 0) {
-      const int per = f32 ? 4 : 8, vecs = n / per;
-      done = vecs * per;
-      for (int i = threadIdx.x; i < vecs; i += 4 * kThreads) {
-        uint4 v[4];
+    const int per = f32 ? 4 : 8, vecs = n / per, done = vecs * per;
+    for (int i = threadIdx.x; i < vecs; i += 4 * kThreads) {
+      uint4 v[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          v[u] = make_uint4(0, 0, 0, 0);
-          if (i + u * kThreads < vecs) v[u] = *reinterpret_cast<const uint4*>(base + 16 * (int64_t)(i + u * kThreads));
-        }
+      for (int u = 0; u < 4; ++u) {
+        v[u] = make_uint4(0, 0, 0, 0);
+        if (i + u * kThreads < vecs) v[u] = ld_any16(base + 16 * (int64_t)(i + u * kThreads));
+      }
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          if (f32) {
-            add_square(s0, __uint_as_float(v[u].x)); add_square(s1, __uint_as_float(v[u].y));
-            add_square(s0, __uint_as_float(v[u].z)); add_square(s1, __uint_as_float(v[u].w));
-          } else {
-            add_square(s0, bf16lo(v[u].x)); add_square(s1, bf16hi(v[u].x));
-            add_square(s0, bf16lo(v[u].y)); add_square(s1, bf16hi(v[u].y));
-            add_square(s0, bf16lo(v[u].z)); add_square(s1, bf16hi(v[u].z));
-            add_square(s0, bf16lo(v[u].w)); add_square(s1, bf16hi(v[u].w));
-          }
+      for (int u = 0; u < 4; ++u) {
+        if (f32) {
+          add_square(s0, __uint_as_float(v[u].x)); add_square(s1, __uint_as_float(v[u].y));
+          add_square(s0, __uint_as_float(v[u].z)); add_square(s1, __uint_as_float(v[u].w));
+        } else {
+          add_square(s0, bf16lo(v[u].x)); add_square(s1, bf16hi(v[u].x));
+          add_square(s0, bf16lo(v[u].y)); add_square(s1, bf16hi(v[u].y));
+          add_square(s0, bf16lo(v[u].z)); add_square(s1, bf16hi(v[u].z));
+          add_square(s0, bf16lo(v[u].w)); add_square(s1, bf16hi(v[u].w));
         }
       }
     }
@@ -129,29 +125,25 @@ __global__ __launch_bounds__(kThreads) void clip_kernel(GradBatch b, const doubl
     const uint8_t* src = reinterpret_cast<const uint8_t*>(b.g[j]) + at * (f32 ? 4 : 2);
     uint8_t* dst = reinterpret_cast<uint8_t*>(b.out[j]) + at * (f32 ? 4 : 2);
     if (src == dst && c == 1.0f) continue;       // nothing changes
-    int done = 0;
-    if (((reinterpret_cast<uintptr_t>(src) | reinterpret_cast<uintptr_t>(dst)) & 15) == 0) {
-      const int per = f32 ? 4 : 8, vecs = n / per;
-      done = vecs * per;
-      for (int i = threadIdx.x; i < vecs; i += 4 * kThreads) {
-        uint4 v[4];
+    const int per = f32 ? 4 : 8, vecs = n / per, done = vecs * per;
+    for (int i = threadIdx.x; i < vecs; i += 4 * kThreads) {
+      uint4 v[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-          if (i + u * kThreads < vecs) v[u] = ld_nt16(src + 16 * (int64_t)(i + u * kThreads));
+      for (int u = 0; u < 4; ++u)
+        if (i + u * kThreads < vecs) v[u] = ld_any_nt16(src + 16 * (int64_t)(i + u * kThreads));
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          if (i + u * kThreads >= vecs) break;
-          uint4 o = v[u];
-          if (c != 1.0f) {
-            if (f32)
-              o = make_uint4(__float_as_uint(__uint_as_float(o.x) * c), __float_as_uint(__uint_as_float(o.y) * c),
-                             __float_as_uint(__uint_as_float(o.z) * c), __float_as_uint(__uint_as_float(o.w) * c));
-            else
-              o = make_uint4(pack_bf16x2(bf16lo(o.x) * c, bf16hi(o.x) * c), pack_bf16x2(bf16lo(o.y) * c, bf16hi(o.y) * c),
-                             pack_bf16x2(bf16lo(o.z) * c, bf16hi(o.z) * c), pack_bf16x2(bf16lo(o.w) * c, bf16hi(o.w) * c));
-          }
-          st_nt16(dst + 16 * (int64_t)(i + u * kThreads), o);
+      for (int u = 0; u < 4; ++u) {
+        if (i + u * kThreads >= vecs) break;
+        uint4 o = v[u];
+        if (c != 1.0f) {
+          if (f32)
+            o = make_uint4(__float_as_uint(__uint_as_float(o.x) * c), __float_as_uint(__uint_as_float(o.y) * c),
+                           __float_as_uint(__uint_as_float(o.z) * c), __float_as_uint(__uint_as_float(o.w) * c));
+          else
+            o = make_uint4(pack_bf16x2(bf16lo(o.x) * c, bf16hi(o.x) * c), pack_bf16x2(bf16lo(o.y) * c, bf16hi(o.y) * c),
+                           pack_bf16x2(bf16lo(o.z) * c, bf16hi(o.z) * c), pack_bf16x2(bf16lo(o.w) * c, bf16hi(o.w) * c));
         }
+        st_any_nt16(dst + 16 * (int64_t)(i + u * kThreads), o);
       }
     }
     for (int i = done + threadIdx.x; i < n; i += kThreads) {
