@@ -140,4 +140,7 @@ def test_the_binding_refuses_tensors_that_the_call_would_misread():
         fog.make_grad_jobs([x.t()])
     with pytest.raises(ValueError):
         fog.grad_sumsq(fog.make_grad_jobs([x]), torch.zeros(1), s)
+    with pytest.raises(ValueError):
+        fog.fp8_gemm_block(fog.NT, 4, 4, 256, q, fog.E4M3, fog.VECTOR, s, q, fog.E4M3, fog.TILE, torch.zeros((1, 2), dtype=torch.uint8),
+                           torch.zeros((4, 4), dtype=torch.bfloat16), workspace=torch.zeros(1, dtype=torch.uint8).expand(1 << 20))
     assert ctypes.sizeof(fog.GradJob) == 32
