@@ -19,7 +19,8 @@ constexpr int OPERAND = 16 * STAGE_K;             // 4 KB of B; a quarter of tha
 constexpr int SCALE = 256;                        // a dword for each of 2 blocks x 16 rows, twice
 constexpr int RING = 2, WAVES = 4;
 template <int AP> constexpr int STAGE = OPERAND + 1024 * AP + 2 * SCALE;   // B, A, scales of A, scales of B
-template <int AP> constexpr int LDS_OF = WAVES * RING * STAGE<AP>;
+// the fragments of a group of 16 rows are read whole: behind the last stage lies room for the rows that A does not have
+template <int AP> constexpr int LDS_OF = WAVES * RING * STAGE<AP> + 1024 * ((AP + 3) / 4 * 4 - AP);
 
 // AP: pieces of four rows that A has.  Rows behind them are read from whatever lies there: they are rows of C that are not stored.
 template <int FA, int FB, int AP>
