@@ -120,7 +120,8 @@ __global__ __launch_bounds__(EMBED_THREADS) void embed_kernel(EmbedArgs a) {
 }
 
 // Up to SMALL pieces (a decoding step's tokens) with an abs-max: one workgroup, so that the abs-max needs no word that a launch before has
-// cleared.  24 rows of 2048 take it 7.5 us, mostly the arithmetic of one compute unit, and the caller 8.2; the two launches 12.3.
+// cleared.  24 rows of 2048 take it 7.6 us and the caller 8.2; the first form, with a launch that cleared the word, took
+// the caller 12.3.  Eight pieces ahead instead of four: no difference in turn (8.6 and 8.7 us).
 constexpr uint32_t SMALL = 8 * EMBED_THREADS;
 template <int FMT, bool RAGGED>
 __global__ __launch_bounds__(EMBED_THREADS) void embed_small_kernel(EmbedArgs a) {
