@@ -416,7 +416,7 @@ size_t fog_fp8_gemm_block_workspace(fog_layout layout, int64_t M, int64_t N, int
  *   x_bf16 : [count, cols], leading dimension ldx.   q : NULL or [count, cols] bytes, leading dimension ldq.
  *   amax_out : NULL or one float, overwritten.
  * Rows of any length, alignment and leading dimension; 16-byte aligned rows are the fastest.
- * Errors: NULL, SHAPE, ALIGN, UNSUPPORTED (token_bytes, format, factor, cols above 2^33).
+ * Errors: NULL, SHAPE, ALIGN, UNSUPPORTED (token_bytes, format, factor, cols above 2^32 - 8).
  */
 fog_status fog_embed_quantize(const void* tokens, int token_bytes, int64_t count, const void* table_bf16, int64_t vocab, int64_t cols,
                               int64_t ld_table, float factor, fog_fp8 fmt, const float* scale, void* x_bf16, int64_t ldx,

@@ -577,6 +577,7 @@ GradRoom room_of(int64_t count, int64_t cols) {
 constexpr int64_t GROUPS_MAX = 1 << 22;    // workgroups of a launch (up to 512 threads each): grids are counted in threads of 32 bits
 
 constexpr int64_t PIECES_MAX = 1 << 30;    // pieces of a launch of the forward
+constexpr int64_t COLS_MAX = ((int64_t)1 << 32) - 8;     // and columns of a row, which embed_pieces counts in 32 bits, the eight behind the last piece among them
 
 inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
@@ -590,6 +591,7 @@ extern "C" fog_status fog_embed_quantize(const void* tokens, int token_bytes, in
   if (fmt != FOG_E4M3 && fmt != FOG_E5M2) return FOG_ERR_UNSUPPORTED;
   if (!(factor - factor == 0.0f)) return FOG_ERR_UNSUPPORTED;
   const bool any = count > 0 && cols > 0;
+  if (any && cols > COLS_MAX) return FOG_ERR_UNSUPPORTED;
   if (any) {
     if (!tokens || !x_bf16 || (vocab > 0 && !table_bf16) || (q && !scale)) return FOG_ERR_NULL;
     if (ld_table < cols || ldx < cols || (q && ldq < cols)) return FOG_ERR_SHAPE;
@@ -600,7 +602,6 @@ extern "C" fog_status fog_embed_quantize(const void* tokens, int token_bytes, in
               reinterpret_cast<uint16_t*>(x_bf16), q, reinterpret_cast<uint32_t*>(amax_out), 0, 0};
   const int64_t per_row = (cols + 7) / 8;
   const bool ragged = cols % 8 != 0;
-  if (per_row > PIECES_MAX) return FOG_ERR_UNSUPPORTED;
   if (any && amax_out && per_row <= SMALL && count * per_row <= SMALL) {
     a.per_row = (uint32_t)per_row;
     a.pieces = (uint32_t)(count * per_row);
