@@ -429,8 +429,9 @@ fog_status fog_embed_quantize(const void* tokens, int token_bytes, int64_t count
  * Tokens outside 0 .. vocab - 1 contribute nothing.
  *   dx_bf16 : [count, cols], leading dimension ld_dx.   type : of dE, [vocab, cols] with leading dimension ld_dE.
  *   workspace : fog_embed_grad_workspace(count, vocab, cols) bytes, 16-byte aligned; contents on entry do not matter.  Calls that may
- *            overlap in time need a workspace each.
- * Limits: count and cols below 2^31, vocab up to 4194302, count * max(cols, 512) up to 2^37.  The tokens are sorted in tiles of 1024 that are
+ *            overlap in time need a workspace each.  (The query gives 0 for sizes that need none and for sizes beyond the limits.)
+ * Limits: count and cols below 2^31, vocab up to 4194302, ceil(count / 64) * ceil(cols / 512) up to 2^22; where dE is overwritten and its rows
+ * do not lie end to end (ld_dE != cols), vocab * ceil(bytes of a row / 4096) below 2^32.  The tokens are sorted in tiles of 1024 that are
  * merged by searching every tile for every token, which grows with count^2 / 1024: 20 us at 65536 tokens, 200 at 300000.
  * Errors: NULL, SHAPE, ALIGN, WORKSPACE, UNSUPPORTED (token_bytes, type, factor, limits).
  */

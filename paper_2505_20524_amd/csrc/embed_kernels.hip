@@ -576,6 +576,11 @@ GradRoom room_of(int64_t count, int64_t cols) {
 
 constexpr int64_t GROUPS_MAX = 1 << 22;    // workgroups of a launch (up to 512 threads each): grids are counted in threads of 32 bits
 
+// The sizes that a call takes.  The sums have to fit one launch: where they come near its limit a wave takes 64 tokens (see chunk_of).
+bool grad_takes(int64_t count, int64_t vocab, int64_t cols) {
+  return count <= 0x7FFFFFFF && vocab <= VOCAB_MAX && cols <= 0x7FFFFFFF && (count + 63) / 64 * ((cols + SLAB - 1) / SLAB) <= GROUPS_MAX;
+}
+
 constexpr int64_t PIECES_MAX = 1 << 30;    // pieces of a launch of the forward
 constexpr int64_t COLS_MAX = ((int64_t)1 << 32) - 8;     // and columns of a row, which embed_pieces counts in 32 bits, the eight behind the last piece among them
 
@@ -635,7 +640,7 @@ extern "C" fog_status fog_embed_quantize(const void* tokens, int token_bytes, in
 }
 
 extern "C" size_t fog_embed_grad_workspace(int64_t count, int64_t vocab, int64_t cols) {
-  if (count <= 0 || vocab <= 0 || cols <= 0 || count > 0x7FFFFFFF || vocab > VOCAB_MAX || cols > 0x7FFFFFFF) return 0;
+  if (count <= 0 || vocab <= 0 || cols <= 0 || !grad_takes(count, vocab, cols)) return 0;
   return room_of(count, cols).total;
 }
 
@@ -649,6 +654,8 @@ extern "C" fog_status fog_embed_grad(const void* tokens, int token_bytes, int64_
   if (count > 0x7FFFFFFF || vocab > VOCAB_MAX || cols > 0x7FFFFFFF) return FOG_ERR_UNSUPPORTED;
   if (vocab == 0 || cols == 0 || (count == 0 && accumulate)) return FOG_OK;
   const int size = type == FOG_F32 ? 4 : 2;
+  const int64_t row_units = (cols * size + FILL_UNIT - 1) / FILL_UNIT;
+  if (!grad_takes(count, vocab, cols) || (!accumulate && ld_dE != cols && vocab * row_units > 0xFFFFFFFFll)) return FOG_ERR_UNSUPPORTED;
   if (!dE || (count > 0 && (!tokens || !dx_bf16))) return FOG_ERR_NULL;
   if (ld_dE < cols || (count > 0 && ld_dx < cols)) return FOG_ERR_SHAPE;
   if (!aligned(dE, size) || (count > 0 && (!aligned(tokens, token_bytes) || !aligned(dx_bf16, 2)))) return FOG_ERR_ALIGN;
@@ -673,14 +680,11 @@ extern "C" fog_status fog_embed_grad(const void* tokens, int token_bytes, int64_
   a.slabs = (int)((cols + SLAB - 1) / SLAB);
   a.chunks = (count + a.chunk - 1) / a.chunk;
   a.units = a.chunks * a.slabs;
-  if (a.units > GROUPS_MAX) return FOG_ERR_UNSUPPORTED;
-  Fill fill{reinterpret_cast<uint8_t*>(dE), cols * size, ld_dE * size, 0, 0, (uint32_t)((cols * size + FILL_UNIT - 1) / FILL_UNIT), ld_dE == cols};
-  int64_t units = accumulate ? 0 : vocab * fill.per_row;
+  Fill fill{reinterpret_cast<uint8_t*>(dE), cols * size, ld_dE * size, 0, 0, (uint32_t)row_units, ld_dE == cols};
+  int64_t units = accumulate ? 0 : vocab * row_units;
   if (fill.one_row) {
     fill.row_bytes = vocab * cols * size;
     units = accumulate ? 0 : (fill.row_bytes + FILL_UNIT - 1) / FILL_UNIT;
-  } else if (units > 0xFFFFFFFFll) {
-    return FOG_ERR_UNSUPPORTED;
   }
   hipStream_t s = (hipStream_t)stream;
   const int wide = token_bytes == 8;
