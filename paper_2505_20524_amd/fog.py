@@ -282,8 +282,9 @@ def fp8_gemm_workspace(layout, M, N, K):
 BLOCK = 128                  # elements of a block scale
 
 
-# what a tensor may be that the calls read or write as codes and scale bytes, as bfloat16, as binary32
-_CODES = (torch.uint8, torch.float8_e4m3fn, torch.float8_e5m2, torch.int8)
+# what a tensor may be that the calls read or write as scale bytes, as codes of a format, as bfloat16, as binary32
+_BYTES = (torch.uint8, torch.int8)
+_CODES = {E4M3: _BYTES + (torch.float8_e4m3fn,), E5M2: _BYTES + (torch.float8_e5m2,)}
 _HALVES = (torch.bfloat16, torch.int16)
 _WORDS = (torch.float32,)
 
@@ -328,6 +329,10 @@ def _room(workspace):
     return workspace.numel() * workspace.element_size()
 
 
+def _codes(fmt):
+    return _CODES.get(fmt, _BYTES)       # the call itself refuses a format that is none
+
+
 def _blocks(n):
     return (n + BLOCK - 1) // BLOCK
 
@@ -337,14 +342,15 @@ def quantize_block(x, fmt, q_row=None, s_row=None, q_col=None, s_col=None, margi
     rows, cols = x.shape
     ldx = _matrix(x, "x", rows, cols, _HALVES)
     ld = [0, 0, 0, 0]
+    codes = _codes(fmt)
     if q_row is not None:
-        ld[0] = _matrix(q_row, "q_row", rows, cols, _CODES)
+        ld[0] = _matrix(q_row, "q_row", rows, cols, codes)
     if s_row is not None:
-        ld[1] = _matrix(s_row, "s_row", _blocks(cols), rows, _CODES)
+        ld[1] = _matrix(s_row, "s_row", _blocks(cols), rows, _BYTES)
     if q_col is not None:
-        ld[2] = _matrix(q_col, "q_col", rows, cols, _CODES)
+        ld[2] = _matrix(q_col, "q_col", rows, cols, codes)
     if s_col is not None:
-        ld[3] = _matrix(s_col, "s_col", _blocks(rows), cols, _CODES)
+        ld[3] = _matrix(s_col, "s_col", _blocks(rows), cols, _BYTES)
     _check(load().fog_quantize_block(_ptr(x), rows, cols, ldx, fmt, margin, _ptr(q_row), ld[0], _ptr(s_row), ld[1],
                                      _ptr(q_col), ld[2], _ptr(s_col), ld[3], _here(stream, x, q_row, s_row, q_col, s_col)), "fog_quantize_block")
 
@@ -352,17 +358,17 @@ def quantize_block(x, fmt, q_row=None, s_row=None, q_col=None, s_col=None, margi
 def quantize_tile(x, fmt, q, s, margin=0, stream=None):
     """The cast with a scale for each tile of 128 x 128."""
     rows, cols = x.shape
-    _check(load().fog_quantize_tile(_ptr(x), rows, cols, _matrix(x, "x", rows, cols, _HALVES), fmt, margin, _ptr(q), _matrix(q, "q", rows, cols, _CODES),
-                                    _ptr(s), _matrix(s, "s", _blocks(rows), _blocks(cols), _CODES), _here(stream, x, q, s)), "fog_quantize_tile")
+    _check(load().fog_quantize_tile(_ptr(x), rows, cols, _matrix(x, "x", rows, cols, _HALVES), fmt, margin, _ptr(q), _matrix(q, "q", rows, cols, _codes(fmt)),
+                                    _ptr(s), _matrix(s, "s", _blocks(rows), _blocks(cols), _BYTES), _here(stream, x, q, s)), "fog_quantize_tile")
 
 
 def fp8_gemm_block(layout, M, N, K, A, fmt_a, block_a, s_a, B, fmt_b, block_b, s_b, C, workspace=None, stream=None):
     """fp8_gemm on operands with a scale for each block of 128 contraction indices; block_a, block_b: VECTOR or TILE."""
     a_rows, a_cols = (K, M) if layout == TN else (M, K)
     b_rows, b_cols = (N, K) if layout == NT else (K, N)
-    lda, ldb = _matrix(A, "A", a_rows, a_cols, _CODES), _matrix(B, "B", b_rows, b_cols, _CODES)
-    lds_a = _matrix(s_a, "s_a", _blocks(a_rows), _blocks(a_cols), _CODES) if block_a == TILE else _matrix(s_a, "s_a", _blocks(K), M, _CODES)
-    lds_b = _matrix(s_b, "s_b", _blocks(b_rows), _blocks(b_cols), _CODES) if block_b == TILE else _matrix(s_b, "s_b", _blocks(K), N, _CODES)
+    lda, ldb = _matrix(A, "A", a_rows, a_cols, _codes(fmt_a)), _matrix(B, "B", b_rows, b_cols, _codes(fmt_b))
+    lds_a = _matrix(s_a, "s_a", _blocks(a_rows), _blocks(a_cols), _BYTES) if block_a == TILE else _matrix(s_a, "s_a", _blocks(K), M, _BYTES)
+    lds_b = _matrix(s_b, "s_b", _blocks(b_rows), _blocks(b_cols), _BYTES) if block_b == TILE else _matrix(s_b, "s_b", _blocks(K), N, _BYTES)
     _check(load().fog_fp8_gemm_block(layout, M, N, K, _ptr(A), fmt_a, lda, block_a, _ptr(s_a), lds_a, _ptr(B), fmt_b, ldb, block_b, _ptr(s_b), lds_b,
                                      _ptr(C), _matrix(C, "C", M, N, _HALVES), _ptr(workspace), _room(workspace), _here(stream, A, s_a, B, s_b, C, workspace)), "fog_fp8_gemm_block")
 
@@ -385,7 +391,7 @@ def embed_quantize(tokens, table, factor, fmt, scale_t, x, q=None, amax_out=None
     _floats(scale_t, "scale_t")
     _floats(amax_out, "amax_out")
     _check(load().fog_embed_quantize(ids, size, count, _ptr(table), vocab, cols, _matrix(table, "table", vocab, cols, _HALVES), factor, fmt, _ptr(scale_t),
-                                     _ptr(x), _matrix(x, "x", count, cols, _HALVES), _ptr(q), _matrix(q, "q", count, cols, _CODES) if q is not None else 0,
+                                     _ptr(x), _matrix(x, "x", count, cols, _HALVES), _ptr(q), _matrix(q, "q", count, cols, _codes(fmt)) if q is not None else 0,
                                      _ptr(amax_out), _here(stream, tokens, table, scale_t, x, q, amax_out)), "fog_embed_quantize")
 
 
