@@ -11,7 +11,10 @@
 // whenever the gradients are, and a sum of 10^9 terms keeps all the places that a binary32 norm has.  The additions cost no time
 // beside the reads.  Every workgroup leaves its sum in its own word and one workgroup adds the words in order: no atomics,
 // the same result on every run.
+#include <algorithm>
 #include <cfloat>
+#include <memory>
+#include <new>
 
 #include "common.h"
 #include "launch.h"
@@ -174,6 +177,37 @@ fog_status check_jobs(const fog_grad_job* jobs, int count, bool with_out) {
   return FOG_OK;
 }
 
+// Whether a result lies where another result, or a gradient that is not its own, lies: the pieces of a call are worked on in no order, and a
+// gradient that is listed twice would be clipped once, twice or in parts.  (49 gradients with results elsewhere: 0.9 us of host time.)
+fog_status check_overlaps(const fog_grad_job* jobs, int count) {
+  struct Span { uintptr_t begin, end; bool written; };
+  constexpr int FEW = 256;
+  Span few[FEW];
+  std::unique_ptr<Span[]> many;
+  Span* spans = few;
+  if (2 * (int64_t)count > FEW) {
+    many.reset(new (std::nothrow) Span[2 * (size_t)count]);
+    spans = many.get();
+    if (!spans) return FOG_ERR_UNSUPPORTED;
+  }
+  int64_t n = 0;
+  for (int i = 0; i < count; ++i) {
+    const fog_grad_job& j = jobs[i];
+    if (j.n == 0) continue;
+    const uintptr_t g = reinterpret_cast<uintptr_t>(j.g), out = reinterpret_cast<uintptr_t>(j.out), bytes = (uintptr_t)j.n * (j.type == FOG_F32 ? 4 : 2);
+    spans[n++] = {out, out + bytes, true};
+    if (g != out) spans[n++] = {g, g + bytes, false};
+  }
+  std::sort(spans, spans + n, [](const Span& a, const Span& b) { return a.begin < b.begin; });
+  uintptr_t end = 0, written_end = 0;      // of what begins before
+  for (int64_t i = 0; i < n; ++i) {
+    if (spans[i].begin < (spans[i].written ? end : written_end)) return FOG_ERR_UNSUPPORTED;
+    end = std::max(end, spans[i].end);
+    if (spans[i].written) written_end = std::max(written_end, spans[i].end);
+  }
+  return FOG_OK;
+}
+
 // The batches of a call, one after the other: take(batch) for each.
 template <typename F>
 void for_batches(const fog_grad_job* jobs, int count, F take) {
@@ -232,6 +266,8 @@ extern "C" fog_status fog_grad_clip(const fog_grad_job* jobs, int count, const d
   if (!sumsq) return FOG_ERR_NULL;
   if (reinterpret_cast<uintptr_t>(sumsq) & 7) return FOG_ERR_ALIGN;
   if (!(max_norm >= 0.0f)) return FOG_ERR_UNSUPPORTED;
+  const fog_status apart = check_overlaps(jobs, count);
+  if (apart != FOG_OK) return apart;
   hipStream_t s = (hipStream_t)stream;
   bool told = false;
   for_batches(jobs, count, [&](const GradBatch& b) {
