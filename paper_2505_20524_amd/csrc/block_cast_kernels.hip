@@ -8,9 +8,10 @@
 // a thread): the maxima along rows are a reduction over 16 lanes, those along columns one over a thread's rows, the wave's four lanes
 // of a column group and, through LDS, the waves.  Both forms of codes then come from the same registers: a tensor that a step
 // multiplies along its rows and along its columns is read once for the two casts.  Bound by memory: 2 bytes read and 1 written (2 for
-// both forms) per element.  us (at 4.8 TB/s, the rate of a large copy): 8192 x 14336 rows 60 (73), both 85 (98), tiles 60 (73);
-// 1777 x 2064 rows 6.1 (2.3), both 7.7 (3.1).  Workgroups of 256 and of 1024 threads: 8192 x 14336 both 88 and 89, 1777 x 2064 both 8.5 and
-// 7.6, 24 x 4096 rows 3.7 and 3.0 where these take 3.1.
+// both forms) per element.  us, launches from a graph (at the rates of a large read and a large fill, 6.99 and 6.86 TB/s): 8192 x 14336 rows 52
+// (51), both 88 (68), tiles 53 (51); 1777 x 2064 rows 5.5 (1.6), both 6.8 (2.1).  Workgroups of 256 and of 1024 threads: 8192 x 14336 rows 55
+// and 60, both 90 and 90, 1777 x 2064 both 7.8 and 6.7, 24 x 4096 rows 3.7 and 2.9 where these take 3.1.
+// Rows that begin at any byte: 4096 x 4096 rows 16 us instead of 12, 8192 x 14336 rows 83 and both 184.
 #include "common.h"
 #include "launch.h"
 

@@ -109,8 +109,10 @@ FOG_DEVICE uint32_t group_amax(uint32_t m) {
 }
 
 // With an abs-max one workgroup a compute unit, which ends with one atomic at most: an atomic of each wave of 1112 rows of 3568, all at the
-// same time, took 30 us where the rows take 8.  Rows and codes are written through, for the cast or the product that reads them next:
-// 8192 x 4096 with codes 26 us (floor at 4.8 TB/s, every row from memory: 35); followed by the block cast 44 us, and 47 with stores past the caches.
+// same time, took 30 us where the rows take 8.  Rows and codes are written through, for the cast or the product that reads them next.  8192 x 4096
+// of 131072 with codes, other ids and results each time (at the rates of a large read and a large fill, 6.99 and 6.86 TB/s: 24): 30 to 34 us by the
+// profiler; from a graph, with the launch that clears the abs-max, 36 with ids as frequent as words and 39 with ids drawn evenly, 35 there
+// with stores past the caches; but rows without codes and the block cast both ways behind them 48, and 52 with such stores.
 template <int FMT, bool RAGGED>
 __global__ __launch_bounds__(EMBED_THREADS) void embed_kernel(EmbedArgs a) {
   const uint32_t m = embed_pieces<FMT, RAGGED>(a, blockIdx.x * EMBED_THREADS + threadIdx.x, gridDim.x * EMBED_THREADS);

@@ -8,8 +8,8 @@
 // are turned by the row's number on the way, so that the fragment reads touch every bank once.
 // The matrix instruction (16 x 16 x 128) takes one scale block: a lane's 32 bytes are a quarter of its row's block, its scale register
 // holds that row's byte.  B is the first operand: a lane ends up with four consecutive columns of a row of C.
-// us, weights that no call has just read (floor at 4.8 TB/s): one row of 4096 x 4096 6.0 (3.5), of 14336 x 4096 13.1 (12.2), of
-// 4096 x 14336 13.4 (12.2); 24 rows of 4096 x 4096 7.6 (3.5).  Eight waves a workgroup: 6.8, 18.2, 13.4; three stages: 6.3, 14.4, 13.5.
+// us, weights that no call has just read (at the rate of a large read, 6.99 TB/s): one row of 4096 x 4096 6.1 (2.4), of 14336 x 4096 13.4 (8.4), of
+// 4096 x 14336 13.2 (8.4); 24 rows of 4096 x 4096 7.6 (2.4).  Eight waves a workgroup: 6.8, 18.2, 13.4; three stages: 6.3, 14.4, 13.5.
 #include "gemm_common.h"
 
 namespace {
@@ -158,11 +158,19 @@ fog_status launch_rows(const GemmArgs& g, hipStream_t s) {
 
 }  // namespace
 
-// Every workgroup reads all of A, so that with more rows, or more workgroups than the chip holds two of on a compute unit (45 to 75 KB of
-// LDS each up to 16 rows; one above), the tiles of fog_fp8_gemm do as well.  us, this kernel and the tiles:
+// Every workgroup reads all of A, so that with more rows, or more workgroups than the chip holds at a time (47 to 68 KiB of LDS each up to 16
+// rows, three or two on a compute unit; 79 to 100 above, two up to 20 rows and one from there), the tiles of fog_fp8_gemm do as well.  us,
+// this kernel and the tiles:
 //   8 rows   8192 x 512 4.2, 4.4   14336 x 512 6.3, 4.8   14336 x 2048 9.5, 9.4   14336 x 4096 14.3, 16.5   8192 x 8192 14.2, 22.3
 //   16 rows  8192 x 512 4.6, 4.3   14336 x 2048 11.9, 9.6   14336 x 4096 16.9, 16.6   14336 x 14336 46.5, 41.4   4096 x 4096 7.1, 11.8
 //   32 rows  2048 x 512 3.8, 3.9   4096 x 1024 4.9, 5.2   4096 x 4096 8.2, 12.0   8192 x 1024 7.4, 5.3   8192 x 4096 13.9, 13.6
+// Weights so narrow that N / 16 workgroups leave compute units idle: this kernel, the tiles with their contraction split (which takes a
+// workspace) and whole:
+//   4 rows   256 x 1024 3.0, 4.6, 4.6   256 x 4096 3.8, 8.4, 8.5   256 x 14336 6.9, 9.5, 20.7   1024 x 4096 4.2, 8.7, 8.7   2048 x 14336 11, 13.9, 31.0
+//   16 rows  1024 x 4096 4.7, 8.7, 8.7   1024 x 14336 11.5, 11.6, 30.9   2048 x 1024 4.0, 5.2, 5.2   2048 x 14336 13, 13.7, 31.5
+//   32 rows  256 x 1024 3.9, 4.7, 4.7   1024 x 4096 5.9, 8.8, 8.8   256 x 14336 10.3, 9.8, 21.1   1024 x 14336 14.7, 11.5, 31.8   2048 x 14336 16.0, 14.0, 32.3
+// (a wave walks its quarter of the contraction through two stages: latency).  The split tiles gain 1 to 3 us from 24 rows of the longest
+// contraction on, for callers that bring the room; without it the tiles lose twice.
 bool gemm_rows_takes(int64_t M, int64_t N, int64_t K, int cus) {
   if (M <= 16) return N <= 32 * (int64_t)cus || (M <= 8 && K >= 4096);
   return M <= 32 && N <= 16 * (int64_t)cus && K >= 1024;
