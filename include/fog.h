@@ -455,14 +455,15 @@ size_t fog_embed_grad_workspace(int64_t count, int64_t vocab, int64_t cols);
  *     out = g * c,   c = fl32(max_norm / norm) where norm is finite and above max_norm, 1 otherwise.
  * Two calls, so that a job over several GPUs can add up the ranks' sums in between (one 8-byte all-reduce).  c is a binary32 number: below
  * 2^-126 it loses places.  A norm that is not finite leaves the gradients as they are and shows in `norm`: skip that step.
- *   jobs  : HOST array of `count` descriptions, read before the call returns; any number of tensors, 120 to a launch.
+ *   jobs  : HOST array of `count` descriptions, read before the call returns; up to 2^24 tensors, 120 to a launch.
  *   g, out : n contiguous elements of `type`, aligned to their size; out may be g (nothing is written then where c is 1) and must not
  *            overlap it otherwise, nor any other gradient or result (one that is listed twice would be clipped twice); fog_grad_sumsq
  *            does not look at it.
  *   sumsq : one double, overwritten by fog_grad_sumsq, 8-byte aligned.   norm : NULL or one float, overwritten
  *            (with FLT_MAX for a finite norm beyond it).
- *   workspace : fog_grad_sumsq_workspace(count) bytes, 8-byte aligned; contents on entry do not matter.
- * Errors: NULL, SHAPE (count, n), ALIGN, WORKSPACE, UNSUPPORTED (type, n above 2^37, max_norm negative or NaN, results that overlap).
+ *   workspace : fog_grad_sumsq_workspace(count) bytes, 8-byte aligned; contents on entry do not matter.  Calls that may overlap in time need a
+ *            workspace each.
+ * Errors: NULL, SHAPE (count, n), ALIGN, WORKSPACE, UNSUPPORTED (type, count above 2^24, n above 2^37, max_norm negative or NaN, results that overlap).
  */
 typedef struct {
   const void* g;

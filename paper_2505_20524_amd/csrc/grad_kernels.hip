@@ -25,6 +25,7 @@ constexpr int kThreads = 256;
 constexpr int BATCH = 120;               // descriptions that fit a launch's arguments
 constexpr int64_t PIECE = 8192;          // elements: 4 loads of 16 bytes a thread in bf16
 constexpr int SUM_GROUPS = 4096;         // most workgroups of a launch that sums: one word of the workspace each
+constexpr int TENSORS_MAX = 1 << 24;     // tensors of a call: their sums, SUM_GROUPS for each BATCH, are counted in 32 bits
 constexpr int CLIP_GROUPS = 1 << 23;     // most workgroups of a launch that clips: grids are counted in threads of 32 bits
 
 struct GradBatch {
@@ -163,6 +164,7 @@ __global__ __launch_bounds__(kThreads) void clip_kernel(GradBatch b, const doubl
 
 fog_status check_jobs(const fog_grad_job* jobs, int count, bool with_out) {
   if (count < 0) return FOG_ERR_SHAPE;
+  if (count > TENSORS_MAX) return FOG_ERR_UNSUPPORTED;
   if (count > 0 && !jobs) return FOG_ERR_NULL;
   for (int i = 0; i < count; ++i) {
     const fog_grad_job& j = jobs[i];
@@ -238,7 +240,7 @@ void for_batches(const fog_grad_job* jobs, int count, F take) {
 }  // namespace
 
 extern "C" size_t fog_grad_sumsq_workspace(int count) {
-  return count <= 0 ? 0 : (size_t)((count + BATCH - 1) / BATCH) * SUM_GROUPS * sizeof(double);
+  return count <= 0 || count > TENSORS_MAX ? 0 : (size_t)((count + BATCH - 1) / BATCH) * SUM_GROUPS * sizeof(double);
 }
 
 extern "C" fog_status fog_grad_sumsq(const fog_grad_job* jobs, int count, double* sumsq, void* workspace, size_t workspace_bytes, void* stream) {

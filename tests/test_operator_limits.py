@@ -49,3 +49,13 @@ def test_rows_of_a_strided_gradient_that_is_overwritten(lib, vocab, cols, type, 
 
 def test_a_table_without_rows_has_no_limit(lib):
     assert embed_grad(lib, 1 << 30, 0, 1 << 20) == OK
+
+
+def test_number_of_gradients(lib):
+    """What a call sums is counted in 32 bits: up to 2^24 tensors, 4096 sums for each 120 of them."""
+    most = 1 << 24
+    for count, inside in ((most, True), (most + 1, False), ((1 << 31) - 1, False)):
+        # nothing of the jobs is looked at before their number
+        assert lib.fog_grad_sumsq(None, count, P, None, 0, None) == (NULL if inside else UNSUPPORTED)
+        assert lib.fog_grad_clip(None, count, P, 1.0, None, None) == (NULL if inside else UNSUPPORTED)
+        assert lib.fog_grad_sumsq_workspace(count) == (-(-count // 120) * 4096 * 8 if inside else 0)
