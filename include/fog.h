@@ -476,6 +476,47 @@ size_t fog_grad_sumsq_workspace(int count);
 fog_status fog_grad_clip(const fog_grad_job* jobs, int count, const double* sumsq, float max_norm, float* norm, void* stream);
 
 /*
+ * The AdamW step (decoupled weight decay) over many tensors:
+ *     gc = g c,   m = beta1 m + (1 - beta1) gc,   v = beta2 v + (1 - beta2) gc gc,
+ *     p  = p (1 - lr weight_decay) - m rate / (sqrt(v) root + eps),     rate = lr / (1 - beta1^t),  root = 1 / sqrt(1 - beta2^t),
+ * binary32, every operation rounded once, products of three from the left (m and v are the same bits in any evaluation that does so).
+ *   c : without sumsq 1; else the factor of fog_grad_clip for *sumsq and max_norm, so that the gradients need not be clipped before.  A sum
+ *       that is not finite leaves the whole step out: nothing is written.
+ *   states : FOG_STATES_F32  m, v are n floats each.
+ *            FOG_STATES_FP8  m is n E4M3 codes, v n E5M2 codes, with a scale byte for each 128 consecutive elements as in fog_quantize_block
+ *            (value = code 2^(byte - 127)) in m_scale and v_scale, ceil(n / 128) each.  Both are rounded to one of the two codes beside them by a
+ *            hash of seed, step, the tensor's place in `jobs` and the element's in the tensor, so that the expected value is kept (to the nearest
+ *            code, a second moment would not move: a step changes it by less than half a code's step); a v above zero keeps a code above
+ *            zero.  Rounding adds noise to the moments, about 0.075 / sqrt(1 - beta2^2) of v (a quarter at 0.95, a half at 0.99) and half
+ *            as much with beta1 of m, which is why betas above 0.99 are refused.  A moment that is not finite spoils its block of 128.
+ *            All states zero (codes and bytes) before the first step.
+ *   p : n of p_type, updated in place.  master : NULL, or n floats (bf16 p only): the step is then made on them and p is their rounding.  A bf16 p
+ *            without a master copy is rounded as the FP8 states are, by sixteen bits of the hash.
+ *   g : n of g_type, read only.   weight_decay : this tensor's.
+ *   lr, step : the rate and the number t = 1, 2, ... of the step; lr_dev (one float) and step_dev (one int64, below 1 counts as 1) take their place
+ *            where they are given, for steps that are captured once and replayed.  seed : any; the step's number enters the hash too.
+ * Tensors of any alignment above their elements'; up to 2^24 of them, 50 to a launch.  The buffers that the call writes must not overlap each other or a
+ * gradient.
+ * Errors: NULL, SHAPE (count, n, step), ALIGN, UNSUPPORTED (types, states, n above 2^37, a beta outside 0 .. 1 (0.99), eps below the smallest
+ * normal number, values that are not finite, max_norm negative, a master copy of binary32 p, buffers that overlap).
+ */
+typedef enum { FOG_STATES_F32 = 0, FOG_STATES_FP8 = 1 } fog_states;
+typedef struct {
+  void* p;
+  const void* g;
+  float* master;       /* may be NULL */
+  void* m;
+  void* v;
+  uint8_t* m_scale;    /* FP8 states only */
+  uint8_t* v_scale;
+  int64_t n;
+  fog_real p_type, g_type;
+  float weight_decay;
+} fog_adamw_job;
+fog_status fog_adamw(const fog_adamw_job* jobs, int count, fog_states states, double lr, const float* lr_dev, double beta1, double beta2,
+                     double eps, int64_t step, const int64_t* step_dev, uint64_t seed, const double* sumsq, float max_norm, void* stream);
+
+/*
  * FP8 dot-product attention forward (Appendix B, eq. P; Appendix E, FP8DPA row):
  *     O = Softmax(s Q K^T + M) V   per (batch, head), M the causal mask when causal != 0,
  * with Q~, K~, V~ in E4M3 and the probabilities cast to E4M3 for the P V product.

@@ -11,13 +11,11 @@
 // whenever the gradients are, and a sum of 10^9 terms keeps all the places that a binary32 norm has.  The additions cost no time
 // beside the reads.  Every workgroup leaves its sum in its own word and one workgroup adds the words in order: no atomics,
 // the same result on every run.
-#include <algorithm>
 #include <cfloat>
-#include <memory>
-#include <new>
 
 #include "common.h"
 #include "launch.h"
+#include "spans.h"
 
 namespace {
 
@@ -182,32 +180,15 @@ fog_status check_jobs(const fog_grad_job* jobs, int count, bool with_out) {
 // Whether a result lies where another result, or a gradient that is not its own, lies: the pieces of a call are worked on in no order, and a
 // gradient that is listed twice would be clipped once, twice or in parts.  (49 gradients with results elsewhere: 0.9 us of host time.)
 fog_status check_overlaps(const fog_grad_job* jobs, int count) {
-  struct Span { uintptr_t begin, end; bool written; };
-  constexpr int FEW = 256;
-  Span few[FEW];
-  std::unique_ptr<Span[]> many;
-  Span* spans = few;
-  if (2 * (int64_t)count > FEW) {
-    many.reset(new (std::nothrow) Span[2 * (size_t)count]);
-    spans = many.get();
-    if (!spans) return FOG_ERR_UNSUPPORTED;
-  }
-  int64_t n = 0;
+  FogSpans<256> spans(2 * (int64_t)count);
+  if (!spans.ok()) return FOG_ERR_UNSUPPORTED;
   for (int i = 0; i < count; ++i) {
     const fog_grad_job& j = jobs[i];
-    if (j.n == 0) continue;
-    const uintptr_t g = reinterpret_cast<uintptr_t>(j.g), out = reinterpret_cast<uintptr_t>(j.out), bytes = (uintptr_t)j.n * (j.type == FOG_F32 ? 4 : 2);
-    spans[n++] = {out, out + bytes, true};
-    if (g != out) spans[n++] = {g, g + bytes, false};
+    const int64_t bytes = j.n * (j.type == FOG_F32 ? 4 : 2);
+    spans.add(j.out, bytes, true);
+    if (j.g != j.out) spans.add(j.g, bytes, false);
   }
-  std::sort(spans, spans + n, [](const Span& a, const Span& b) { return a.begin < b.begin; });
-  uintptr_t end = 0, written_end = 0;      // of what begins before
-  for (int64_t i = 0; i < n; ++i) {
-    if (spans[i].begin < (spans[i].written ? end : written_end)) return FOG_ERR_UNSUPPORTED;
-    end = std::max(end, spans[i].end);
-    if (spans[i].written) written_end = std::max(written_end, spans[i].end);
-  }
-  return FOG_OK;
+  return spans.apart() ? FOG_OK : FOG_ERR_UNSUPPORTED;
 }
 
 // The batches of a call, one after the other: take(batch) for each.

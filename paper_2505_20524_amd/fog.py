@@ -13,6 +13,7 @@ E4M3, E5M2 = 0, 1
 NT, NN, TN = 0, 1, 2
 VECTOR, TILE = 0, 1          # fog_block: how an operand's block scales lie
 BF16, F32 = 0, 1             # fog_real
+STATES_F32, STATES_FP8 = 0, 1    # fog_states
 CAST_BATCH_MAX = 32          # FOG_CAST_BATCH_MAX of the header
 
 _LIB = None
@@ -20,7 +21,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libfog.so")
 
 _c = ctypes
-_P, _I64, _I, _F, _SZ = _c.c_void_p, _c.c_int64, _c.c_int, _c.c_float, _c.c_size_t
+_P, _I64, _I, _F, _D, _SZ = _c.c_void_p, _c.c_int64, _c.c_int, _c.c_float, _c.c_double, _c.c_size_t
 
 SIGNATURES = {
     "fog_status_string": (_c.c_char_p, [_I]),
@@ -55,6 +56,7 @@ SIGNATURES = {
     "fog_grad_sumsq": (_I, [_P, _I, _P, _P, _SZ, _P]),
     "fog_grad_sumsq_workspace": (_SZ, [_I]),
     "fog_grad_clip": (_I, [_P, _I, _P, _F, _P, _P]),
+    "fog_adamw": (_I, [_P, _I, _I, _D, _P, _D, _D, _D, _I64, _P, _c.c_uint64, _P, _F, _P]),
     "fog_fp8_attn_fwd": (_I, [_I, _I, _I, _I, _I, _F, _I, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P]),
     "fog_fp8_attn_bwd": (_I, [_I, _I, _I, _I, _I, _F, _I, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P,
                               _P, _P, _P, _P, _P, _SZ, _P]),
@@ -454,6 +456,54 @@ def grad_clip(jobs, sumsq, max_norm, norm=None, stream=None):
     _floats(norm, "norm")
     _jobs_here(jobs)
     _check(load().fog_grad_clip(jobs, len(jobs), _ptr(sumsq), max_norm, _ptr(norm), _here(stream, sumsq, norm)), "fog_grad_clip")
+
+
+class AdamwJob(ctypes.Structure):
+    """Mirror of fog_adamw_job."""
+    _fields_ = [("p", _P), ("g", _P), ("master", _P), ("m", _P), ("v", _P), ("m_scale", _P), ("v_scale", _P), ("n", _I64), ("p_type", _I), ("g_type", _I),
+                ("weight_decay", _F)]
+
+
+def make_adamw_jobs(items):
+    """items: dicts of a parameter's contiguous tensors p, g, m, v, where it has them master, m_scale and v_scale, and its weight_decay (0 if
+    missing) -> ctypes array for adamw (built once, reused while the tensors stay in place).  Moments in float32, or codes with scale bytes."""
+    arr = (AdamwJob * len(items))()
+    arr.tensors, arr.states = [], None          # the array keeps them alive
+    for job, item in zip(arr, items):
+        t = {k: item.get(k) for k in ("p", "g", "master", "m", "v", "m_scale", "v_scale")}
+        if t["p"] is None or t["m"] is None:
+            raise ValueError("a parameter p and its states m and v are needed")
+        n, states = t["p"].numel(), STATES_F32 if t["m"].dtype == torch.float32 else STATES_FP8
+        fp8, blocks = states == STATES_FP8, _blocks(n)
+        want = {"p": (_WORDS + _HALVES, n), "g": (_WORDS + _HALVES, n), "master": (_WORDS, n), "m": (_codes(E4M3) if fp8 else _WORDS, n),
+                "v": (_codes(E5M2) if fp8 else _WORDS, n), "m_scale": (_BYTES, blocks), "v_scale": (_BYTES, blocks)}
+        for k, (types, size) in want.items():
+            if t[k] is None and (k == "master" or (k in ("m_scale", "v_scale") and not fp8)):
+                continue
+            if t[k] is None or not t[k].is_contiguous() or t[k].dtype not in types or t[k].numel() != size:
+                raise ValueError("%s: a contiguous tensor of %d elements of one of %s is needed" % (k, size, types))
+        if arr.states not in (None, states):
+            raise ValueError("states of one kind are needed for all tensors of a call")
+        arr.states = states
+        job.p, job.g, job.master, job.m, job.v = _ptr(t["p"]), _ptr(t["g"]), _ptr(t["master"]), _ptr(t["m"]), _ptr(t["v"])
+        job.m_scale, job.v_scale, job.n = _ptr(t["m_scale"]) if fp8 else None, _ptr(t["v_scale"]) if fp8 else None, n
+        job.p_type, job.g_type = (F32 if t[k].dtype == torch.float32 else BF16 for k in ("p", "g"))
+        job.weight_decay = item.get("weight_decay", 0.0)
+        arr.tensors += [x for x in t.values() if x is not None]
+    arr.devices = {t.get_device() for t in arr.tensors}
+    return arr
+
+
+def adamw(jobs, lr, step, beta1=0.9, beta2=0.95, eps=1e-8, seed=0, sumsq=None, max_norm=1.0, stream=None):
+    """One AdamW step.  lr, step: numbers, or one float32 and one int64 in device memory (for a step that is captured and replayed); sumsq: the sum of
+    squares from grad_sumsq, by which the gradients are clipped to max_norm on their way, None for no clipping."""
+    lr_dev, step_dev = (t if isinstance(t, torch.Tensor) else None for t in (lr, step))
+    _floats(sumsq, "sumsq", torch.float64)
+    _floats(lr_dev, "lr")
+    _floats(step_dev, "step", torch.int64)
+    _jobs_here(jobs)
+    _check(load().fog_adamw(jobs, len(jobs), jobs.states or 0, 0.0 if lr_dev is not None else lr, _ptr(lr_dev), beta1, beta2, eps,
+                            0 if step_dev is not None else step, _ptr(step_dev), seed, _ptr(sumsq), max_norm, _here(stream, lr_dev, step_dev, sumsq)), "fog_adamw")
 
 
 def fp8_attn_fwd(B, H, S, D, softmax_scale, causal, Q, K, V, sinv_q, sinv_k, sinv_v, scale_p, O, lse,

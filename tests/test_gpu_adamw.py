@@ -1,0 +1,342 @@
+"""GPU parity: the AdamW step.  Moments and FP8 states bit for bit against the oracle, parameters against float64."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import adamw, fp8
+from paper_2505_20524_amd import fog
+
+pytestmark = pytest.mark.gpu
+
+B, F = torch.bfloat16, torch.float32
+EPS32 = 2.0 ** -24
+
+
+def host(t):
+    """float64 of a tensor's values, bytes as they are."""
+    return t.cpu().numpy() if t.dtype == torch.uint8 else t.double().cpu().numpy()
+
+
+def bits(t):
+    return t.cpu().contiguous().view(torch.uint8)
+
+
+class Tensor:
+    """A parameter with its gradient and states after some steps; `skew` moves every buffer off its alignment by so many elements."""
+
+    def __init__(self, gen, n, states, p=B, g=B, master=True, decay=0.1, skew=0, zero=False):
+        self.n, self.fp8, self.decay = n, states == fog.STATES_FP8, decay
+
+        def room(size, dtype):
+            return torch.full((size + skew + 16,), 77, dtype=dtype, device="cuda")[skew:skew + size]
+        normal = lambda std: torch.randn(n, device="cuda", generator=gen) * std  # noqa: E731
+        w = normal(0.02)
+        self.p, self.g = room(n, p), room(n, g)
+        self.p.copy_(w)
+        self.g.copy_(normal(1e-2))
+        self.master = room(n, F) if master and p == B else None
+        if self.master is not None:
+            self.master.copy_(w)
+        m, v = normal(1e-3), normal(1e-3) ** 2
+        if zero:
+            m, v = m * 0, v * 0
+        self.m_scale = self.v_scale = None
+        if self.fp8:
+            self.m, self.v = room(n, torch.uint8), room(n, torch.uint8)
+            self.m_scale, self.v_scale = room(-(-n // 128), torch.uint8), room(-(-n // 128), torch.uint8)
+            if zero:
+                qm, sm = np.zeros(n, np.uint8), np.zeros(-(-n // 128), np.uint8)
+                qv, sv = qm, sm
+            else:
+                qm, sm = adamw.encode(m.cpu().numpy(), np.zeros(n, np.int64), fp8.E4M3)
+                qv, sv = adamw.encode(v.cpu().numpy(), np.zeros(n, np.int64), fp8.E5M2)
+            for t, a in ((self.m, qm), (self.m_scale, sm), (self.v, qv), (self.v_scale, sv)):
+                t.copy_(torch.from_numpy(a))
+        else:
+            self.m, self.v = room(n, F), room(n, F)
+            self.m.copy_(m)
+            self.v.copy_(v)
+
+    def item(self):
+        return dict(p=self.p, g=self.g, m=self.m, v=self.v, master=self.master, m_scale=self.m_scale, v_scale=self.v_scale, weight_decay=self.decay)
+
+    def written(self):
+        return {k: t for k, t in self.item().items() if k != "g" and isinstance(t, torch.Tensor)}
+
+    def values(self):
+        """p, g, m, v as the step reads them."""
+        m, v = (host(self.m), host(self.v)) if not self.fp8 else (adamw.decode(host(self.m), host(self.m_scale), fp8.E4M3),
+                                                                 adamw.decode(host(self.v), host(self.v_scale), fp8.E5M2))
+        return host(self.master if self.master is not None else self.p), host(self.g), m, v
+
+
+def check(tensors, lr=1e-2, t=7, beta1=0.9, beta2=0.95, eps=1e-8, seed=0x123456789ABC, clip=None, **call):
+    """One step on all of them against the oracle."""
+    before = [x.values() for x in tensors]
+    grads = [x.g.clone() for x in tensors]
+    c, more = np.float32(1), {}
+    if clip is not None:
+        sumsq = torch.full((1,), math.fsum(float((g ** 2).sum()) for _, g, _, _ in before), dtype=torch.float64, device="cuda")
+        c, more = adamw.clip_factor(sumsq.item(), clip), dict(sumsq=sumsq, max_norm=clip)
+    jobs = fog.make_adamw_jobs([x.item() for x in tensors])
+    fog.adamw(jobs, call.get("lr", lr), call.get("step", t), beta1=beta1, beta2=beta2, eps=eps, seed=seed, **more)
+    torch.cuda.synchronize()
+    for i, (x, (p, g, m, v), g0) in enumerate(zip(tensors, before, grads)):
+        assert torch.equal(bits(x.g), bits(g0))
+        m, v = adamw.moments(m, v, g, c, beta1, beta2)
+        want, u = adamw.update(p, m, v, lr, beta1, beta2, eps, x.decay, t)
+        # p keep: 1 + 1 roundings.  The quotient: rate 1, its product 1, the root of v 1, its factor 1 + 1, the sum with eps 1, the division 1; eps itself is
+        # taken rounded.  The difference 1, of a number of at most |p| + |u| (1 + small).
+        tol = 1.01 * EPS32 * (3 * np.abs(p) + 8 * u) + 2.0 ** -149
+        if x.fp8 or (x.master is None and x.p.dtype == B):
+            r = adamw.random_bits(seed, t, i, 0, x.n)
+        if x.fp8:
+            for got, scales, state, fmt in ((x.m, x.m_scale, m, fp8.E4M3), (x.v, x.v_scale, v, fp8.E5M2)):
+                q, s = adamw.encode(state, r, fmt)
+                assert np.array_equal(host(scales), s)
+                assert np.array_equal(host(got), q)
+        else:
+            assert np.array_equal(host(x.m).astype(np.float32), m) and np.array_equal(host(x.v).astype(np.float32), v)
+        got = host(x.p)
+        if x.master is not None:
+            kept = host(x.master)
+            assert np.all(np.abs(kept - want) <= tol), (i, np.abs(kept - want).max())
+            assert torch.equal(bits(x.p), bits(x.master.to(B)))
+        elif x.p.dtype == F:
+            assert np.all(np.abs(got - want) <= tol), (i, np.abs(got - want).max())
+        else:
+            # one of the two bf16 numbers beside a binary32 number within tol
+            step = np.exp2(np.floor(np.log2(np.maximum(np.abs(want), 2.0 ** -126))) - 7)
+            assert np.all(np.abs(got - want) <= step * 1.01 + tol)
+            far = (np.abs(want) % step) / step * 65536                                         # the share dropped, and the random bits that carry it
+            up = (far + ((r.astype(np.int64) * 0x9E3779B1 & adamw.MASK) >> 16)) >= 65536
+            sure = np.abs(far + ((r.astype(np.int64) * 0x9E3779B1 & adamw.MASK) >> 16) - 65536) > 1 + tol / step * 65536
+            assert sure.mean() > 0.9
+            pick = np.sign(want) * (np.floor(np.abs(want) / step) + up) * step
+            assert np.array_equal(got[sure], pick[sure])
+
+
+def gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+STATES = [fog.STATES_F32, fog.STATES_FP8]
+
+
+@pytest.mark.parametrize("states", STATES)
+@pytest.mark.parametrize("n", [1, 7, 8, 127, 128, 129, 1000, 2048, 8191, 8192, 8193, 40003])
+def test_sizes(states, n):
+    check([Tensor(gen(n), n, states)])
+
+
+@pytest.mark.parametrize("states", STATES)
+@pytest.mark.parametrize("p,g,master", [(B, B, True), (B, F, True), (B, B, False), (B, F, False), (F, B, False), (F, F, False)])
+@pytest.mark.parametrize("clip", [None, 1e-3, 1e6])
+def test_types_and_clipping(states, p, g, master, clip):
+    k = gen(3)
+    check([Tensor(k, n, states, p=p, g=g, master=master, decay=d) for n, d in ((5000, 0.1), (300, 0.0), (1, 0.0))], clip=clip)
+
+
+@pytest.mark.parametrize("states", STATES)
+@pytest.mark.parametrize("skew", [1, 3, 5])
+@pytest.mark.parametrize("master", [True, False])
+def test_every_alignment(states, skew, master):
+    x = Tensor(gen(skew), 9001, states, skew=skew, master=master)
+    edges = {k: t._base for k, t in x.written().items()}
+    keep = {k: (b[:skew].clone(), b[skew + x.written()[k].numel():].clone()) for k, b in edges.items()}
+    check([x])
+    for k, b in edges.items():       # what lies around a buffer is left
+        assert torch.equal(b[:skew], keep[k][0]) and torch.equal(b[skew + x.written()[k].numel():], keep[k][1]), k
+
+
+@pytest.mark.parametrize("states", STATES)
+def test_more_tensors_than_a_launch_takes_and_empty_ones(states):
+    k = gen(4)
+    check([Tensor(k, (37 * i) % 301, states, p=(B, F)[i % 2], master=i % 4 == 0, decay=0.01 * (i % 3)) for i in range(112)], clip=0.5)
+
+
+@pytest.mark.parametrize("states", STATES)
+@pytest.mark.parametrize("t", [1, 2, 100, 1000000, (1 << 33) + 5])
+@pytest.mark.parametrize("betas", [(0.9, 0.95), (0.0, 0.5), (0.5, 0.0), (0.99, 0.99)])
+def test_steps_and_betas(states, t, betas):
+    check([Tensor(gen(5), 3000, states, zero=t == 1)], t=t, beta1=betas[0], beta2=betas[1])
+
+
+def test_slow_second_moment_in_32_bits():
+    check([Tensor(gen(6), 3000, fog.STATES_F32)], beta1=0.9, beta2=0.9999, t=3, eps=1e-6)
+
+
+@pytest.mark.parametrize("states", STATES)
+def test_gradients_of_zero_and_first_step(states):
+    x = Tensor(gen(7), 500, states, zero=True)
+    x.g.zero_()
+    check([x], t=1)
+    assert bool((x.m == 0).all()) and bool((x.v == 0).all())
+
+
+def test_states_over_many_binades_stay_above_zero():
+    """Gradients over 40 binades in one block: second moments below the format's reach keep the smallest code above zero, and first moments round to zero or to it."""
+    x = Tensor(gen(8), 1024, fog.STATES_FP8, zero=True, g=F)
+    x.g.copy_(torch.exp2(torch.arange(1024, device="cuda").float() % 41 - 30) * torch.where(torch.arange(1024, device="cuda") % 2 == 0, 1.0, -1.0))
+    check([x], t=1)
+    assert bool((x.v > 0).all())
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("states", STATES)
+def test_a_norm_that_is_not_finite_leaves_the_step_out(states, bad):
+    k = gen(9)
+    xs = [Tensor(k, n, states) for n in (3000, 40)]
+    xs[1].g[3] = bad
+    keep = [{n: bits(t) for n, t in x.written().items()} for x in xs]
+    sumsq = torch.zeros(1, dtype=torch.float64, device="cuda")
+    fog.grad_sumsq(fog.make_grad_jobs([x.g for x in xs]), sumsq, torch.empty(fog.grad_sumsq_workspace(2), dtype=torch.uint8, device="cuda"))
+    fog.adamw(fog.make_adamw_jobs([x.item() for x in xs]), 1e-2, 5, sumsq=sumsq, max_norm=1.0)
+    torch.cuda.synchronize()
+    assert not math.isfinite(sumsq.item())
+    for x, kept in zip(xs, keep):
+        for n, t in x.written().items():
+            assert torch.equal(bits(t), kept[n]), n
+
+
+@pytest.mark.parametrize("states", STATES)
+def test_a_moment_that_is_not_finite_shows_and_spoils_its_block_only(states):
+    x, y = Tensor(gen(10), 1000, states), Tensor(gen(10), 1000, states)
+    x.g[200] = float("nan")
+    fog.adamw(fog.make_adamw_jobs([x.item()]), 1e-2, 5)
+    fog.adamw(fog.make_adamw_jobs([y.item()]), 1e-2, 5)
+    assert math.isnan(x.p[200].item()) and math.isnan(x.master[200].item())
+    for name in ("p", "m", "v"):
+        a, b = x.item()[name], y.item()[name]
+        assert torch.equal(a[:128], b[:128]) and torch.equal(a[256:], b[256:])
+    if states == fog.STATES_FP8:
+        assert np.isnan(fp8.decode(x.m.cpu().numpy(), fp8.E4M3)[200]) and np.isnan(fp8.decode(x.v.cpu().numpy(), fp8.E5M2)[200])
+    else:
+        assert math.isnan(x.m[200].item()) and math.isnan(x.v[200].item())
+
+
+@pytest.mark.parametrize("states", STATES)
+def test_rate_and_step_in_device_memory(states):
+    """The numbers of the host and those of the device give the same bits."""
+    xs = [Tensor(gen(11), 3000, states) for _ in range(2)]
+    lr = torch.full((1,), 2.0 ** -7, device="cuda")
+    fog.adamw(fog.make_adamw_jobs([xs[0].item()]), 2.0 ** -7, 12, seed=99)
+    fog.adamw(fog.make_adamw_jobs([xs[1].item()]), lr, torch.full((1,), 12, dtype=torch.int64, device="cuda"), seed=99)
+    for (k, a), b in zip(xs[0].written().items(), xs[1].written().values()):
+        assert torch.equal(bits(a), bits(b)), k
+
+
+@pytest.mark.parametrize("states", STATES)
+def test_steps_in_a_graph(states):
+    """Captured once with its rate and step in device memory, replayed over several steps with eager work between: the eager steps' bits."""
+    k = [gen(12), gen(12)]
+    a, b = ([Tensor(g, n, states, master=n != 700) for n in (20000, 700, 5)] for g in k)
+    lr, step = torch.zeros(1, device="cuda"), torch.zeros(1, dtype=torch.int64, device="cuda")
+    sumsq = torch.zeros(1, dtype=torch.float64, device="cuda")
+    jobs_a, jobs_b = (fog.make_adamw_jobs([x.item() for x in xs]) for xs in (a, b))
+    sums = fog.make_grad_jobs([x.g for x in b])
+    ws = torch.empty(fog.grad_sumsq_workspace(3), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step.add_(1)
+        fog.grad_sumsq(sums, sumsq, ws)
+        fog.adamw(jobs_b, lr, step, seed=5, sumsq=sumsq, max_norm=0.3)
+    noise = gen(13)
+    for t in range(1, 6):
+        for x, y in zip(a, b):
+            x.g.copy_(torch.randn(x.n, device="cuda", generator=noise) * 1e-2)
+            y.g.copy_(x.g)
+        lr.fill_(2.0 ** -t)
+        fog.grad_sumsq(fog.make_grad_jobs([x.g for x in a]), sumsq, ws)
+        fog.adamw(jobs_a, 2.0 ** -t, t, seed=5, sumsq=sumsq, max_norm=0.3)
+        torch.cuda.synchronize()
+        sumsq.fill_(-1.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert step.item() == t
+        for x, y in zip(a, b):
+            for name, s in x.written().items():
+                assert torch.equal(bits(s), bits(y.written()[name])), (t, name)
+
+
+def test_two_streams_at_once():
+    xs = [[Tensor(gen(20 + i), 100003, fog.STATES_FP8) for i in range(2)] for _ in range(2)]
+    for t in range(1, 4):
+        for x in xs[0]:
+            fog.adamw(fog.make_adamw_jobs([x.item()]), 1e-2, t, seed=1)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for t in range(1, 4):
+        for x, s in zip(xs[1], streams):
+            fog.adamw(fog.make_adamw_jobs([x.item()]), 1e-2, t, seed=1, stream=s)
+    torch.cuda.synchronize()
+    for x, y in zip(*xs):
+        for name, s in x.written().items():
+            assert torch.equal(bits(s), bits(y.written()[name])), name
+
+
+def test_rounding_keeps_the_expected_value():
+    """The same step under 4000 seeds: the mean of a state's values is the state.  A value lies between its two codes, at most a step apart, with the standard
+    deviation of at most half a step: the mean of 4000 within six times that over sqrt 4000."""
+    n, seeds = 256, 4000
+    base = Tensor(gen(30), n, fog.STATES_FP8, master=False)
+    _, g, m, v = base.values()
+    m, v = adamw.moments(m, v, g, np.float32(1), 0.9, 0.95)
+    rows = [Tensor(gen(30), n, fog.STATES_FP8, master=False) for _ in range(8)]
+    jobs = [fog.make_adamw_jobs([x.item()]) for x in rows]
+    total, square, p_total = {"m": 0.0, "v": 0.0}, {}, 0.0
+    start = {k: t.clone() for k, t in base.written().items()}
+    for s in range(seeds):
+        x = rows[s % 8]
+        for k, t in x.written().items():
+            t.copy_(start[k])
+        fog.adamw(jobs[s % 8], 1e-2, 7, seed=s)
+        for k, fmt in (("m", torch.float8_e4m3fn), ("v", torch.float8_e5m2)):
+            scale = torch.exp2(x.item()[k + "_scale"].double() - 127).repeat_interleave(128)
+            total[k] = total[k] + x.item()[k].view(fmt).double() * scale
+        p_total = p_total + x.p.double()
+    for k, want, places in (("m", m, 3), ("v", v, 2)):
+        scale = np.repeat(np.exp2(host(rows[0].item()[k + "_scale"]).astype(float) - 127), 128)
+        low = {3: 2.0 ** -6, 2: 2.0 ** -14}[places] * scale
+        step = np.maximum(np.exp2(np.floor(np.log2(np.maximum(np.abs(want), low)))), low) * 2.0 ** -places
+        floor = (want > 0) * 2.0 ** -16 * scale if k == "v" else 0.0       # a second moment below the smallest code is raised to it
+        assert np.all(np.abs(host(total[k]) / seeds - want) <= 6 * 0.5 * step / math.sqrt(seeds) + floor), k
+    want, _ = adamw.update(host(base.p), m, v, 1e-2, 0.9, 0.95, 1e-8, 0.1, 7)
+    step = np.exp2(np.floor(np.log2(np.abs(want))) - 7)
+    assert np.all(np.abs(host(p_total) / seeds - want) <= 6 * 0.5 * step / math.sqrt(seeds) + 2.0 ** -16 * step + 12 * EPS32)
+
+
+def test_a_tensor_of_more_than_2_to_the_32_elements():
+    """The last elements of a long tensor: their codes, their scales and the random numbers of element numbers above 32 bits."""
+    n, tail = (1 << 32) + 300, 1000
+    p, g = torch.zeros(n, dtype=B, device="cuda"), torch.zeros(n, dtype=B, device="cuda")
+    m, v = torch.zeros(n, dtype=torch.uint8, device="cuda"), torch.zeros(n, dtype=torch.uint8, device="cuda")
+    ms, vs = (torch.zeros(-(-n // 128), dtype=torch.uint8, device="cuda") for _ in range(2))
+    g[n - tail:] = (torch.randn(tail, device="cuda", generator=gen(40)) * 1e-2).to(B)
+    fog.adamw(fog.make_adamw_jobs([dict(p=p, g=g, m=m, v=v, m_scale=ms, v_scale=vs)]), 1e-2, 1, seed=3)
+    torch.cuda.synchronize()
+    first = (n - tail) // 128 * 128
+    want_m, want_v = adamw.moments(np.zeros(n - first), np.zeros(n - first), host(g[first:]), np.float32(1), 0.9, 0.95)
+    r = adamw.random_bits(3, 1, 0, first, n - first)
+    for got, scales, state, fmt in ((m, ms, want_m, fp8.E4M3), (v, vs, want_v, fp8.E5M2)):
+        q, s = adamw.encode(state, r, fmt)
+        assert np.array_equal(got[first:].cpu().numpy(), q) and np.array_equal(scales[first // 128:].cpu().numpy(), s)
+    assert bool((p[:first] == 0).all()) and bool((m[:first] == 0).all()) and bool((p[n - tail:][g[n - tail:] != 0] != 0).all())
+
+
+def test_the_binding_refuses_tensors_of_other_devices_and_types():
+    x = Tensor(gen(50), 100, fog.STATES_F32)
+    jobs = fog.make_adamw_jobs([x.item()])
+    with pytest.raises(ValueError):
+        fog.adamw(fog.make_adamw_jobs([{k: t.cpu() if isinstance(t, torch.Tensor) else t for k, t in x.item().items()}]), 1e-2, 1)
+    with pytest.raises(ValueError):
+        fog.adamw(jobs, torch.full((1,), 1e-2), 1)
+    with pytest.raises(ValueError):
+        fog.adamw(jobs, 1e-2, torch.ones(1, device="cuda"))
+    with pytest.raises(ValueError):
+        fog.adamw(jobs, 1e-2, 1, sumsq=torch.ones(1, device="cuda"))
