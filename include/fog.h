@@ -243,6 +243,76 @@ fog_status fog_rmsnorm_quantize(const void* x_bf16, int64_t rows, int64_t cols, 
                                 const float* scale, uint8_t* q, int64_t ldq, float* amax_out, void* stream);
 
 /*
+ * Rotary positions (Appendix B), between the projection of a block and attention: QK norm, turn, FP8 cast and the change of layout in one pass over Q, K and V.
+ * Per token and head, x a vector of D elements, p the token's position, c_i and s_i row p of the table:
+ *     z = gain x / rms(x)                     (as fog_rmsnorm_quantize; gain == 0: z = x)
+ *     y_a = z_a c_i - z_b s_i,  y_b = z_b c_i + z_a s_i      for the pairs i of the first `rot` elements, the others stay:
+ *         FOG_ROPE_HALF         (a, b) = (i, i + rot / 2)          FOG_ROPE_INTERLEAVED  (a, b) = (2i, 2i + 1)
+ *     q = sat_rne_fmt( fl32( y * scale ) ),   amax = max |y| over the job      (binary32; y is not stored)
+ *   jobs : HOST array of `count` (0 .. FOG_ROPE_JOBS_MAX) tensors of B sequences of S tokens, typically Q, K and V; read before the call returns.
+ *     x, q  : element (b, s, h, d) at p + b batch + s token + h head + d, strides in elements, any that are not negative (and under which no
+ *             vector of q meets another): ranges of the projection's columns, [B, heads, S, D], rows of a cache.   x bfloat16, q codes.
+ *     rotate == 0 : no positions (V).   scale : one float.   amax : NULL or one float, overwritten; jobs may name the same one, for their common maximum.
+ *   table : [positions, rot] floats, a row the cosines of the pairs, then their sines: fog_rope_table, or any other.  c^2 + s^2 need not be 1.
+ *   pos : B * S positions of pos_bytes (4 or 8) bytes, signed; NULL: token s of every sequence has position offset + s.  A token whose position is no row of the
+ *         table (padding) has y = 0 in the jobs that are turned.
+ *   D up to FOG_ROPE_DIM_MAX, rot even, up to D; rows of any alignment.  Multiples of 16 for both, with a 16-byte aligned table, are the fastest.
+ *   workspace : fog_rope_workspace() bytes (64 KB), 4-byte aligned, where a job has an amax; contents on entry do not matter.  Calls that may overlap in
+ *         time need a workspace each.
+ * Errors: NULL, SHAPE (count, sizes, strides), ALIGN, WORKSPACE, UNSUPPORTED (format, layout, odd rot, D, B * S above 2^31 - 1, heads above 2^24, pos_bytes, gain
+ * negative or not finite; an output that lies within an input's first and last element, or outputs that are not seen to lie apart).
+ *
+ * fog_rope_grad is the way back, per token and head with dy the gradient of y:
+ *     dz = the transposed turn of dy;     dx = gain / rms(x) (dz - x (x . dz) / (x . x))      (gain == 0: dx = dz; x is not looked at; a vector of zeros: 0)
+ * rounded once to bfloat16.  dx receives it, q its cast (of the ROUNDED value, as fog_quantize of a stored dx would give); either may have p == NULL.
+ * amax = max |dx|, the rounded.  Padding has dx = 0 where it is turned.  Jobs that write ranges of one matrix (the gradient of the projection's result, one operand of
+ * its products) name one scale and one amax.
+ * A sum of squares is held in binary32: vectors beyond 10^18 lose their norm, in either direction.
+ */
+#define FOG_ROPE_JOBS_MAX 8
+#define FOG_ROPE_DIM_MAX 1008
+typedef enum { FOG_ROPE_HALF = 0, FOG_ROPE_INTERLEAVED = 1 } fog_rope_layout;
+typedef struct {
+  void* p;
+  int64_t batch, token, head;
+} fog_heads;
+typedef struct {
+  fog_heads x, q;
+  int heads, rotate;
+  float gain;
+  fog_fp8 fmt;
+  const float* scale;
+  float* amax;
+} fog_rope_job;
+typedef struct {
+  fog_heads dy, x, dx, q;
+  int heads, rotate;
+  float gain;
+  fog_fp8 fmt;
+  const float* scale;   /* may be NULL without q */
+  float* amax;
+} fog_rope_grad_job;
+fog_status fog_rope_quantize(const fog_rope_job* jobs, int count, int B, int S, int D, int rot, fog_rope_layout layout, const float* table,
+                             int64_t positions, const void* pos, int pos_bytes, int64_t offset, void* workspace, size_t workspace_bytes, void* stream);
+fog_status fog_rope_grad(const fog_rope_grad_job* jobs, int count, int B, int S, int D, int rot, fog_rope_layout layout, const float* table,
+                         int64_t positions, const void* pos, int pos_bytes, int64_t offset, void* workspace, size_t workspace_bytes, void* stream);
+size_t fog_rope_workspace(void);
+
+/*
+ * The table of the calls above for positions first .. first + positions - 1, from binary64 angles (far positions keep their places):
+ *     f_i = base^(-2i / rot), row p: amplitude cos(p f_i), then amplitude sin(p f_i), i = 0 .. rot / 2 - 1.
+ * For contexts longer than the `original` number of tokens that a model was trained on: f_i is divided by factor where a pair turns less than `low` times in
+ * the original length, kept where it turns more than `high` times, and blended in between: f_i ((1 - k) / factor + k), k = clamp((original f_i / 2 pi - low)
+ * / (high - low), 0, 1).  original == 0: every f_i is divided (positions interpolated).  factor == 1: none is.
+ *   scaling : HOST struct, or NULL for {base 10000, factor 1, amplitude 1}.   table : [positions, rot] floats, overwritten.
+ * Errors: NULL, SHAPE, ALIGN, UNSUPPORTED (odd rot, positions above 2^31, |first| above 2^52, base or factor not above 0, high not above low, values that are not finite).
+ */
+typedef struct {
+  double base, factor, low, high, original, amplitude;
+} fog_rope_scaling;
+fog_status fog_rope_table(const fog_rope_scaling* scaling, int64_t first, int64_t positions, int rot, float* table, void* stream);
+
+/*
  * xIELU activation fused with the FP8 cast (Appendix B, equation xIELU: the activation of the
  * FOG-max variant, between the two GEMMs of the feed-forward block):
  *     y = alpha_p x^2 + 0.5 x                       for x > 0

@@ -1,0 +1,555 @@
+// Rotary positions between the projection and attention: the QK norm, the turn by the token's position, the FP8 cast and the change from the projection's
+// layout to the heads that attention reads, in one pass; and the way back.
+//
+// Bound by memory: forward 2 bytes read and 1 written an element, backward 2 (4 with the norm) and 1 or 3.
+//
+// A token's vector of one head (D elements) belongs to LPR lanes, a wave takes 64 / LPR tokens and walks some heads of them, so that the cosines
+// and sines, 16 of them a lane, are loaded once for all of these.  A lane holds two runs of eight elements: in the half layout eight elements and their
+// eight partners, side by side eight pairs that lie together, and sixteen elements behind the turned part: no element has its partner in another lane.
+#include <cfloat>
+#include <cmath>
+
+#include "common.h"
+#include "launch.h"
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int WORDS = 16384;             // most workgroups of a launch: an abs-max of each in the workspace
+constexpr int JOBS = FOG_ROPE_JOBS_MAX;
+constexpr int HEADS_MAX = 1 << 24;
+
+struct Job {
+  fog_heads in, x, dx, q;                // in: x of the forward, dy of the backward; x, dx: backward only
+  const float* scale;
+  int heads, first;                      // first: number of the job's first workgroup
+  float gain;
+  uint8_t rotate, e5m2;
+};
+struct Jobs {
+  Job job[JOBS];
+  int count;
+};
+struct Shape {
+  const float* table;
+  const void* pos;
+  uint32_t* part;                        // a word for each workgroup, or NULL
+  int64_t positions, offset;
+  uint32_t tokens, S, groups;            // groups: of tokens that a job's workgroups walk side by side
+  int D, rot, segment, pos_bytes;        // segment: heads of a workgroup
+};
+static_assert(sizeof(Jobs) + sizeof(Shape) <= 4096, "arguments of a launch");
+
+template <int CTRL>
+FOG_DEVICE float dpp_add(float s) {
+  return s + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(s), CTRL, 0xF, 0xF, false));
+}
+// Sum over the LPR lanes of a vector, in every lane.
+template <int LPR>
+FOG_DEVICE float row_sum(float s) {
+  s = dpp_add<0xB1>(s);                  // lane ^ 1
+  s = dpp_add<0x4E>(s);                  // lane ^ 2
+  if (LPR >= 8) s = dpp_add<0x141>(s);   // the other four of eight
+  if (LPR >= 16) s = dpp_add<0x140>(s);  // the other eight of sixteen
+  if (LPR >= 32) s += __shfl_xor(s, 16, 64);
+  if (LPR >= 64) s += __shfl_xor(s, 32, 64);
+  return s;
+}
+
+// 1 / rms with a gain, correctly rounded; 0 for a vector of zeros (NaN for one that holds a NaN).
+FOG_DEVICE float inv_rms(float sumsq, float cols, float gain) { return sumsq != 0.0f ? gain / __builtin_sqrtf(sumsq / cols) : 0.0f; }
+
+FOG_DEVICE void unpack8(uint4 v, float (&f)[8]) {
+  f[0] = bf16lo(v.x); f[1] = bf16hi(v.x); f[2] = bf16lo(v.y); f[3] = bf16hi(v.y);
+  f[4] = bf16lo(v.z); f[5] = bf16hi(v.z); f[6] = bf16lo(v.w); f[7] = bf16hi(v.w);
+}
+FOG_DEVICE uint4 pack8(const float (&f)[8]) {
+  return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
+}
+
+template <bool FULL>
+FOG_DEVICE uint4 fetch(const uint16_t* p, int n) {
+  if (FULL) return n > 0 ? ld_any_nt16(p) : make_uint4(0, 0, 0, 0);
+  return n >= 8 ? ld_any_nt16(p) : ld_upto8(p, n);
+}
+typedef u32x2 __attribute__((aligned(1))) u32x2_byte;
+template <bool FULL>
+FOG_DEVICE void store_codes(uint8_t* p, uint2 w, int n) {
+  if (FULL ? n > 0 : n >= 8) {
+    u32x2 v = {w.x, w.y};
+    *reinterpret_cast<u32x2_byte*>(p) = v;
+  } else if (!FULL) {
+    st_upto8(p, w, n);
+  }
+}
+template <bool FULL>
+FOG_DEVICE void store_half(uint16_t* p, uint4 w, int n) {
+  if (FULL ? n > 0 : n >= 8) st_any16(p, w);
+  else if (!FULL) st_upto8(p, w, n);
+}
+
+FOG_DEVICE uint2 cast8(const float (&y)[8], float rho, bool e5m2, bool& nan) {
+  if (e5m2)
+    return make_uint2(cvt4_fp8_nan<FOG_E5M2>(y[0] * rho, y[1] * rho, y[2] * rho, y[3] * rho, &nan), cvt4_fp8_nan<FOG_E5M2>(y[4] * rho, y[5] * rho, y[6] * rho, y[7] * rho, &nan));
+  return make_uint2(cvt4_fp8_nan<FOG_E4M3>(y[0] * rho, y[1] * rho, y[2] * rho, y[3] * rho, &nan), cvt4_fp8_nan<FOG_E4M3>(y[4] * rho, y[5] * rho, y[6] * rho, y[7] * rho, &nan));
+}
+
+// The turn by (c, s) of eight pairs, or with BACK its transpose.
+template <bool INTER, bool BACK>
+FOG_DEVICE void turn(float (&a)[8], float (&b)[8], const float (&c)[8], const float (&s)[8]) {
+  auto pair = [](float& u, float& w, float c, float s) {
+    const float v = BACK ? __builtin_fmaf(u, c, w * s) : __builtin_fmaf(u, c, -(w * s));
+    w = BACK ? __builtin_fmaf(w, c, -(u * s)) : __builtin_fmaf(w, c, u * s);
+    u = v;
+  };
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    if (!INTER) pair(a[k], b[k], c[k], s[k]);
+    else if (k < 4) pair(a[2 * k], a[2 * k + 1], c[k], s[k]);
+    else pair(b[2 * k - 8], b[2 * k - 7], c[k], s[k]);
+  }
+}
+
+template <int LPR, bool INTER, bool GRAD, bool FULL>
+__global__ __launch_bounds__(kThreads) void rope_kernel(Jobs jobs, Shape sh) {
+  constexpr int TOKENS = kThreads / LPR;        // of a workgroup and trip
+  constexpr int U = GRAD ? 2 : 4;               // heads in flight
+  int j = 0;
+  while (j + 1 < jobs.count && (int)blockIdx.x >= jobs.job[j + 1].first) ++j;
+  const Job& job = jobs.job[j];
+  const uint32_t at = blockIdx.x - job.first;
+  const int h0 = (int)(at / sh.groups) * sh.segment, h1 = h0 + sh.segment < job.heads ? h0 + sh.segment : job.heads;
+  const int lane = threadIdx.x % LPR;
+  const bool rotate = job.rotate != 0;
+  const int half = rotate ? sh.rot >> 1 : 0, turners = (half + 7) >> 3;
+  const bool on = lane < turners;
+  int offA, offB, nA, nB;
+  if (on) {
+    const int pairs = half - 8 * lane < 8 ? half - 8 * lane : 8;
+    offA = (INTER ? 16 : 8) * lane;
+    offB = INTER ? offA + 8 : offA + half;
+    nA = INTER ? (2 * pairs < 8 ? 2 * pairs : 8) : pairs;
+    nB = INTER ? 2 * pairs - nA : pairs;
+  } else {
+    offA = 2 * half + 16 * (lane - turners);
+    offB = offA + 8;
+    const int n = sh.D - offA;
+    nA = n < 0 ? 0 : n < 8 ? n : 8;
+    nB = n - 8 < 0 ? 0 : n - 8 < 8 ? n - 8 : 8;
+  }
+  const float rho = job.q.p ? *job.scale : 0.0f;
+  const bool norm = job.gain > 0.0f, e5m2 = job.e5m2 != 0;
+  const float cols = (float)sh.D;
+  float top = 0.0f;
+  bool nan = false;
+  uint32_t top_bits = 0u;
+  for (uint32_t group = at % sh.groups; group * (uint64_t)TOKENS < sh.tokens; group += sh.groups) {
+    const uint32_t t = group * TOKENS + threadIdx.x / LPR;
+    if (t >= sh.tokens) break;           // (whole vectors: their lanes leave together)
+    const uint32_t b = t / sh.S, s = t - b * sh.S;
+    bool there = true;
+    float c[8], sn[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) { c[k] = 1.0f; sn[k] = 0.0f; }
+    if (rotate) {
+      const int64_t p = !sh.pos ? sh.offset + (int64_t)s
+                                : sh.pos_bytes == 8 ? reinterpret_cast<const int64_t*>(sh.pos)[t] : (int64_t)reinterpret_cast<const int32_t*>(sh.pos)[t];
+      there = p >= 0 && p < sh.positions;
+      if (on && there) {
+        const float* row = sh.table + p * sh.rot + 8 * lane;
+        if (FULL) {
+          const float4 c0 = *reinterpret_cast<const float4*>(row), c1 = *reinterpret_cast<const float4*>(row + 4);
+          const float4 s0 = *reinterpret_cast<const float4*>(row + half), s1 = *reinterpret_cast<const float4*>(row + half + 4);
+          c[0] = c0.x; c[1] = c0.y; c[2] = c0.z; c[3] = c0.w; c[4] = c1.x; c[5] = c1.y; c[6] = c1.z; c[7] = c1.w;
+          sn[0] = s0.x; sn[1] = s0.y; sn[2] = s0.z; sn[3] = s0.w; sn[4] = s1.x; sn[5] = s1.y; sn[6] = s1.z; sn[7] = s1.w;
+        } else {
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            if (8 * lane + k < half) { c[k] = row[k]; sn[k] = row[half + k]; }
+        }
+      }
+    }
+    const uint16_t* in = reinterpret_cast<const uint16_t*>(job.in.p) + b * job.in.batch + s * job.in.token;
+    const uint16_t* xin = GRAD && norm ? reinterpret_cast<const uint16_t*>(job.x.p) + b * job.x.batch + s * job.x.token : nullptr;
+    uint8_t* q = job.q.p ? reinterpret_cast<uint8_t*>(job.q.p) + b * job.q.batch + s * job.q.token : nullptr;
+    uint16_t* dx = GRAD && job.dx.p ? reinterpret_cast<uint16_t*>(job.dx.p) + b * job.dx.batch + s * job.dx.token : nullptr;
+    for (int h = h0; h < h1; h += U) {
+      uint4 va[U], vb[U], xa[U], xb[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        va[u] = vb[u] = xa[u] = xb[u] = make_uint4(0, 0, 0, 0);
+        if (h + u < h1) {
+          const uint16_t* p = in + (h + u) * job.in.head;
+          va[u] = fetch<FULL>(p + offA, nA);
+          vb[u] = fetch<FULL>(p + offB, nB);
+          if (GRAD && norm) {
+            const uint16_t* x = xin + (h + u) * job.x.head;
+            xa[u] = fetch<FULL>(x + offA, nA);
+            xb[u] = fetch<FULL>(x + offB, nB);
+          }
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (h + u >= h1) break;
+        float a[8], e[8];
+        unpack8(va[u], a);
+        unpack8(vb[u], e);
+        if (!GRAD) {
+          if (norm) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum = __builtin_fmaf(a[k], a[k], sum);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum = __builtin_fmaf(e[k], e[k], sum);
+            const float inv = inv_rms(row_sum<LPR>(sum), cols, job.gain);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) { a[k] *= inv; e[k] *= inv; }
+          }
+          if (on) turn<INTER, false>(a, e, c, sn);
+          if (!there) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) a[k] = e[k] = 0.0f;
+          }
+#pragma unroll
+          for (int k = 0; k < 8; ++k) top = fmaxf(top, fmaxf(fabsf(a[k]), fabsf(e[k])));
+          uint8_t* to = q + (h + u) * job.q.head;
+          store_codes<FULL>(to + offA, cast8(a, rho, e5m2, nan), nA);
+          store_codes<FULL>(to + offB, cast8(e, rho, e5m2, nan), nB);
+        } else {
+          if (on) turn<INTER, true>(a, e, c, sn);
+          if (norm) {
+            float x0[8], x1[8], xx = 0.0f, xd = 0.0f;
+            unpack8(xa[u], x0);
+            unpack8(xb[u], x1);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) { xx = __builtin_fmaf(x0[k], x0[k], xx); xd = __builtin_fmaf(x0[k], a[k], xd); }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) { xx = __builtin_fmaf(x1[k], x1[k], xx); xd = __builtin_fmaf(x1[k], e[k], xd); }
+            xx = row_sum<LPR>(xx);
+            xd = row_sum<LPR>(xd);
+            const float inv = inv_rms(xx, cols, job.gain), along = xx != 0.0f ? xd / xx : 0.0f;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              a[k] = inv * __builtin_fmaf(-x0[k], along, a[k]);
+              e[k] = inv * __builtin_fmaf(-x1[k], along, e[k]);
+            }
+          }
+          uint4 wa = pack8(a), wb = pack8(e);
+          if (!there) wa = wb = make_uint4(0, 0, 0, 0);
+          top_bits = pkmax_abs_bf16(top_bits, wa.x); top_bits = pkmax_abs_bf16(top_bits, wa.y);
+          top_bits = pkmax_abs_bf16(top_bits, wa.z); top_bits = pkmax_abs_bf16(top_bits, wa.w);
+          top_bits = pkmax_abs_bf16(top_bits, wb.x); top_bits = pkmax_abs_bf16(top_bits, wb.y);
+          top_bits = pkmax_abs_bf16(top_bits, wb.z); top_bits = pkmax_abs_bf16(top_bits, wb.w);
+          if (dx) {
+            uint16_t* to = dx + (h + u) * job.dx.head;
+            store_half<FULL>(to + offA, wa, nA);
+            store_half<FULL>(to + offB, wb, nB);
+          }
+          if (q) {
+            float ra[8], rb[8];
+            unpack8(wa, ra);
+            unpack8(wb, rb);
+            uint8_t* to = q + (h + u) * job.q.head;
+            store_codes<FULL>(to + offA, cast8(ra, rho, e5m2, nan), nA);
+            store_codes<FULL>(to + offB, cast8(rb, rho, e5m2, nan), nB);
+          }
+        }
+      }
+    }
+  }
+  if (sh.part) {
+    const uint32_t m = wave_max_u32(GRAD ? max_of_pair(top_bits) << 16 : amax_bits(top, nan));
+    __shared__ uint32_t wave[kThreads / 64];
+    if ((threadIdx.x & 63) == 0) wave[threadIdx.x >> 6] = m;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      uint32_t r = wave[0];
+#pragma unroll
+      for (int w = 1; w < kThreads / 64; ++w) r = r > wave[w] ? r : wave[w];
+      sh.part[blockIdx.x] = r;
+    }
+  }
+}
+
+// The largest of the words of all jobs that name a result.
+struct Tops {
+  uint32_t* amax[JOBS];
+  int first[JOBS + 1];
+  uint8_t same[JOBS];      // jobs that name the result of job j
+};
+__global__ __launch_bounds__(kThreads) void rope_top_kernel(Tops t, const uint32_t* __restrict__ part) {
+  const int j = blockIdx.x;
+  if (!t.amax[j] || (t.same[j] & ((1 << j) - 1))) return;      // the first of them writes it
+  uint32_t m = 0u;
+  for (int k = 0; k < JOBS; ++k)
+    if (t.same[j] >> k & 1)
+      for (int i = t.first[k] + (int)threadIdx.x; i < t.first[k + 1]; i += kThreads) m = m > part[i] ? m : part[i];
+  m = wave_max_u32(m);
+  __shared__ uint32_t wave[kThreads / 64];
+  if ((threadIdx.x & 63) == 0) wave[threadIdx.x >> 6] = m;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+#pragma unroll
+    for (int w = 1; w < kThreads / 64; ++w) m = m > wave[w] ? m : wave[w];
+    *t.amax[j] = m;
+  }
+}
+
+// cos and sin of every position and pair from binary64 angles: far positions turn 10^5 times and more.  A thread keeps its pair's frequency for
+// sixteen positions.
+constexpr int TABLE_ROWS = 64;
+__global__ __launch_bounds__(kThreads) void rope_table_kernel(fog_rope_scaling sc, int64_t first, int64_t positions, int half, float* __restrict__ table) {
+  const int64_t p0 = (int64_t)blockIdx.x * TABLE_ROWS;
+  for (int i = threadIdx.x & 63; i < half; i += 64) {
+    double f = exp2(-(double)i / (double)half * log2(sc.base));
+    if (sc.factor != 1.0) {
+      double keep = 0.0;
+      if (sc.original > 0.0) {
+        keep = (sc.original * f * 0.15915494309189533577 - sc.low) / (sc.high - sc.low);
+        keep = keep < 0.0 ? 0.0 : keep > 1.0 ? 1.0 : keep;
+      }
+      f = f * ((1.0 - keep) / sc.factor + keep);
+    }
+    for (int r = threadIdx.x >> 6; r < TABLE_ROWS; r += kThreads / 64) {
+      if (p0 + r >= positions) break;
+      double s, c;
+      sincos((double)(first + p0 + r) * f, &s, &c);
+      float* row = table + (p0 + r) * 2 * half;
+      row[i] = (float)(c * sc.amplitude);
+      row[half + i] = (float)(s * sc.amplitude);
+    }
+  }
+}
+
+// ---------------------------------------------------------------- host
+// Where [B, S, heads] vectors of `row` bytes lie: bytes between neighbours, largest first, of the dimensions that have more than one.
+struct Box {
+  uintptr_t base;
+  int dims;
+  int64_t n[3], stride[3], row;
+  int64_t extent(int from) const {
+    int64_t e = row;
+    for (int i = from; i < dims; ++i) e += (n[i] - 1) * stride[i];
+    return e;
+  }
+};
+fog_status make_box(const fog_heads& h, int B, int S, int heads, int D, int size, Box* box) {
+  if (!h.p) return FOG_ERR_NULL;
+  const int64_t n[3] = {B, S, heads}, stride[3] = {h.batch, h.token, h.head};
+  box->base = reinterpret_cast<uintptr_t>(h.p);
+  if (box->base & (size - 1)) return FOG_ERR_ALIGN;
+  box->dims = 0;
+  box->row = (int64_t)D * size;
+  for (int i = 0; i < 3; ++i) {
+    if (n[i] <= 1) continue;
+    if (stride[i] < 0) return FOG_ERR_SHAPE;
+    if ((double)(n[i] - 1) * (double)stride[i] * size > 140737488355328.0) return FOG_ERR_UNSUPPORTED;      // 2^47 bytes: more than an address space holds
+    int at = box->dims++;
+    for (; at > 0 && box->stride[at - 1] < stride[i] * size; --at) {
+      box->n[at] = box->n[at - 1];
+      box->stride[at] = box->stride[at - 1];
+    }
+    box->n[at] = n[i];
+    box->stride[at] = stride[i] * size;
+  }
+  return FOG_OK;
+}
+// Whether no vector of a box lies on another of it.
+bool injective(const Box& a) {
+  for (int i = 0; i < a.dims; ++i)
+    if (a.stride[i] < a.extent(i + 1)) return false;
+  return true;
+}
+// Whether two boxes are seen to lie apart, b's first vector `off` bytes behind a's: one ends before the other begins, or both step by the same
+// distance and lie apart within a step.  (A step of a has two neighbours of b: the one at `off` modulo the distance and the one before.)
+bool apart(const Box& a, int ia, const Box& b, int ib, int64_t off) {
+  if (off >= a.extent(ia) || -off >= b.extent(ib)) return true;
+  if (ia >= a.dims || ib >= b.dims || a.stride[ia] != b.stride[ib] || a.stride[ia] <= 0) return false;
+  const int64_t s = a.stride[ia], r = ((off % s) + s) % s;
+  return apart(a, ia + 1, b, ib + 1, r) && apart(a, ia + 1, b, ib + 1, r - s);
+}
+bool apart_as_spans(const Box& a, const Box& b) {
+  return a.base + (uintptr_t)a.extent(0) <= b.base || b.base + (uintptr_t)b.extent(0) <= a.base;
+}
+
+struct Call {
+  Box in[2 * JOBS], out[2 * JOBS];
+  int ins = 0, outs = 0;
+  fog_status add(const fog_heads& h, int B, int S, int heads, int D, int size, bool written) {
+    const fog_status st = make_box(h, B, S, heads, D, size, written ? &out[outs] : &in[ins]);
+    if (st != FOG_OK) return st;
+    if (written && !injective(out[outs])) return FOG_ERR_SHAPE;
+    ++(written ? outs : ins);
+    return FOG_OK;
+  }
+  bool fine() const {
+    for (int i = 0; i < outs; ++i) {
+      for (int k = 0; k < ins; ++k)
+        if (!apart_as_spans(out[i], in[k])) return false;
+      for (int k = 0; k < i; ++k)
+        if (!apart(out[k], 0, out[i], 0, (int64_t)(out[i].base - out[k].base))) return false;
+    }
+    return true;
+  }
+};
+
+// What both directions look at before their jobs.
+fog_status check_call(int count, const void* jobs, int B, int S, int D, int rot, fog_rope_layout layout, const float* table, int64_t positions, const void* pos,
+                      int pos_bytes, int64_t offset) {
+  if (count < 0 || count > JOBS || B < 0 || S < 0 || D < 0 || rot < 0 || rot > D || positions < 0) return FOG_ERR_SHAPE;
+  if (count > 0 && !jobs) return FOG_ERR_NULL;
+  if (layout != FOG_ROPE_HALF && layout != FOG_ROPE_INTERLEAVED) return FOG_ERR_UNSUPPORTED;
+  if ((rot & 1) || D > FOG_ROPE_DIM_MAX || (int64_t)B * S > 0x7FFFFFFF) return FOG_ERR_UNSUPPORTED;
+  if (pos && pos_bytes != 4 && pos_bytes != 8) return FOG_ERR_UNSUPPORTED;
+  if (offset > ((int64_t)1 << 62) || offset < -((int64_t)1 << 62)) return FOG_ERR_UNSUPPORTED;
+  if ((reinterpret_cast<uintptr_t>(table) & 3) || (pos && (reinterpret_cast<uintptr_t>(pos) & (uintptr_t)(pos_bytes - 1)))) return FOG_ERR_ALIGN;
+  return FOG_OK;
+}
+
+template <bool GRAD>
+fog_status launch(Jobs& jobs, Shape& sh, float* const* amax, bool any_amax, int B, bool inter, void* workspace, hipStream_t s) {
+  const int lanes = (sh.rot / 2 + 7) / 8 + (sh.D - sh.rot + 15) / 16, plain = (sh.D + 15) / 16, need = lanes > plain ? lanes : plain;
+  const int lpr = need <= 4 ? 4 : need <= 8 ? 8 : need <= 16 ? 16 : need <= 32 ? 32 : 64;
+  const bool full = sh.rot % 16 == 0 && sh.D % 16 == 0 && (reinterpret_cast<uintptr_t>(sh.table) & 15) == 0;
+  sh.tokens = (uint32_t)((int64_t)B * sh.S);
+  const int64_t groups = ((int64_t)sh.tokens * lpr + kThreads - 1) / kThreads;
+  // Heads of a workgroup: as few as fill the chip, up to eight.
+  const int64_t want = 8 * (int64_t)fog_compute_units();
+  auto segments = [&](int64_t segment) {
+    int64_t n = 0;
+    for (int j = 0; j < jobs.count; ++j) n += (jobs.job[j].heads + segment - 1) / segment;
+    return n;
+  };
+  int64_t segment = 1;
+  while ((segment < 8 && segments(segment) * groups > want) || segments(segment) > WORDS / 2) segment *= 2;
+  sh.segment = (int)segment;
+  const int64_t all = segments(segment), most = all > 0 ? WORDS / all : 1;
+  sh.groups = (uint32_t)(groups < most ? groups : most);
+  int next = 0;
+  Tops tops = {};
+  for (int j = 0; j < jobs.count; ++j) {
+    jobs.job[j].first = tops.first[j] = next;
+    next += (int)((jobs.job[j].heads + segment - 1) / segment) * (int)sh.groups;
+    tops.amax[j] = reinterpret_cast<uint32_t*>(amax[j]);
+    for (int k = 0; k < jobs.count; ++k)
+      if (amax[j] && amax[k] == amax[j]) tops.same[j] |= (uint8_t)(1 << k);
+  }
+  for (int j = jobs.count; j <= JOBS; ++j) tops.first[j] = next;
+  sh.part = any_amax ? reinterpret_cast<uint32_t*>(workspace) : nullptr;
+  if (next > 0 && sh.tokens > 0 && sh.D > 0) {
+#define FOG_ROPE2(L, I, F) rope_kernel<L, I, GRAD, F><<<next, kThreads, 0, s>>>(jobs, sh)
+#define FOG_ROPE(L)                                             \
+  do {                                                          \
+    if (inter) { if (full) FOG_ROPE2(L, true, true); else FOG_ROPE2(L, true, false); }    \
+    else       { if (full) FOG_ROPE2(L, false, true); else FOG_ROPE2(L, false, false); }  \
+  } while (0)
+    if (lpr == 4) FOG_ROPE(4);
+    else if (lpr == 8) FOG_ROPE(8);
+    else if (lpr == 16) FOG_ROPE(16);
+    else if (lpr == 32) FOG_ROPE(32);
+    else FOG_ROPE(64);
+#undef FOG_ROPE
+#undef FOG_ROPE2
+  } else {
+    for (int j = 0; j <= JOBS; ++j) tops.first[j] = 0;
+    if (!any_amax) return FOG_OK;
+  }
+  if (any_amax) rope_top_kernel<<<jobs.count, kThreads, 0, s>>>(tops, sh.part);
+  return fog_launch_status();
+}
+
+}  // namespace
+
+extern "C" fog_status fog_rope_table(const fog_rope_scaling* scaling, int64_t first, int64_t positions, int rot, float* table, void* stream) {
+  fog_rope_scaling sc = {10000.0, 1.0, 0.0, 0.0, 0.0, 1.0};
+  if (scaling) sc = *scaling;
+  if (positions < 0 || rot < 0) return FOG_ERR_SHAPE;
+  if ((rot & 1) || positions > ((int64_t)1 << 31) || first < -((int64_t)1 << 52) || first > ((int64_t)1 << 52)) return FOG_ERR_UNSUPPORTED;
+  if (!(sc.base > 0.0) || !(sc.factor > 0.0) || !std::isfinite(sc.base) || !std::isfinite(sc.factor) || !std::isfinite(sc.amplitude)) return FOG_ERR_UNSUPPORTED;
+  if (!(sc.original >= 0.0) || !std::isfinite(sc.original)) return FOG_ERR_UNSUPPORTED;
+  if (sc.original > 0.0 && (!std::isfinite(sc.low) || !std::isfinite(sc.high) || !(sc.high > sc.low))) return FOG_ERR_UNSUPPORTED;
+  if (positions == 0 || rot == 0) return FOG_OK;
+  if (!table) return FOG_ERR_NULL;
+  if (reinterpret_cast<uintptr_t>(table) & 3) return FOG_ERR_ALIGN;
+  rope_table_kernel<<<(int)((positions + TABLE_ROWS - 1) / TABLE_ROWS), kThreads, 0, (hipStream_t)stream>>>(sc, first, positions, rot / 2, table);
+  return fog_launch_status();
+}
+
+extern "C" size_t fog_rope_workspace(void) { return WORDS * sizeof(uint32_t); }
+
+extern "C" fog_status fog_rope_quantize(const fog_rope_job* jobs, int count, int B, int S, int D, int rot, fog_rope_layout layout, const float* table,
+                                        int64_t positions, const void* pos, int pos_bytes, int64_t offset, void* workspace, size_t workspace_bytes,
+                                        void* stream) {
+  const fog_status st = check_call(count, jobs, B, S, D, rot, layout, table, positions, pos, pos_bytes, offset);
+  if (st != FOG_OK) return st;
+  Jobs all = {};
+  Call call;
+  float* amax[JOBS] = {};
+  bool any_amax = false;
+  const bool empty = B == 0 || S == 0 || D == 0;
+  all.count = count;
+  for (int j = 0; j < count; ++j) {
+    const fog_rope_job& in = jobs[j];
+    if (in.heads < 0) return FOG_ERR_SHAPE;
+    if (in.heads > HEADS_MAX) return FOG_ERR_UNSUPPORTED;
+    if ((in.fmt != FOG_E4M3 && in.fmt != FOG_E5M2) || !(in.gain >= 0.0f && in.gain <= FLT_MAX)) return FOG_ERR_UNSUPPORTED;
+    if (!in.scale) return FOG_ERR_NULL;
+    if ((reinterpret_cast<uintptr_t>(in.scale) | reinterpret_cast<uintptr_t>(in.amax)) & 3) return FOG_ERR_ALIGN;
+    if (in.heads > 0 && !empty) {
+      if (in.rotate && rot > 0 && !table) return FOG_ERR_NULL;
+      fog_status s = call.add(in.x, B, S, in.heads, D, 2, false);
+      if (s == FOG_OK) s = call.add(in.q, B, S, in.heads, D, 1, true);
+      if (s != FOG_OK) return s;
+    }
+    Job& to = all.job[j];
+    to.in = in.x; to.q = in.q; to.scale = in.scale; to.heads = empty ? 0 : in.heads; to.gain = in.gain; to.rotate = in.rotate && rot > 0; to.e5m2 = in.fmt == FOG_E5M2;
+    amax[j] = in.amax;
+    any_amax |= in.amax != nullptr;
+  }
+  if (!call.fine()) return FOG_ERR_UNSUPPORTED;
+  if (any_amax && (!workspace || workspace_bytes < fog_rope_workspace())) return FOG_ERR_WORKSPACE;
+  if (reinterpret_cast<uintptr_t>(workspace) & 3) return FOG_ERR_ALIGN;
+  Shape sh = {};
+  sh.table = table; sh.pos = pos; sh.positions = positions; sh.offset = offset; sh.S = (uint32_t)S; sh.D = D; sh.rot = rot; sh.pos_bytes = pos_bytes;
+  return launch<false>(all, sh, amax, any_amax, B, layout == FOG_ROPE_INTERLEAVED, workspace, (hipStream_t)stream);
+}
+
+extern "C" fog_status fog_rope_grad(const fog_rope_grad_job* jobs, int count, int B, int S, int D, int rot, fog_rope_layout layout, const float* table,
+                                    int64_t positions, const void* pos, int pos_bytes, int64_t offset, void* workspace, size_t workspace_bytes, void* stream) {
+  const fog_status st = check_call(count, jobs, B, S, D, rot, layout, table, positions, pos, pos_bytes, offset);
+  if (st != FOG_OK) return st;
+  Jobs all = {};
+  Call call;
+  float* amax[JOBS] = {};
+  bool any_amax = false;
+  const bool empty = B == 0 || S == 0 || D == 0;
+  all.count = count;
+  for (int j = 0; j < count; ++j) {
+    const fog_rope_grad_job& in = jobs[j];
+    if (in.heads < 0) return FOG_ERR_SHAPE;
+    if (in.heads > HEADS_MAX) return FOG_ERR_UNSUPPORTED;
+    if ((in.fmt != FOG_E4M3 && in.fmt != FOG_E5M2) || !(in.gain >= 0.0f && in.gain <= FLT_MAX)) return FOG_ERR_UNSUPPORTED;
+    if (in.q.p && !in.scale) return FOG_ERR_NULL;
+    if ((reinterpret_cast<uintptr_t>(in.scale) | reinterpret_cast<uintptr_t>(in.amax)) & 3) return FOG_ERR_ALIGN;
+    if (in.heads > 0 && !empty) {
+      if ((in.rotate && rot > 0 && !table) || (!in.q.p && !in.dx.p)) return FOG_ERR_NULL;
+      fog_status s = call.add(in.dy, B, S, in.heads, D, 2, false);
+      if (s == FOG_OK && in.gain > 0.0f) s = call.add(in.x, B, S, in.heads, D, 2, false);
+      if (s == FOG_OK && in.dx.p) s = call.add(in.dx, B, S, in.heads, D, 2, true);
+      if (s == FOG_OK && in.q.p) s = call.add(in.q, B, S, in.heads, D, 1, true);
+      if (s != FOG_OK) return s;
+    }
+    Job& to = all.job[j];
+    to.in = in.dy; to.x = in.x; to.dx = in.dx; to.q = in.q; to.scale = in.scale; to.heads = empty ? 0 : in.heads; to.gain = in.gain;
+    to.rotate = in.rotate && rot > 0; to.e5m2 = in.fmt == FOG_E5M2;
+    amax[j] = in.amax;
+    any_amax |= in.amax != nullptr;
+  }
+  if (!call.fine()) return FOG_ERR_UNSUPPORTED;
+  if (any_amax && (!workspace || workspace_bytes < fog_rope_workspace())) return FOG_ERR_WORKSPACE;
+  if (reinterpret_cast<uintptr_t>(workspace) & 3) return FOG_ERR_ALIGN;
+  Shape sh = {};
+  sh.table = table; sh.pos = pos; sh.positions = positions; sh.offset = offset; sh.S = (uint32_t)S; sh.D = D; sh.rot = rot; sh.pos_bytes = pos_bytes;
+  return launch<true>(all, sh, amax, any_amax, B, layout == FOG_ROPE_INTERLEAVED, workspace, (hipStream_t)stream);
+}

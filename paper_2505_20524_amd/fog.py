@@ -14,6 +14,8 @@ NT, NN, TN = 0, 1, 2
 VECTOR, TILE = 0, 1          # fog_block: how an operand's block scales lie
 BF16, F32 = 0, 1             # fog_real
 STATES_F32, STATES_FP8 = 0, 1    # fog_states
+HALF, INTERLEAVED = 0, 1     # fog_rope_layout
+ROPE_JOBS_MAX, ROPE_DIM_MAX = 8, 1008      # FOG_ROPE_JOBS_MAX, FOG_ROPE_DIM_MAX of the header
 CAST_BATCH_MAX = 32          # FOG_CAST_BATCH_MAX of the header
 
 _LIB = None
@@ -39,6 +41,10 @@ SIGNATURES = {
     "fog_quantize_delayed_state": (_SZ, []),
     "fog_delayed_amax": (_I, [_P, _I64, _P, _P]),
     "fog_rmsnorm_quantize": (_I, [_P, _I64, _I64, _I64, _F, _I, _P, _P, _I64, _P, _P]),
+    "fog_rope_quantize": (_I, [_P, _I, _I, _I, _I, _I, _I, _P, _I64, _P, _I, _I64, _P, _SZ, _P]),
+    "fog_rope_grad": (_I, [_P, _I, _I, _I, _I, _I, _I, _P, _I64, _P, _I, _I64, _P, _SZ, _P]),
+    "fog_rope_workspace": (_SZ, []),
+    "fog_rope_table": (_I, [_P, _I64, _I64, _I, _P, _P]),
     "fog_xielu_quantize": (_I, [_P, _I64, _I64, _I64, _F, _F, _I, _P, _P, _I64, _P, _P]),
     "fog_gelu_quantize": (_I, [_P, _I64, _I64, _I64, _I, _P, _P, _I64, _P, _P]),
     "fog_tanh_quantize": (_I, [_P, _I64, _I64, _I64, _F, _I, _P, _P, _I64, _P, _P]),
@@ -236,6 +242,107 @@ def rmsnorm_quantize(x, fmt, scale_t, q, gain=1.0, amax_out=None, stream=None):
     _check(load().fog_rmsnorm_quantize(_ptr(x), rows, cols, x.stride(0), gain, fmt, _ptr(scale_t), _ptr(q),
                                        q.stride(0) if q is not None else 0, _ptr(amax_out), _stream(stream)),
            "fog_rmsnorm_quantize")
+
+
+class RopeScaling(ctypes.Structure):
+    """Mirror of fog_rope_scaling."""
+    _fields_ = [(k, _D) for k in ("base", "factor", "low", "high", "original", "amplitude")]
+
+
+def rope_table(table, base=10000.0, first=0, factor=1.0, low=1.0, high=4.0, original=0.0, amplitude=1.0, stream=None):
+    """table [positions, rot]: cosines, then sines, of the pairs at positions first, first + 1, ...; factor, low, high, original: frequencies scaled for long contexts."""
+    positions, rot = table.shape
+    if table.dtype != torch.float32 or not table.is_contiguous():
+        raise ValueError("table: a contiguous float32 matrix is needed, got %s with strides %s" % (table.dtype, table.stride()))
+    scaling = RopeScaling(base, factor, low, high, original, amplitude)
+    _check(load().fog_rope_table(_c.byref(scaling), first, positions, rot, _ptr(table), _here(stream, table)), "fog_rope_table")
+
+
+class Heads(ctypes.Structure):
+    """Mirror of fog_heads."""
+    _fields_ = [("p", _P), ("batch", _I64), ("token", _I64), ("head", _I64)]
+
+
+class RopeJob(ctypes.Structure):
+    """Mirror of fog_rope_job."""
+    _fields_ = [("x", Heads), ("q", Heads), ("heads", _I), ("rotate", _I), ("gain", _F), ("fmt", _I), ("scale", _P), ("amax", _P)]
+
+
+class RopeGradJob(ctypes.Structure):
+    """Mirror of fog_rope_grad_job."""
+    _fields_ = [("dy", Heads), ("x", Heads), ("dx", Heads), ("q", Heads), ("heads", _I), ("rotate", _I), ("gain", _F), ("fmt", _I), ("scale", _P), ("amax", _P)]
+
+
+def _rope_jobs(kind, items, names, fmt):
+    arr = (kind * len(items))()
+    arr.tensors, arr.shape = [], None           # the array keeps the tensors alive
+    for job, item in zip(arr, items):
+        given = {k: item.get(k) for k in names}
+        B, S, heads, D = given[names[0]].shape
+        job.fmt = item.get("fmt", fmt)
+        for k, t in given.items():
+            if t is None:
+                continue
+            types = _codes(job.fmt) if k == "q" else _HALVES
+            if tuple(t.shape) != (B, S, heads, D) or t.dtype not in types or (D > 1 and t.stride(3) != 1):
+                raise ValueError("%s: a [%d, %d, %d, %d] tensor of one of %s with contiguous vectors is needed, got %s of %s with strides %s"
+                                 % (k, B, S, heads, D, types, tuple(t.shape), t.dtype, t.stride()))
+            setattr(job, k, Heads(_ptr(t), t.stride(0), t.stride(1), t.stride(2)))
+            arr.tensors.append(t)
+        if arr.shape not in (None, (B, S, D)):
+            raise ValueError("tensors of one batch, length and head size are needed, got %s beside %s" % ((B, S, D), arr.shape))
+        arr.shape = (B, S, D)
+        job.heads, job.rotate, job.gain = heads, int(item.get("rotate", True)), item.get("gain", 0.0)
+        for k in ("scale", "amax"):
+            _floats(item.get(k), k)
+            setattr(job, k, _ptr(item.get(k)))
+            arr.tensors += [item[k]] if item.get(k) is not None else []
+    arr.devices = {t.get_device() for t in arr.tensors}
+    return arr
+
+
+def make_rope_jobs(items):
+    """items: dicts of a tensor's x (bfloat16 [B, S, heads, D], any strides between vectors), q (codes, the same shape, any strides), scale, and where they are
+    wanted amax, rotate (True if missing), gain (0: no norm) and fmt (E4M3) -> ctypes array for rope_quantize (built once, reused while the tensors stay in place)."""
+    if any(item.get("q") is None for item in items):
+        raise ValueError("q: the codes' tensor is needed")
+    return _rope_jobs(RopeJob, items, ("x", "q"), E4M3)
+
+
+def make_rope_grad_jobs(items):
+    """items: dicts of dy (bfloat16 [B, S, heads, D]), x (the forward's, where gain is above 0), dx and / or q with its scale, amax, rotate, gain, fmt (E5M2)
+    -> ctypes array for rope_grad."""
+    return _rope_jobs(RopeGradJob, items, ("dy", "x", "dx", "q"), E5M2)
+
+
+def _rope(name, jobs, table, workspace, layout, positions, offset, stream):
+    rows, rot = (0, 0) if table is None else table.shape
+    if table is not None and (table.dtype != torch.float32 or not table.is_contiguous()):
+        raise ValueError("table: a contiguous float32 matrix is needed, got %s with strides %s" % (table.dtype, table.stride()))
+    B, S, D = jobs.shape or (0, 0, rot)
+    pos, size = None, 0
+    if positions is not None:
+        pos, size, count = _ids(positions)
+        if count != B * S:
+            raise ValueError("positions: one for each of the %d x %d tokens is needed, got %d" % (B, S, count))
+    _jobs_here(jobs)
+    _check(getattr(load(), name)(jobs, len(jobs), B, S, D, rot, layout, _ptr(table), rows, pos, size, offset, _ptr(workspace), _room(workspace),
+                                 _here(stream, table, positions, workspace)), name)
+
+
+def rope_quantize(jobs, table, workspace=None, layout=HALF, positions=None, offset=0, stream=None):
+    """QK norm, rotary positions and FP8 cast of the jobs' tensors.  table: [positions, rot] of rope_table; positions: an int32 or int64 row of the table for
+    every token, [B, S], or None for offset + s; workspace: rope_workspace() bytes, where a job has an amax."""
+    _rope("fog_rope_quantize", jobs, table, workspace, layout, positions, offset, stream)
+
+
+def rope_grad(jobs, table, workspace=None, layout=HALF, positions=None, offset=0, stream=None):
+    """The gradients of rope_quantize's tensors from those of its results (table, layout, positions and offset as there)."""
+    _rope("fog_rope_grad", jobs, table, workspace, layout, positions, offset, stream)
+
+
+def rope_workspace():
+    return load().fog_rope_workspace()
 
 
 def xielu_quantize(x, alpha_p, alpha_n, fmt, scale_t, q, amax_out=None, stream=None):

@@ -90,3 +90,117 @@ def test_the_binding_looks_at_types_and_sizes():
     with pytest.raises(ValueError):
         fog.make_adamw_jobs([good, {**good, **codes}])
     assert ctypes.sizeof(fog.AdamwJob) == 80
+
+
+# ---------------------------------------------------------------------------------------------- rotary positions
+def heads(p=P, batch=4096, token=256, head=128):
+    return fog.Heads(p, batch, token, head)
+
+
+def rope_job(heads_n=2, **change):
+    a = dict(x=heads(), q=heads(P + MB), heads=heads_n, rotate=1, gain=1.0, fmt=0, scale=P, amax=P)
+    a.update(change)
+    return fog.RopeJob(**a)
+
+
+def rope_grad_job(heads_n=2, **change):
+    a = dict(dy=heads(), x=heads(P + MB), dx=heads(P + 2 * MB), q=heads(P + 3 * MB), heads=heads_n, rotate=1, gain=1.0, fmt=1, scale=P, amax=P)
+    a.update(change)
+    return fog.RopeGradJob(**a)
+
+
+def rope(lib, jobs, grad=False, B=3, S=16, D=128, rot=128, layout=0, table=P, positions=16, pos=None, pos_bytes=0, offset=0, ws=P, ws_bytes=1 << 16, count=None):
+    arr = ((fog.RopeGradJob if grad else fog.RopeJob) * len(jobs))(*jobs) if jobs is not None else None
+    call = lib.fog_rope_grad if grad else lib.fog_rope_quantize
+    return call(arr, len(jobs) if count is None else count, B, S, D, rot, layout, table, positions, pos, pos_bytes, offset, ws, ws_bytes, None)
+
+
+CALLS = [
+    (SHAPE, dict(count=-1)), (SHAPE, dict(count=9)), (NULL, dict(jobs=None, count=1)), (SHAPE, dict(B=-1)), (SHAPE, dict(S=-1)), (SHAPE, dict(D=-1, rot=-1)),
+    (SHAPE, dict(rot=-2)), (SHAPE, dict(rot=130)), (SHAPE, dict(positions=-1)), (UNSUPPORTED, dict(rot=127)), (UNSUPPORTED, dict(D=1009)),
+    (UNSUPPORTED, dict(layout=2)), (UNSUPPORTED, dict(layout=-1)), (UNSUPPORTED, dict(B=1 << 16, S=1 << 15)), (UNSUPPORTED, dict(pos=P, pos_bytes=2)),
+    (UNSUPPORTED, dict(offset=-(1 << 63))), (ALIGN, dict(table=P + 2)), (ALIGN, dict(pos=P + 4, pos_bytes=8)), (ALIGN, dict(pos=P + 2, pos_bytes=4)),
+    (NULL, dict(table=None)), (WORKSPACE, dict(ws=None)), (WORKSPACE, dict(ws_bytes=(1 << 16) - 1)), (ALIGN, dict(ws=P + 2))]
+
+
+@pytest.mark.parametrize("status,change", CALLS)
+@pytest.mark.parametrize("grad", [False, True])
+def test_rope(lib, grad, status, change):
+    make = rope_grad_job if grad else rope_job
+    assert rope(lib, **{**dict(jobs=[make()]), **change}, grad=grad) == status
+
+
+JOB = [
+    (SHAPE, dict(heads_n=-1)), (UNSUPPORTED, dict(heads_n=(1 << 24) + 1)), (UNSUPPORTED, dict(fmt=2)), (UNSUPPORTED, dict(gain=-1.0)), (UNSUPPORTED, dict(gain=NAN)),
+    (UNSUPPORTED, dict(gain=INF)), (NULL, dict(scale=None)), (ALIGN, dict(scale=P + 1)), (ALIGN, dict(amax=P + 2)), (NULL, dict(x=heads(None))),
+    (ALIGN, dict(x=heads(P + MB + 1))), (SHAPE, dict(x=heads(P + MB, batch=-1))), (UNSUPPORTED, dict(x=heads(P + MB, token=1 << 60)))]
+
+
+@pytest.mark.parametrize("status,change", JOB + [
+    (NULL, dict(q=heads(None))), (SHAPE, dict(q=heads(P + MB, token=-1))),
+    (SHAPE, dict(q=heads(P + MB, head=127))), (SHAPE, dict(q=heads(P + MB, head=0))), (SHAPE, dict(q=heads(P + MB, token=255))),      # vectors of q on each other
+    (SHAPE, dict(q=heads(P + MB, batch=256))), (UNSUPPORTED, dict(q=heads(P)))])
+def test_rope_job(lib, status, change):
+    if "x" in change and change["x"].p == P + MB:
+        change = {**change, "q": heads(P + 4 * MB)}
+    assert rope(lib, [rope_job(**change)]) == status
+
+
+@pytest.mark.parametrize("status,change", JOB + [
+    (NULL, dict(dy=heads(None))), (NULL, dict(dx=heads(None), q=heads(None))), (ALIGN, dict(dx=heads(P + 2 * MB + 1))), (SHAPE, dict(dx=heads(P + 2 * MB, head=64))),
+    (SHAPE, dict(q=heads(P + 3 * MB, head=64))), (UNSUPPORTED, dict(dx=heads(P))), (UNSUPPORTED, dict(dx=heads(P + MB))), (UNSUPPORTED, dict(q=heads(P + 2 * MB)))])
+def test_rope_grad_job(lib, status, change):
+    assert rope(lib, [rope_grad_job(**change)], grad=True) == status
+
+
+def outputs(lib, a, b, **call):
+    """Whether two jobs' codes may lie like this: HIP (there is no device to launch on) or UNSUPPORTED."""
+    (pa, ha), (pb, hb) = a, b
+    return rope(lib, [rope_job(ha, q=pa, amax=None), rope_job(hb, q=pb, amax=None)], **call)
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="would be launched on addresses that are none")
+def test_rope_outputs_that_lie_between_each_other(lib):
+    Q = P + MB
+    row = lambda first, n: (heads(Q + 128 * first, 16 * 1024, 1024, 128), n)  # noqa: E731      eight heads of 128 a token
+    assert outputs(lib, row(0, 4), row(4, 4)) == HIP
+    assert outputs(lib, row(4, 4), row(0, 4)) == HIP
+    assert outputs(lib, row(0, 4), row(3, 4)) == UNSUPPORTED
+    assert outputs(lib, row(0, 8), row(7, 1)) == UNSUPPORTED
+    assert outputs(lib, row(0, 1), row(7, 1)) == HIP
+    assert outputs(lib, row(0, 5), row(7, 1)) == HIP
+    assert outputs(lib, row(0, 5), row(7, 2)) == UNSUPPORTED              # the second head lies in the next token's first
+    assert outputs(lib, row(0, 4), row(4, 4), B=1) == HIP and outputs(lib, row(0, 4), row(4, 4), S=1) == HIP
+    assert outputs(lib, row(0, 4), row(3, 4), B=1, S=1) == UNSUPPORTED
+    kv = lambda i, n: (heads(Q + i * 16 * 1024, 2 * 16 * 1024, 128, 16 * 128), n)  # noqa: E731      [B, 2, 8 heads, 16 tokens, 128]
+    assert outputs(lib, kv(0, 8), kv(1, 8)) == HIP and outputs(lib, kv(1, 8), kv(0, 8)) == HIP
+    assert outputs(lib, kv(0, 8), kv(0, 8)) == UNSUPPORTED
+    assert outputs(lib, kv(0, 8), row(0, 8)) == UNSUPPORTED               # other strides in the same range: not seen to lie apart
+    assert outputs(lib, kv(0, 8), (heads(Q + MB, 4096, 256, 128), 2)) == HIP
+
+
+def table(lib, first=0, positions=10, rot=64, t=P, **scaling):
+    s = dict(base=10000.0, factor=2.0, low=1.0, high=4.0, original=4096.0, amplitude=1.0)
+    s.update(scaling)
+    return lib.fog_rope_table(ctypes.byref(fog.RopeScaling(**s)), first, positions, rot, t, None)
+
+
+@pytest.mark.parametrize("status,change", [
+    (OK, dict(positions=0)), (OK, dict(rot=0, t=None)), (NULL, dict(t=None)), (SHAPE, dict(positions=-1)), (SHAPE, dict(rot=-2)), (ALIGN, dict(t=P + 2)),
+    (UNSUPPORTED, dict(rot=63)), (UNSUPPORTED, dict(positions=(1 << 31) + 1)), (UNSUPPORTED, dict(first=1 << 53)), (UNSUPPORTED, dict(base=0.0)), (UNSUPPORTED, dict(base=INF)),
+    (UNSUPPORTED, dict(factor=0.0)), (UNSUPPORTED, dict(factor=NAN)), (UNSUPPORTED, dict(low=4.0)), (UNSUPPORTED, dict(high=NAN)), (UNSUPPORTED, dict(original=-1.0)),
+    (UNSUPPORTED, dict(original=INF)), (UNSUPPORTED, dict(amplitude=NAN))])
+def test_rope_table(lib, status, change):
+    assert table(lib, **change) == status
+
+
+def test_rope_bindings_look_at_types_and_shapes():
+    x, q, s = torch.zeros((2, 3, 4, 8), dtype=torch.bfloat16), torch.zeros((2, 3, 4, 8), dtype=torch.uint8), torch.ones(1)
+    good = dict(x=x, q=q, scale=s)
+    assert fog.make_rope_jobs([good]).shape == (2, 3, 8)
+    for bad in (dict(x=x.float()), dict(x=x[..., ::2]), dict(q=q[:, :2]), dict(q=q.view(torch.float8_e5m2)), dict(q=None), dict(scale=s.double()), dict(amax=s.half())):
+        with pytest.raises((ValueError, AttributeError)):
+            fog.make_rope_jobs([{**good, **bad}])
+    with pytest.raises(ValueError):
+        fog.make_rope_jobs([good, dict(x=x[:1], q=q[:1], scale=s)])
+    assert ctypes.sizeof(fog.RopeJob) == 96 and ctypes.sizeof(fog.RopeGradJob) == 160
