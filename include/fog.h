@@ -385,6 +385,54 @@ fog_status fog_postnorm_residual_quantize(const void* x_bf16, int64_t ldx, const
                                           int64_t ldo, uint8_t* q, int64_t ldq, float* amax_out, void* stream);
 
 /*
+ * The way back through fog_postnorm_residual_quantize.  The gradient of the stream behind it comes from two sides, from the residual connection and from the next
+ * sub-layer's first product (there is no pre-normalisation), and goes on to two, the stream before it and the sub-layer's result y:
+ *     G  = bf16( dres + dbranch )                 (dbranch NULL: G = dres),   dstream = G, which is also the gradient of the stream before
+ *     dy = bf16( 1 / rms(y) ( gamma G - y (gamma G . y) / (y . y) ) )         (binary32; a row of zeros: 0),   q = sat_rne_fmt( fl32( dy * scale ) )
+ *     dgamma = sum over the rows of G y / rms(y),        amax_out = max |dy|   (dy, q, amax_out: of the rounded value)
+ *   dres_bf16, dbranch_bf16, y_bf16 : [rows, cols] bfloat16, leading dimensions ld_*.   gamma : [cols] floats.   scale : one float; may be NULL without q.
+ *   dstream_bf16, dy_bf16, q : each may be NULL; [rows, cols], leading dimensions.  One may lie in the place of an input of its type (the same address and leading
+ *             dimension); otherwise no result may meet an input or another result.
+ *   dgamma : NULL, or [cols] floats, overwritten (accumulate == 0) or added to.  Sums in a fixed order, the same bits on every run.
+ *   amax_out : NULL or one float, overwritten.
+ *   workspace : fog_postnorm_residual_grad_workspace(rows, cols) bytes, 4-byte aligned, where dgamma or amax_out is given; contents on entry do not matter.  Calls
+ *             that may overlap in time need a workspace each.
+ * Rows of any alignment, up to 32768 columns.  A sum of squares is held in binary32: rows beyond 10^18 lose their norm, as in the forward.
+ * Errors: NULL, SHAPE, ALIGN, WORKSPACE, UNSUPPORTED (format, cols, results that meet an input or each other).
+ */
+fog_status fog_postnorm_residual_grad(const void* dres_bf16, int64_t ld_dres, const void* dbranch_bf16, int64_t ld_dbranch, const void* y_bf16,
+                                      int64_t ldy, int64_t rows, int64_t cols, const float* gamma, fog_fp8 fmt, const float* scale,
+                                      void* dstream_bf16, int64_t ld_dstream, void* dy_bf16, int64_t ld_dy, uint8_t* q, int64_t ldq, float* amax_out,
+                                      float* dgamma, int accumulate, void* workspace, size_t workspace_bytes, void* stream);
+size_t fog_postnorm_residual_grad_workspace(int64_t rows, int64_t cols);
+
+/*
+ * The way back through the activations, x the producer's input, dy the gradient of its result:
+ *     dx = bf16( dy f'(x) )  (binary32),   q = sat_rne_fmt( fl32( dx * scale ) ),   amax_out = max |dx|      (q, amax_out: of the rounded value)
+ *   xIELU:  f' = 2 alpha_p x + 0.5 for x > 0, alpha_n (e^x - 1) + 0.5 for x <= 0;     dalpha = (sum of dy x^2 over x > 0, sum of dy (e^x - 1 - x) over x <= 0)
+ *   GeLU:   f' = Phi(x) + x phi(x), phi the normal density
+ *   tanh:   f' = alpha (1 - tanh^2(alpha x));                                         dalpha = sum of dy x (1 - tanh^2(alpha x))
+ *   x_bf16, dy_bf16 : [rows, cols] bfloat16, leading dimensions.   scale : one float; may be NULL without q.
+ *   dx_bf16, q : either may be NULL; [rows, cols], leading dimensions.  dx may lie in the place of x or dy (the same address and leading dimension); otherwise no
+ *             result may meet an input or the other result.
+ *   dalpha : NULL, or two floats (xIELU) or one (tanh), overwritten (accumulate == 0) or added to; joined in binary64 in a fixed order, the same bits on every run.
+ *   amax_out : NULL or one float, overwritten.
+ *   workspace : fog_act_grad_workspace() bytes (40 KB), 8-byte aligned, where dalpha or amax_out is given; contents on entry do not matter.  Calls that may overlap in
+ *             time need a workspace each.
+ * Rows of any length and alignment.  f' is within 2^-19 of its terms' size (GeLU: and x^2 2^-23, tanh: and |alpha x| 2^-22).
+ * Errors: NULL, SHAPE, ALIGN, WORKSPACE, UNSUPPORTED (format, alpha as in the producers, rows * cols above 2^47, results that meet an input or each other).
+ */
+fog_status fog_xielu_grad(const void* x_bf16, int64_t ldx, const void* dy_bf16, int64_t ld_dy, int64_t rows, int64_t cols, float alpha_p, float alpha_n,
+                          fog_fp8 fmt, const float* scale, void* dx_bf16, int64_t ld_dx, uint8_t* q, int64_t ldq, float* amax_out, float* dalpha,
+                          int accumulate, void* workspace, size_t workspace_bytes, void* stream);
+fog_status fog_gelu_grad(const void* x_bf16, int64_t ldx, const void* dy_bf16, int64_t ld_dy, int64_t rows, int64_t cols, fog_fp8 fmt, const float* scale,
+                         void* dx_bf16, int64_t ld_dx, uint8_t* q, int64_t ldq, float* amax_out, void* workspace, size_t workspace_bytes, void* stream);
+fog_status fog_tanh_grad(const void* x_bf16, int64_t ldx, const void* dy_bf16, int64_t ld_dy, int64_t rows, int64_t cols, float alpha, fog_fp8 fmt,
+                         const float* scale, void* dx_bf16, int64_t ld_dx, uint8_t* q, int64_t ldq, float* amax_out, float* dalpha, int accumulate,
+                         void* workspace, size_t workspace_bytes, void* stream);
+size_t fog_act_grad_workspace(void);
+
+/*
  * Activation kurtosis, the paper's outlier diagnostic (Section 4): for each token vector x (a row),
  * kurt(x) = mu[x^4] / (mu[x^2])^2 (element-wise powers, x not centred); the result is the mean over
  * the rows.  The denominator is read as the squared un-centred second moment (1 for a constant

@@ -1,0 +1,304 @@
+// The way back through the post-norm and its residual connection: the two gradients that meet in the stream are added, the norm's output gradient is
+// taken back to the sub-layer's result and cast for that sub-layer's products, and the gains' gradient is summed over the rows.
+//
+// Bound by memory: 6 bytes read and 3 (5 with dy) written an element.  A row belongs to W waves that keep it in registers between the sums over
+// it and its results, so that every tensor is read once.  A lane keeps its columns over all rows of its wave, so that the gains' gradient is summed in registers;
+// a workgroup's waves join in LDS, the workgroups' sums in a second launch, in a fixed order: the same bits on every run.
+#include <cfloat>
+
+#include "common.h"
+#include "launch.h"
+#include "layout.h"
+
+namespace {
+
+constexpr int kThreads = 512;
+constexpr int WAVES = kThreads / 64;
+constexpr int GROUPS = 256;              // most workgroups: one row of sums and one abs-max each in the workspace
+constexpr int COLS_MAX = 512 * 8 * WAVES;
+
+// Whether a workgroup's sets of W waves join their sums; one or two sets, whose sums would fill LDS, leave them side by side.
+__host__ __device__ constexpr bool joins(int W) { return W <= 2; }
+
+struct Args {
+  const uint16_t *dres, *dbranch, *y;
+  const float *gamma, *scale;
+  uint16_t *dstream, *dy;
+  uint8_t* q;
+  float* sums;             // [workgroups, or their sets of waves][cols], or NULL
+  uint32_t* tops;          // [workgroups], or NULL
+  int64_t ld_dres, ld_dbranch, ldy, ld_dstream, ld_dy, ldq, rows;
+  int cols;
+};
+
+FOG_DEVICE void unpack8(uint4 v, float (&f)[8]) {
+  f[0] = bf16lo(v.x); f[1] = bf16hi(v.x); f[2] = bf16lo(v.y); f[3] = bf16hi(v.y);
+  f[4] = bf16lo(v.z); f[5] = bf16hi(v.z); f[6] = bf16lo(v.w); f[7] = bf16hi(v.w);
+}
+FOG_DEVICE uint4 pack8(const float (&f)[8]) {
+  return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
+}
+FOG_DEVICE uint4 fetch(const uint16_t* p, int n) { return n >= 8 ? ld_any_nt16(p) : ld_upto8(p, n); }
+FOG_DEVICE void put(uint16_t* p, uint4 w, int n) {
+  if (n >= 8) st_any_nt16(p, w);
+  else st_upto8(p, w, n);
+}
+typedef u32x2 __attribute__((aligned(1))) u32x2_byte;
+FOG_DEVICE void put_codes(uint8_t* p, uint2 w, int n) {
+  if (n >= 8) {
+    u32x2 v = {w.x, w.y};
+    *reinterpret_cast<u32x2_byte*>(p) = v;
+  } else {
+    st_upto8(p, w, n);
+  }
+}
+FOG_DEVICE void gains8(const float* p, int n, float (&g)[8]) {
+  if (n >= 8) {
+    const uint4 a = ld_any16(p), b = ld_any16(p + 4);
+    g[0] = __uint_as_float(a.x); g[1] = __uint_as_float(a.y); g[2] = __uint_as_float(a.z); g[3] = __uint_as_float(a.w);
+    g[4] = __uint_as_float(b.x); g[5] = __uint_as_float(b.y); g[6] = __uint_as_float(b.z); g[7] = __uint_as_float(b.w);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) g[k] = k < n ? p[k] : 0.0f;
+  }
+}
+
+template <int FMT, int W, int C>
+__global__ __launch_bounds__(kThreads) void postnorm_grad_kernel(Args a) {
+  constexpr int ROWS = WAVES / W;           // rows of a workgroup at a time
+  constexpr bool JOINED = joins(W);
+  __shared__ float joined[JOINED ? 512 * C * W : 1];
+  __shared__ float part[2][WAVES][2];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, w = wave % W;
+  const float rho = a.q ? *a.scale : 0.0f;
+  const float cols = (float)a.cols;
+  float sum[C][8];
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum[c][k] = 0.0f;
+  uint32_t top = 0u;
+  int turn = 0;
+  for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < a.rows; r0 += (int64_t)gridDim.x * ROWS, turn ^= 1) {
+    const int64_t r = r0 + wave / W;
+    const bool there = r < a.rows;
+    uint4 y[C], G[C];
+    float yy = 0.0f, ty = 0.0f;
+    if (there) {
+      uint4 b[C];
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const int col = 8 * (64 * (c * W + w) + lane), n = a.cols - col;
+        y[c] = G[c] = b[c] = make_uint4(0, 0, 0, 0);
+        if (n > 0) {
+          y[c] = fetch(a.y + r * a.ldy + col, n);
+          G[c] = fetch(a.dres + r * a.ld_dres + col, n);
+          if (a.dbranch) b[c] = fetch(a.dbranch + r * a.ld_dbranch + col, n);
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const int col = 8 * (64 * (c * W + w) + lane), n = a.cols - col;
+        if (n <= 0) continue;
+        if (a.dbranch) {
+          float f[8], h[8];
+          unpack8(G[c], f);
+          unpack8(b[c], h);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) f[k] += h[k];
+          G[c] = pack8(f);
+        }
+        if (a.dstream) put(a.dstream + r * a.ld_dstream + col, G[c], n);
+        float f[8], h[8], g[8];
+        unpack8(G[c], f);
+        unpack8(y[c], h);
+        gains8(a.gamma + col, n, g);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          yy = __builtin_fmaf(h[k], h[k], yy);
+          ty = __builtin_fmaf(f[k] * g[k], h[k], ty);
+        }
+      }
+    }
+    yy = wave_sum_f32(yy);
+    ty = wave_sum_f32(ty);
+    if (W > 1) {
+      // two sets of words in turn: a wave that is a row ahead writes the other one
+      if (lane == 0) { part[turn][wave][0] = yy; part[turn][wave][1] = ty; }
+      __syncthreads();
+      yy = ty = 0.0f;
+#pragma unroll
+      for (int i = 0; i < W; ++i) { yy += part[turn][wave - w + i][0]; ty += part[turn][wave - w + i][1]; }
+    }
+    if (!there) continue;
+    // 1 / rms, correctly rounded square root and divisions; a row of zeros gets no gradient
+    const float inv = yy != 0.0f ? 1.0f / __builtin_sqrtf(yy / cols) : 0.0f, along = yy != 0.0f ? ty / yy : 0.0f;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int col = 8 * (64 * (c * W + w) + lane), n = a.cols - col;
+      if (n <= 0) continue;
+      float f[8], h[8], g[8];
+      unpack8(G[c], f);
+      unpack8(y[c], h);
+      gains8(a.gamma + col, n, g);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        sum[c][k] = __builtin_fmaf(f[k], h[k] * inv, sum[c][k]);
+        f[k] = inv * __builtin_fmaf(-h[k], along, f[k] * g[k]);
+      }
+      const uint4 o = pack8(f);
+      top = pkmax_abs_bf16(top, o.x); top = pkmax_abs_bf16(top, o.y); top = pkmax_abs_bf16(top, o.z); top = pkmax_abs_bf16(top, o.w);
+      if (a.dy) put(a.dy + r * a.ld_dy + col, o, n);
+      if (a.q) {
+        unpack8(o, f);
+        put_codes(a.q + r * a.ldq + col, make_uint2(cvt4_fp8_nan<FMT>(f[0] * rho, f[1] * rho, f[2] * rho, f[3] * rho),
+                                                    cvt4_fp8_nan<FMT>(f[4] * rho, f[5] * rho, f[6] * rho, f[7] * rho)), n);
+      }
+    }
+  }
+  if (a.sums && !JOINED) {
+    float* out = a.sums + ((int64_t)blockIdx.x * ROWS + wave / W) * a.cols;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int col = 8 * (64 * (c * W + w) + lane);
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (col + k < a.cols) out[col + k] = sum[c][k];
+    }
+  } else if (a.sums) {
+    // the rows' sums, one wave (of each set of W) after the other
+    for (int i = 0; i < ROWS; ++i) {
+      if (wave / W == i) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          const int col = 8 * (64 * (c * W + w) + lane);
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            if (col + k < a.cols) joined[col + k] = i == 0 ? sum[c][k] : joined[col + k] + sum[c][k];
+        }
+      }
+      __syncthreads();
+    }
+    float* out = a.sums + (int64_t)blockIdx.x * a.cols;
+    for (int i = threadIdx.x; i < a.cols; i += kThreads) out[i] = joined[i];
+  }
+  if (a.tops) {
+    __shared__ uint32_t tops[WAVES];
+    const uint32_t m = wave_max_u32(max_of_pair(top));
+    if (lane == 0) tops[wave] = m;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      uint32_t t = tops[0];
+#pragma unroll
+      for (int i = 1; i < WAVES; ++i) t = t > tops[i] ? t : tops[i];
+      a.tops[blockIdx.x] = t << 16;      // the float with that bf16 pattern
+    }
+  }
+}
+
+// The gains' gradient from the workgroups' sums: 32 columns a workgroup, 32 threads for each, each with every 32nd sum.
+constexpr int kJoinThreads = 1024;
+__global__ __launch_bounds__(kJoinThreads) void postnorm_grad_join_kernel(const float* __restrict__ sums, const uint32_t* __restrict__ tops, int rows, int groups, int cols,
+                                                                          float* __restrict__ dgamma, int accumulate, uint32_t* __restrict__ amax) {
+  __shared__ float part[32][33];
+  const int x = threadIdx.x & 31, z = threadIdx.x >> 5, col = (int)blockIdx.x * 32 + x;
+  if (dgamma) {
+    float s = 0.0f;
+    if (col < cols)
+      for (int i = z; i < rows; i += 32) s += sums[(int64_t)i * cols + col];
+    part[z][x] = s;
+    __syncthreads();
+    if (z == 0 && col < cols) {
+      float t = accumulate ? dgamma[col] : 0.0f;
+      float u = 0.0f;
+      for (int i = 0; i < 32; ++i) u += part[i][x];
+      dgamma[col] = t + u;
+    }
+  }
+  if (amax && blockIdx.x == 0 && threadIdx.x < 64) {
+    uint32_t m = 0u;
+    for (int i = threadIdx.x; i < groups; i += 64) m = m > tops[i] ? m : tops[i];
+    m = wave_max_u32(m);
+    if (threadIdx.x == 0) *amax = m;
+  }
+}
+
+template <int FMT, int W, int C>
+void launch(const Args& a, int groups, hipStream_t s) {
+  postnorm_grad_kernel<FMT, W, C><<<groups, kThreads, 0, s>>>(a);
+}
+
+// Waves of a row: one up to 4096 columns.
+int waves_of(int64_t cols) { return cols <= 4096 ? 1 : cols <= 8192 ? 2 : cols <= 16384 ? 4 : 8; }
+int groups_of(int64_t rows, int64_t cols) {
+  const int64_t n = WAVES / waves_of(cols), g = (rows + n - 1) / n;
+  return (int)(g < GROUPS ? g : GROUPS);
+}
+// Rows of sums in the workspace.
+int sums_of(int64_t rows, int64_t cols) {
+  const int W = waves_of(cols);
+  return groups_of(rows, cols) * (joins(W) ? 1 : WAVES / W);
+}
+
+}  // namespace
+
+extern "C" size_t fog_postnorm_residual_grad_workspace(int64_t rows, int64_t cols) {
+  if (rows <= 0 || cols <= 0 || cols > COLS_MAX) return 0;
+  return (size_t)sums_of(rows, cols) * (size_t)cols * sizeof(float) + (size_t)groups_of(rows, cols) * sizeof(uint32_t);
+}
+
+extern "C" fog_status fog_postnorm_residual_grad(const void* dres_bf16, int64_t ld_dres, const void* dbranch_bf16, int64_t ld_dbranch, const void* y_bf16,
+                                                 int64_t ldy, int64_t rows, int64_t cols, const float* gamma, fog_fp8 fmt, const float* scale,
+                                                 void* dstream_bf16, int64_t ld_dstream, void* dy_bf16, int64_t ld_dy, uint8_t* q, int64_t ldq, float* amax_out,
+                                                 float* dgamma, int accumulate, void* workspace, size_t workspace_bytes, void* stream) {
+  if (rows < 0 || cols < 0) return FOG_ERR_SHAPE;
+  if (fmt != FOG_E4M3 && fmt != FOG_E5M2) return FOG_ERR_UNSUPPORTED;
+  if (cols > COLS_MAX) return FOG_ERR_UNSUPPORTED;
+  if (q && !scale) return FOG_ERR_NULL;
+  if ((reinterpret_cast<uintptr_t>(gamma) | reinterpret_cast<uintptr_t>(scale) | reinterpret_cast<uintptr_t>(amax_out) | reinterpret_cast<uintptr_t>(dgamma)) & 3)
+    return FOG_ERR_ALIGN;
+  hipStream_t s = (hipStream_t)stream;
+  Args a = {};
+  int groups = 0;
+  if (rows > 0 && cols > 0) {
+    if (!dres_bf16 || !y_bf16 || !gamma) return FOG_ERR_NULL;
+    FogMatrices m;
+    fog_status st = m.add(dres_bf16, rows, cols, ld_dres, 2, false);
+    if (st == FOG_OK) st = m.add(dbranch_bf16, rows, cols, ld_dbranch, 2, false);
+    if (st == FOG_OK) st = m.add(y_bf16, rows, cols, ldy, 2, false);
+    if (st == FOG_OK) st = m.add(gamma, 1, cols, cols, 4, false);
+    if (st == FOG_OK) st = m.add(dstream_bf16, rows, cols, ld_dstream, 2, true);
+    if (st == FOG_OK) st = m.add(dy_bf16, rows, cols, ld_dy, 2, true);
+    if (st == FOG_OK) st = m.add(q, rows, cols, ldq, 1, true);
+    if (st == FOG_OK) st = m.add(dgamma, 1, cols, cols, 4, true);
+    if (st != FOG_OK) return st;
+    if (!m.fine()) return FOG_ERR_UNSUPPORTED;
+    groups = groups_of(rows, cols);
+    if (dgamma || amax_out) {
+      if (!workspace || workspace_bytes < fog_postnorm_residual_grad_workspace(rows, cols)) return FOG_ERR_WORKSPACE;
+      if (reinterpret_cast<uintptr_t>(workspace) & 3) return FOG_ERR_ALIGN;
+    }
+    float* sums = reinterpret_cast<float*>(workspace);
+    a.dres = reinterpret_cast<const uint16_t*>(dres_bf16); a.dbranch = reinterpret_cast<const uint16_t*>(dbranch_bf16); a.y = reinterpret_cast<const uint16_t*>(y_bf16);
+    a.gamma = gamma; a.scale = scale; a.dstream = reinterpret_cast<uint16_t*>(dstream_bf16); a.dy = reinterpret_cast<uint16_t*>(dy_bf16); a.q = q;
+    a.sums = dgamma ? sums : nullptr;
+    a.tops = amax_out ? reinterpret_cast<uint32_t*>(sums + (int64_t)sums_of(rows, cols) * cols) : nullptr;
+    a.ld_dres = ld_dres; a.ld_dbranch = ld_dbranch; a.ldy = ldy; a.ld_dstream = ld_dstream; a.ld_dy = ld_dy; a.ldq = ldq; a.rows = rows; a.cols = (int)cols;
+#define FOG_PNG(W, C) (fmt == FOG_E4M3 ? launch<FOG_E4M3, W, C>(a, groups, s) : launch<FOG_E5M2, W, C>(a, groups, s))
+    if (cols <= 512) FOG_PNG(1, 1);
+    else if (cols <= 1024) FOG_PNG(1, 2);
+    else if (cols <= 2048) FOG_PNG(1, 4);
+    else if (cols <= 4096) FOG_PNG(1, 8);
+    else if (cols <= 8192) FOG_PNG(2, 8);
+    else if (cols <= 16384) FOG_PNG(4, 8);
+    else FOG_PNG(8, 8);
+#undef FOG_PNG
+  } else if ((!dgamma || accumulate || cols == 0) && !amax_out) {
+    return FOG_OK;
+  }
+  if ((dgamma && cols > 0) || amax_out) {
+    const int64_t blocks = dgamma && cols > 0 ? (cols + 31) / 32 : 1;
+    postnorm_grad_join_kernel<<<(int)blocks, kJoinThreads, 0, s>>>(a.sums, a.tops, groups ? sums_of(rows, cols) : 0, groups, (int)cols, cols > 0 ? dgamma : nullptr, accumulate, reinterpret_cast<uint32_t*>(amax_out));
+  }
+  return fog_launch_status();
+}

@@ -11,6 +11,7 @@
 
 #include "common.h"
 #include "launch.h"
+#include "layout.h"
 
 namespace {
 
@@ -323,72 +324,28 @@ __global__ __launch_bounds__(kThreads) void rope_table_kernel(fog_rope_scaling s
 }
 
 // ---------------------------------------------------------------- host
-// Where [B, S, heads] vectors of `row` bytes lie: bytes between neighbours, largest first, of the dimensions that have more than one.
-struct Box {
-  uintptr_t base;
-  int dims;
-  int64_t n[3], stride[3], row;
-  int64_t extent(int from) const {
-    int64_t e = row;
-    for (int i = from; i < dims; ++i) e += (n[i] - 1) * stride[i];
-    return e;
-  }
-};
-fog_status make_box(const fog_heads& h, int B, int S, int heads, int D, int size, Box* box) {
-  if (!h.p) return FOG_ERR_NULL;
+// Where [B, S, heads] vectors of D elements lie.
+fog_status make_box(const fog_heads& h, int B, int S, int heads, int D, int size, FogBox* box) {
   const int64_t n[3] = {B, S, heads}, stride[3] = {h.batch, h.token, h.head};
-  box->base = reinterpret_cast<uintptr_t>(h.p);
-  if (box->base & (size - 1)) return FOG_ERR_ALIGN;
-  box->dims = 0;
-  box->row = (int64_t)D * size;
-  for (int i = 0; i < 3; ++i) {
-    if (n[i] <= 1) continue;
-    if (stride[i] < 0) return FOG_ERR_SHAPE;
-    if ((double)(n[i] - 1) * (double)stride[i] * size > 140737488355328.0) return FOG_ERR_UNSUPPORTED;      // 2^47 bytes: more than an address space holds
-    int at = box->dims++;
-    for (; at > 0 && box->stride[at - 1] < stride[i] * size; --at) {
-      box->n[at] = box->n[at - 1];
-      box->stride[at] = box->stride[at - 1];
-    }
-    box->n[at] = n[i];
-    box->stride[at] = stride[i] * size;
-  }
-  return FOG_OK;
-}
-// Whether no vector of a box lies on another of it.
-bool injective(const Box& a) {
-  for (int i = 0; i < a.dims; ++i)
-    if (a.stride[i] < a.extent(i + 1)) return false;
-  return true;
-}
-// Whether two boxes are seen to lie apart, b's first vector `off` bytes behind a's: one ends before the other begins, or both step by the same
-// distance and lie apart within a step.  (A step of a has two neighbours of b: the one at `off` modulo the distance and the one before.)
-bool apart(const Box& a, int ia, const Box& b, int ib, int64_t off) {
-  if (off >= a.extent(ia) || -off >= b.extent(ib)) return true;
-  if (ia >= a.dims || ib >= b.dims || a.stride[ia] != b.stride[ib] || a.stride[ia] <= 0) return false;
-  const int64_t s = a.stride[ia], r = ((off % s) + s) % s;
-  return apart(a, ia + 1, b, ib + 1, r) && apart(a, ia + 1, b, ib + 1, r - s);
-}
-bool apart_as_spans(const Box& a, const Box& b) {
-  return a.base + (uintptr_t)a.extent(0) <= b.base || b.base + (uintptr_t)b.extent(0) <= a.base;
+  return fog_make_box(h.p, 3, n, stride, D, size, box);
 }
 
 struct Call {
-  Box in[2 * JOBS], out[2 * JOBS];
+  FogBox in[2 * JOBS], out[2 * JOBS];
   int ins = 0, outs = 0;
   fog_status add(const fog_heads& h, int B, int S, int heads, int D, int size, bool written) {
     const fog_status st = make_box(h, B, S, heads, D, size, written ? &out[outs] : &in[ins]);
     if (st != FOG_OK) return st;
-    if (written && !injective(out[outs])) return FOG_ERR_SHAPE;
+    if (written && !fog_injective(out[outs])) return FOG_ERR_SHAPE;
     ++(written ? outs : ins);
     return FOG_OK;
   }
   bool fine() const {
     for (int i = 0; i < outs; ++i) {
       for (int k = 0; k < ins; ++k)
-        if (!apart_as_spans(out[i], in[k])) return false;
+        if (!fog_apart_as_spans(out[i], in[k])) return false;
       for (int k = 0; k < i; ++k)
-        if (!apart(out[k], 0, out[i], 0, (int64_t)(out[i].base - out[k].base))) return false;
+        if (!fog_apart(out[k], out[i])) return false;
     }
     return true;
   }

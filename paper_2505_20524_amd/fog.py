@@ -49,6 +49,12 @@ SIGNATURES = {
     "fog_gelu_quantize": (_I, [_P, _I64, _I64, _I64, _I, _P, _P, _I64, _P, _P]),
     "fog_tanh_quantize": (_I, [_P, _I64, _I64, _I64, _F, _I, _P, _P, _I64, _P, _P]),
     "fog_postnorm_residual_quantize": (_I, [_P, _I64, _P, _I64, _I64, _I64, _P, _I, _P, _P, _I64, _P, _I64, _P, _P]),
+    "fog_postnorm_residual_grad": (_I, [_P, _I64, _P, _I64, _P, _I64, _I64, _I64, _P, _I, _P, _P, _I64, _P, _I64, _P, _I64, _P, _P, _I, _P, _SZ, _P]),
+    "fog_postnorm_residual_grad_workspace": (_SZ, [_I64, _I64]),
+    "fog_xielu_grad": (_I, [_P, _I64, _P, _I64, _I64, _I64, _F, _F, _I, _P, _P, _I64, _P, _I64, _P, _P, _I, _P, _SZ, _P]),
+    "fog_gelu_grad": (_I, [_P, _I64, _P, _I64, _I64, _I64, _I, _P, _P, _I64, _P, _I64, _P, _P, _SZ, _P]),
+    "fog_tanh_grad": (_I, [_P, _I64, _P, _I64, _I64, _I64, _F, _I, _P, _P, _I64, _P, _I64, _P, _P, _I, _P, _SZ, _P]),
+    "fog_act_grad_workspace": (_SZ, []),
     "fog_kurtosis": (_I, [_P, _I64, _I64, _I64, _P, _P, _P]),
     "fog_fp8_gemm": (_I, [_I, _I64, _I64, _I64, _P, _I, _I64, _P, _P, _I, _I64, _P, _P, _I64, _P, _SZ, _P]),
     "fog_fp8_gemm_workspace": (_SZ, [_I, _I64, _I64, _I64]),
@@ -563,6 +569,65 @@ def grad_clip(jobs, sumsq, max_norm, norm=None, stream=None):
     _floats(norm, "norm")
     _jobs_here(jobs)
     _check(load().fog_grad_clip(jobs, len(jobs), _ptr(sumsq), max_norm, _ptr(norm), _here(stream, sumsq, norm)), "fog_grad_clip")
+
+
+def _vector(t, what, n):
+    """A contiguous vector of n floats, or None."""
+    if t is not None and (t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous()):
+        raise ValueError("%s: %d contiguous float32 numbers are needed, got %s of %s with strides %s" % (what, n, tuple(t.shape), t.dtype, t.stride()))
+    return _ptr(t)
+
+
+def _some(t, what, rows, cols, types):
+    """Pointer and leading dimension of a matrix that may be missing."""
+    return (None, 0) if t is None else (t.data_ptr(), _matrix(t, what, rows, cols, types))
+
+
+def postnorm_residual_grad(dres, y, gamma, fmt, scale_t, dgamma, workspace, dbranch=None, dstream=None, dy=None, q=None, amax_out=None, accumulate=False, stream=None):
+    """The way back through postnorm_residual_quantize: dstream = dres + dbranch, the gradient dy of y and / or its codes q, their abs-max, and the gains' gradient dgamma
+    (None for none; accumulate: added to)."""
+    rows, cols = y.shape
+    _floats(scale_t, "scale_t")
+    _floats(amax_out, "amax_out")
+    where = _here(stream, dres, y, gamma, scale_t, dgamma, workspace, dbranch, dstream, dy, q, amax_out)
+    _check(load().fog_postnorm_residual_grad(*_some(dres, "dres", rows, cols, _HALVES), *_some(dbranch, "dbranch", rows, cols, _HALVES), *_some(y, "y", rows, cols, _HALVES),
+                                             rows, cols, _vector(gamma, "gamma", cols), fmt, _ptr(scale_t), *_some(dstream, "dstream", rows, cols, _HALVES),
+                                             *_some(dy, "dy", rows, cols, _HALVES), *_some(q, "q", rows, cols, _codes(fmt)), _ptr(amax_out),
+                                             _vector(dgamma, "dgamma", cols), int(accumulate), _ptr(workspace), _room(workspace), where), "fog_postnorm_residual_grad")
+
+
+def postnorm_residual_grad_workspace(rows, cols):
+    return load().fog_postnorm_residual_grad_workspace(rows, cols)
+
+
+def _act_grad(name, x, dy, alpha, params, fmt, scale_t, workspace, dx, q, amax_out, dalpha, accumulate, stream):
+    rows, cols = x.shape
+    _floats(scale_t, "scale_t")
+    _floats(amax_out, "amax_out")
+    where = _here(stream, x, dy, scale_t, workspace, dx, q, amax_out, dalpha)
+    own = (_vector(dalpha, "dalpha", params), int(accumulate)) if params else ()
+    _check(getattr(load(), name)(*_some(x, "x", rows, cols, _HALVES), *_some(dy, "dy", rows, cols, _HALVES), rows, cols, *alpha, fmt, _ptr(scale_t),
+                                 *_some(dx, "dx", rows, cols, _HALVES), *_some(q, "q", rows, cols, _codes(fmt)), _ptr(amax_out), *own, _ptr(workspace), _room(workspace),
+                                 where), name)
+
+
+def xielu_grad(x, dy, alpha_p, alpha_n, fmt, scale_t, workspace, dx=None, q=None, amax_out=None, dalpha=None, accumulate=False, stream=None):
+    """The way back through xielu_quantize: dx and / or its codes q, their abs-max, and dalpha, two floats for alpha_p and alpha_n (accumulate: added to)."""
+    _act_grad("fog_xielu_grad", x, dy, (alpha_p, alpha_n), 2, fmt, scale_t, workspace, dx, q, amax_out, dalpha, accumulate, stream)
+
+
+def gelu_grad(x, dy, fmt, scale_t, workspace, dx=None, q=None, amax_out=None, stream=None):
+    """The way back through gelu_quantize: dx and / or its codes q, and their abs-max."""
+    _act_grad("fog_gelu_grad", x, dy, (), 0, fmt, scale_t, workspace, dx, q, amax_out, None, False, stream)
+
+
+def tanh_grad(x, dy, alpha, fmt, scale_t, workspace, dx=None, q=None, amax_out=None, dalpha=None, accumulate=False, stream=None):
+    """The way back through tanh_quantize: dx and / or its codes q, their abs-max, and dalpha, one float (accumulate: added to)."""
+    _act_grad("fog_tanh_grad", x, dy, (alpha,), 1, fmt, scale_t, workspace, dx, q, amax_out, dalpha, accumulate, stream)
+
+
+def act_grad_workspace():
+    return load().fog_act_grad_workspace()
 
 
 class AdamwJob(ctypes.Structure):

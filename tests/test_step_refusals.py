@@ -204,3 +204,75 @@ def test_rope_bindings_look_at_types_and_shapes():
     with pytest.raises(ValueError):
         fog.make_rope_jobs([good, dict(x=x[:1], q=q[:1], scale=s)])
     assert ctypes.sizeof(fog.RopeJob) == 96 and ctypes.sizeof(fog.RopeGradJob) == 160
+
+
+# ---------------------------------------------------------------------------------------------- gradients of post-norm and activations
+def norm_grad(lib, dres=P, ld_dres=64, dbranch=P + MB, ld_dbranch=64, y=P + 2 * MB, ldy=64, rows=4, cols=64, gamma=P + 3 * MB, fmt=1, scale=P + 4 * MB, dstream=P + 5 * MB,
+              ld_dstream=64, dy=P + 6 * MB, ld_dy=64, q=P + 7 * MB, ldq=64, amax=P, dgamma=P + 8 * MB, accumulate=0, ws=P, ws_bytes=1 << 30):
+    return lib.fog_postnorm_residual_grad(dres, ld_dres, dbranch, ld_dbranch, y, ldy, rows, cols, gamma, fmt, scale, dstream, ld_dstream, dy, ld_dy, q, ldq, amax,
+                                          dgamma, accumulate, ws, ws_bytes, None)
+
+
+NORM = [
+    (OK, dict(rows=0, amax=None, dgamma=None)), (OK, dict(rows=0, amax=None, accumulate=1)), (OK, dict(cols=0, amax=None)),
+    (NULL, dict(dres=None)), (NULL, dict(y=None)), (NULL, dict(gamma=None)), (NULL, dict(scale=None)), (SHAPE, dict(rows=-1)), (SHAPE, dict(cols=-1)),
+    (SHAPE, dict(ld_dres=63)), (SHAPE, dict(ld_dbranch=63)), (SHAPE, dict(ldy=63)), (SHAPE, dict(ld_dstream=63)), (SHAPE, dict(ld_dy=63)), (SHAPE, dict(ldq=63)),
+    (ALIGN, dict(dres=P + 1)), (ALIGN, dict(dbranch=P + MB + 1)), (ALIGN, dict(y=P + 2 * MB + 1)), (ALIGN, dict(dstream=P + 5 * MB + 1)), (ALIGN, dict(dy=P + 6 * MB + 1)),
+    (ALIGN, dict(gamma=P + 3 * MB + 2)), (ALIGN, dict(dgamma=P + 8 * MB + 2)), (ALIGN, dict(amax=P + 1)), (ALIGN, dict(scale=P + 1)), (ALIGN, dict(ws=P + 2)),
+    (WORKSPACE, dict(ws=None)), (WORKSPACE, dict(ws_bytes=64 * 4 + 3)), (UNSUPPORTED, dict(fmt=2)), (UNSUPPORTED, dict(cols=32769)),
+    (UNSUPPORTED, dict(ldy=1 << 60)),
+    # results on inputs and on each other
+    (UNSUPPORTED, dict(dstream=P + 2)), (UNSUPPORTED, dict(dy=P + 5 * MB)), (UNSUPPORTED, dict(q=P + 6 * MB + 100)), (UNSUPPORTED, dict(dgamma=P + 7 * MB)),
+    (UNSUPPORTED, dict(dstream=P, ld_dstream=80)), (UNSUPPORTED, dict(dy=P, dstream=P)), (UNSUPPORTED, dict(q=P)), (UNSUPPORTED, dict(dy=P + 3 * MB - 4)),
+    (UNSUPPORTED, dict(dstream=P + 64, ld_dres=96, ld_dstream=96))]
+
+
+@pytest.mark.parametrize("status,change", NORM)
+def test_postnorm_grad(lib, status, change):
+    assert norm_grad(lib, **change) == status
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="would be launched on addresses that are none")
+@pytest.mark.parametrize("change", [
+    {}, dict(dstream=P), dict(dstream=P + MB), dict(dy=P + 2 * MB), dict(dy=P), dict(dbranch=P), dict(dbranch=None, dstream=None), dict(q=None, scale=None),
+    dict(amax=None, dgamma=None, ws=None), dict(dstream=P + 2 * 64, ld_dres=128, ld_dstream=128)])      # the last: the columns beside
+def test_postnorm_grad_takes(lib, change):
+    assert norm_grad(lib, **change) == HIP
+
+
+def test_postnorm_grad_workspace(lib):
+    size = lib.fog_postnorm_residual_grad_workspace
+    assert size(0, 64) == 0 and size(4, 0) == 0 and size(4, 32769) == 0 and size(-1, -1) == 0
+    assert size(1, 64) == 64 * 4 + 4 and size(8, 64) == size(1, 64) and size(9, 64) == 2 * size(1, 64) and size(1 << 40, 64) == 256 * size(1, 64)
+    assert size(1 << 40, 4096) == 256 * (4 * 4096 + 4) and size(1 << 40, 16384) == 256 * (2 * 4 * 16384 + 4) and size(1 << 40, 32768) == 256 * (4 * 32768 + 4)
+
+
+def act_grad(lib, which, x=P, ldx=64, dy=P + MB, ld_dy=64, rows=4, cols=64, alpha=(0.8, 0.6), fmt=1, scale=P + 2 * MB, dx=P + 3 * MB, ld_dx=64, q=P + 4 * MB, ldq=64,
+             amax=P, dalpha=P, accumulate=0, ws=P, ws_bytes=1 << 20):
+    own = () if which == "gelu" else (dalpha, accumulate)
+    params = {"xielu": alpha, "tanh": alpha[:1], "gelu": ()}[which]
+    return getattr(lib, "fog_%s_grad" % which)(x, ldx, dy, ld_dy, rows, cols, *params, fmt, scale, dx, ld_dx, q, ldq, amax, *own, ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("which", ["xielu", "gelu", "tanh"])
+@pytest.mark.parametrize("status,change", [
+    (OK, dict(rows=0, amax=None, dalpha=None)), (OK, dict(cols=0, amax=None, accumulate=1)),
+    (NULL, dict(x=None)), (NULL, dict(dy=None)), (NULL, dict(scale=None)), (SHAPE, dict(rows=-1)), (SHAPE, dict(cols=-1)), (SHAPE, dict(ldx=63)), (SHAPE, dict(ld_dy=63)),
+    (SHAPE, dict(ld_dx=63)), (SHAPE, dict(ldq=63)), (ALIGN, dict(x=P + 1)), (ALIGN, dict(dy=P + MB + 1)), (ALIGN, dict(dx=P + 3 * MB + 1)), (ALIGN, dict(amax=P + 2)),
+    (ALIGN, dict(scale=P + 2)), (ALIGN, dict(ws=P + 4)), (WORKSPACE, dict(ws=None)), (WORKSPACE, dict(ws_bytes=2048 * 20 - 1)), (UNSUPPORTED, dict(fmt=3)),
+    (UNSUPPORTED, dict(rows=1 << 40, cols=1 << 20, ldx=1 << 20, ld_dy=1 << 20, ld_dx=1 << 20, ldq=1 << 20)),
+    (UNSUPPORTED, dict(dx=P + 2)), (UNSUPPORTED, dict(q=P)), (UNSUPPORTED, dict(q=P + 3 * MB + 4)), (UNSUPPORTED, dict(dx=P, ld_dx=80))])
+def test_act_grad(lib, which, status, change):
+    assert act_grad(lib, which, **change) == status
+
+
+@pytest.mark.parametrize("which,alpha", [("xielu", (-0.1, 0.0)), ("xielu", (0.0, -1.0)), ("xielu", (NAN, 0.0)), ("xielu", (0.0, INF)), ("tanh", (NAN,)), ("tanh", (INF,))])
+def test_act_grad_parameters(lib, which, alpha):
+    assert act_grad(lib, which, alpha=alpha) == UNSUPPORTED
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="would be launched on addresses that are none")
+@pytest.mark.parametrize("which", ["xielu", "gelu", "tanh"])
+def test_act_grad_takes(lib, which):
+    for change in ({}, dict(dx=P), dict(dx=P + MB), dict(dx=None), dict(q=None, scale=None), dict(amax=None, dalpha=None, ws=None), dict(x=P + MB)):
+        assert act_grad(lib, which, **change) == HIP
