@@ -14,18 +14,15 @@ namespace {
 
 constexpr int kThreads = 512;
 constexpr int WAVES = kThreads / 64;
-constexpr int GROUPS = 256;              // most workgroups: one row of sums and one abs-max each in the workspace
+constexpr int GROUPS = 512;              // most workgroups, two a CU: one row of sums and one abs-max each in the workspace
 constexpr int COLS_MAX = 512 * 8 * WAVES;
-
-// Whether a workgroup's sets of W waves join their sums; one or two sets, whose sums would fill LDS, leave them side by side.
-__host__ __device__ constexpr bool joins(int W) { return W <= 2; }
 
 struct Args {
   const uint16_t *dres, *dbranch, *y;
   const float *gamma, *scale;
   uint16_t *dstream, *dy;
   uint8_t* q;
-  float* sums;             // [workgroups, or their sets of waves][cols], or NULL
+  float* sums;             // [workgroups][cols], or NULL
   uint32_t* tops;          // [workgroups], or NULL
   int64_t ld_dres, ld_dbranch, ldy, ld_dstream, ld_dy, ldq, rows;
   int cols;
@@ -66,8 +63,8 @@ FOG_DEVICE void gains8(const float* p, int n, float (&g)[8]) {
 template <int FMT, int W, int C>
 __global__ __launch_bounds__(kThreads) void postnorm_grad_kernel(Args a) {
   constexpr int ROWS = WAVES / W;           // rows of a workgroup at a time
-  constexpr bool JOINED = joins(W);
-  __shared__ float joined[JOINED ? 512 * C * W : 1];
+  constexpr int WIDTH = 512 * C * W;        // most columns
+  __shared__ __attribute__((aligned(16))) float joined[ROWS > 1 ? ROWS * WIDTH : 4];
   __shared__ float part[2][WAVES][2];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, w = wave % W;
   const float rho = a.q ? *a.scale : 0.0f;
@@ -79,13 +76,13 @@ __global__ __launch_bounds__(kThreads) void postnorm_grad_kernel(Args a) {
     for (int k = 0; k < 8; ++k) sum[c][k] = 0.0f;
   uint32_t top = 0u;
   int turn = 0;
-  for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < a.rows; r0 += (int64_t)gridDim.x * ROWS, turn ^= 1) {
-    const int64_t r = r0 + wave / W;
+  const int64_t step = (int64_t)gridDim.x * ROWS;
+  int64_t r = (int64_t)blockIdx.x * ROWS + wave / W;
+  for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < a.rows; r0 += step, r += step, turn ^= 1) {
     const bool there = r < a.rows;
-    uint4 y[C], G[C];
+    uint4 y[C], G[C], b[C];
     float yy = 0.0f, ty = 0.0f;
     if (there) {
-      uint4 b[C];
 #pragma unroll
       for (int c = 0; c < C; ++c) {
         const int col = 8 * (64 * (c * W + w) + lane), n = a.cols - col;
@@ -100,17 +97,16 @@ __global__ __launch_bounds__(kThreads) void postnorm_grad_kernel(Args a) {
       for (int c = 0; c < C; ++c) {
         const int col = 8 * (64 * (c * W + w) + lane), n = a.cols - col;
         if (n <= 0) continue;
+        float f[8], h[8], g[8];
+        unpack8(G[c], f);
         if (a.dbranch) {
-          float f[8], h[8];
-          unpack8(G[c], f);
           unpack8(b[c], h);
 #pragma unroll
           for (int k = 0; k < 8; ++k) f[k] += h[k];
           G[c] = pack8(f);
+          unpack8(G[c], f);
         }
         if (a.dstream) put(a.dstream + r * a.ld_dstream + col, G[c], n);
-        float f[8], h[8], g[8];
-        unpack8(G[c], f);
         unpack8(y[c], h);
         gains8(a.gamma + col, n, g);
 #pragma unroll
@@ -156,31 +152,33 @@ __global__ __launch_bounds__(kThreads) void postnorm_grad_kernel(Args a) {
       }
     }
   }
-  if (a.sums && !JOINED) {
-    float* out = a.sums + ((int64_t)blockIdx.x * ROWS + wave / W) * a.cols;
+  if (a.sums) {
+    if (ROWS > 1) {
+      // every set of waves leaves its sums in LDS; then each thread adds what the sets have for its columns, in order
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const int col = 8 * (64 * (c * W + w) + lane);
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (col + k < a.cols) out[col + k] = sum[c][k];
-    }
-  } else if (a.sums) {
-    // the rows' sums, one wave (of each set of W) after the other
-    for (int i = 0; i < ROWS; ++i) {
-      if (wave / W == i) {
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-          const int col = 8 * (64 * (c * W + w) + lane);
-#pragma unroll
-          for (int k = 0; k < 8; ++k)
-            if (col + k < a.cols) joined[col + k] = i == 0 ? sum[c][k] : joined[col + k] + sum[c][k];
-        }
+      for (int c = 0; c < C; ++c) {
+        float* to = joined + (wave / W) * WIDTH + 8 * (64 * (c * W + w) + lane);
+        *reinterpret_cast<float4*>(to) = make_float4(sum[c][0], sum[c][1], sum[c][2], sum[c][3]);
+        *reinterpret_cast<float4*>(to + 4) = make_float4(sum[c][4], sum[c][5], sum[c][6], sum[c][7]);
       }
       __syncthreads();
+      float* out = a.sums + (int64_t)blockIdx.x * a.cols;
+      for (int i = threadIdx.x; i < a.cols; i += kThreads) {
+        float t = joined[i];
+#pragma unroll
+        for (int k = 1; k < ROWS; ++k) t += joined[k * WIDTH + i];
+        out[i] = t;
+      }
+    } else {
+      float* out = a.sums + (int64_t)blockIdx.x * a.cols;
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const int col = 8 * (64 * (c * W + w) + lane);
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (col + k < a.cols) out[col + k] = sum[c][k];
+      }
     }
-    float* out = a.sums + (int64_t)blockIdx.x * a.cols;
-    for (int i = threadIdx.x; i < a.cols; i += kThreads) out[i] = joined[i];
   }
   if (a.tops) {
     __shared__ uint32_t tops[WAVES];
@@ -196,24 +194,42 @@ __global__ __launch_bounds__(kThreads) void postnorm_grad_kernel(Args a) {
   }
 }
 
-// The gains' gradient from the workgroups' sums: 32 columns a workgroup, 32 threads for each, each with every 32nd sum.
+// The gains' gradient from the workgroups' sums: 32 columns a workgroup, four to a thread and a row in every 128, added in order.
 constexpr int kJoinThreads = 1024;
-__global__ __launch_bounds__(kJoinThreads) void postnorm_grad_join_kernel(const float* __restrict__ sums, const uint32_t* __restrict__ tops, int rows, int groups, int cols,
+__global__ __launch_bounds__(kJoinThreads) void postnorm_grad_join_kernel(const float* __restrict__ sums, const uint32_t* __restrict__ tops, int groups, int cols,
                                                                           float* __restrict__ dgamma, int accumulate, uint32_t* __restrict__ amax) {
-  __shared__ float part[32][33];
-  const int x = threadIdx.x & 31, z = threadIdx.x >> 5, col = (int)blockIdx.x * 32 + x;
+  constexpr int SLICES = kJoinThreads / 8, LOADS = GROUPS / SLICES;
+  __shared__ float part[SLICES][33];
   if (dgamma) {
-    float s = 0.0f;
-    if (col < cols)
-      for (int i = z; i < rows; i += 32) s += sums[(int64_t)i * cols + col];
-    part[z][x] = s;
-    __syncthreads();
-    if (z == 0 && col < cols) {
-      float t = accumulate ? dgamma[col] : 0.0f;
-      float u = 0.0f;
-      for (int i = 0; i < 32; ++i) u += part[i][x];
-      dgamma[col] = t + u;
+    const int x = threadIdx.x & 7, z = threadIdx.x >> 3, col = (int)blockIdx.x * 32 + 4 * x, n = cols - col;
+    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    uint4 v[LOADS];
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int g = z + i * SLICES;
+      v[i] = make_uint4(0, 0, 0, 0);
+      if (g < groups && n > 0) {
+        const float* p = sums + (int64_t)g * cols + col;
+        if (n >= 4) v[i] = ld_any16(p);
+        else v[i] = make_uint4(__float_as_uint(p[0]), n > 1 ? __float_as_uint(p[1]) : 0u, n > 2 ? __float_as_uint(p[2]) : 0u, 0u);
+      }
     }
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      s[0] += __uint_as_float(v[i].x); s[1] += __uint_as_float(v[i].y); s[2] += __uint_as_float(v[i].z); s[3] += __uint_as_float(v[i].w);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) part[z][4 * x + k] = s[k];
+    __syncthreads();
+    // 32 threads a column: four slices each, then the wave's halves by lane exchanges
+    const int c = threadIdx.x >> 5, l = threadIdx.x & 31;
+    float t = 0.0f;
+#pragma unroll
+    for (int i = 0; i < SLICES / 32; ++i) t += part[l + 32 * i][c];
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) t += __shfl_xor(t, o, 64);
+    const int to = (int)blockIdx.x * 32 + c;
+    if (l == 0 && to < cols) dgamma[to] = accumulate ? dgamma[to] + t : t;
   }
   if (amax && blockIdx.x == 0 && threadIdx.x < 64) {
     uint32_t m = 0u;
@@ -228,23 +244,18 @@ void launch(const Args& a, int groups, hipStream_t s) {
   postnorm_grad_kernel<FMT, W, C><<<groups, kThreads, 0, s>>>(a);
 }
 
-// Waves of a row: one up to 4096 columns.
-int waves_of(int64_t cols) { return cols <= 4096 ? 1 : cols <= 8192 ? 2 : cols <= 16384 ? 4 : 8; }
+// Waves of a row, two chunks of eight a lane (16 sums of the gains' gradient); rows of more columns than eight waves hold so take four and eight chunks.
+int waves_of(int64_t cols) { return cols <= 1024 ? 1 : cols <= 2048 ? 2 : cols <= 4096 ? 4 : 8; }
 int groups_of(int64_t rows, int64_t cols) {
   const int64_t n = WAVES / waves_of(cols), g = (rows + n - 1) / n;
   return (int)(g < GROUPS ? g : GROUPS);
-}
-// Rows of sums in the workspace.
-int sums_of(int64_t rows, int64_t cols) {
-  const int W = waves_of(cols);
-  return groups_of(rows, cols) * (joins(W) ? 1 : WAVES / W);
 }
 
 }  // namespace
 
 extern "C" size_t fog_postnorm_residual_grad_workspace(int64_t rows, int64_t cols) {
   if (rows <= 0 || cols <= 0 || cols > COLS_MAX) return 0;
-  return (size_t)sums_of(rows, cols) * (size_t)cols * sizeof(float) + (size_t)groups_of(rows, cols) * sizeof(uint32_t);
+  return (size_t)groups_of(rows, cols) * ((size_t)cols * sizeof(float) + sizeof(uint32_t));
 }
 
 extern "C" fog_status fog_postnorm_residual_grad(const void* dres_bf16, int64_t ld_dres, const void* dbranch_bf16, int64_t ld_dbranch, const void* y_bf16,
@@ -282,15 +293,15 @@ extern "C" fog_status fog_postnorm_residual_grad(const void* dres_bf16, int64_t 
     a.dres = reinterpret_cast<const uint16_t*>(dres_bf16); a.dbranch = reinterpret_cast<const uint16_t*>(dbranch_bf16); a.y = reinterpret_cast<const uint16_t*>(y_bf16);
     a.gamma = gamma; a.scale = scale; a.dstream = reinterpret_cast<uint16_t*>(dstream_bf16); a.dy = reinterpret_cast<uint16_t*>(dy_bf16); a.q = q;
     a.sums = dgamma ? sums : nullptr;
-    a.tops = amax_out ? reinterpret_cast<uint32_t*>(sums + (int64_t)sums_of(rows, cols) * cols) : nullptr;
+    a.tops = amax_out ? reinterpret_cast<uint32_t*>(sums + (int64_t)groups * cols) : nullptr;
     a.ld_dres = ld_dres; a.ld_dbranch = ld_dbranch; a.ldy = ldy; a.ld_dstream = ld_dstream; a.ld_dy = ld_dy; a.ldq = ldq; a.rows = rows; a.cols = (int)cols;
 #define FOG_PNG(W, C) (fmt == FOG_E4M3 ? launch<FOG_E4M3, W, C>(a, groups, s) : launch<FOG_E5M2, W, C>(a, groups, s))
     if (cols <= 512) FOG_PNG(1, 1);
     else if (cols <= 1024) FOG_PNG(1, 2);
-    else if (cols <= 2048) FOG_PNG(1, 4);
-    else if (cols <= 4096) FOG_PNG(1, 8);
-    else if (cols <= 8192) FOG_PNG(2, 8);
-    else if (cols <= 16384) FOG_PNG(4, 8);
+    else if (cols <= 2048) FOG_PNG(2, 2);
+    else if (cols <= 4096) FOG_PNG(4, 2);
+    else if (cols <= 8192) FOG_PNG(8, 2);
+    else if (cols <= 16384) FOG_PNG(8, 4);
     else FOG_PNG(8, 8);
 #undef FOG_PNG
   } else if ((!dgamma || accumulate || cols == 0) && !amax_out) {
@@ -298,7 +309,7 @@ extern "C" fog_status fog_postnorm_residual_grad(const void* dres_bf16, int64_t 
   }
   if ((dgamma && cols > 0) || amax_out) {
     const int64_t blocks = dgamma && cols > 0 ? (cols + 31) / 32 : 1;
-    postnorm_grad_join_kernel<<<(int)blocks, kJoinThreads, 0, s>>>(a.sums, a.tops, groups ? sums_of(rows, cols) : 0, groups, (int)cols, cols > 0 ? dgamma : nullptr, accumulate, reinterpret_cast<uint32_t*>(amax_out));
+    postnorm_grad_join_kernel<<<(int)blocks, kJoinThreads, 0, s>>>(a.sums, a.tops, groups, (int)cols, cols > 0 ? dgamma : nullptr, accumulate, reinterpret_cast<uint32_t*>(amax_out));
   }
   return fog_launch_status();
 }

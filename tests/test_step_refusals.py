@@ -243,8 +243,8 @@ def test_postnorm_grad_takes(lib, change):
 def test_postnorm_grad_workspace(lib):
     size = lib.fog_postnorm_residual_grad_workspace
     assert size(0, 64) == 0 and size(4, 0) == 0 and size(4, 32769) == 0 and size(-1, -1) == 0
-    assert size(1, 64) == 64 * 4 + 4 and size(8, 64) == size(1, 64) and size(9, 64) == 2 * size(1, 64) and size(1 << 40, 64) == 256 * size(1, 64)
-    assert size(1 << 40, 4096) == 256 * (4 * 4096 + 4) and size(1 << 40, 16384) == 256 * (2 * 4 * 16384 + 4) and size(1 << 40, 32768) == 256 * (4 * 32768 + 4)
+    assert size(1, 64) == 64 * 4 + 4 and size(8, 64) == size(1, 64) and size(9, 64) == 2 * size(1, 64) and size(1 << 40, 64) == 512 * size(1, 64)
+    assert size(1 << 40, 4096) == 512 * (4 * 4096 + 4) and size(1 << 40, 16384) == 512 * (4 * 16384 + 4) and size(1 << 40, 32768) == 512 * (4 * 32768 + 4)
 
 
 def act_grad(lib, which, x=P, ldx=64, dy=P + MB, ld_dy=64, rows=4, cols=64, alpha=(0.8, 0.6), fmt=1, scale=P + 2 * MB, dx=P + 3 * MB, ld_dx=64, q=P + 4 * MB, ldq=64,
