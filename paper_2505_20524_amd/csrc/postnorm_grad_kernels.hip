@@ -127,8 +127,8 @@ __global__ __launch_bounds__(kThreads) void postnorm_grad_kernel(Args a) {
       for (int i = 0; i < W; ++i) { yy += part[turn][wave - w + i][0]; ty += part[turn][wave - w + i][1]; }
     }
     if (!there) continue;
-    // 1 / rms, correctly rounded square root and divisions; a row of zeros gets no gradient
-    const float inv = yy != 0.0f ? 1.0f / __builtin_sqrtf(yy / cols) : 0.0f, along = yy != 0.0f ? ty / yy : 0.0f;
+    // 1 / rms, correctly rounded square root and divisions; a row of zeros, or of numbers whose squares vanish, gets no gradient
+    const float mean = yy / cols, inv = mean != 0.0f ? 1.0f / __builtin_sqrtf(mean) : 0.0f, along = inv != 0.0f ? ty / yy : 0.0f;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const int col = 8 * (64 * (c * W + w) + lane), n = a.cols - col;

@@ -37,7 +37,10 @@ struct Shape {
   uint32_t* part;                        // a word for each workgroup, or NULL
   int64_t positions, offset;
   uint32_t tokens, S, groups;            // groups: of tokens that a job's workgroups walk side by side
+  float inv_cols;                        // 1 / D
+  bool overlap;                          // eight does not divide a stretch of the FULL form
   int D, rot, segment, pos_bytes;        // segment: heads of a workgroup
+  int side;                              // log2 of the tokens that a workgroup takes side by side; its other vectors are more of their heads
 };
 static_assert(sizeof(Jobs) + sizeof(Shape) <= 4096, "arguments of a launch");
 
@@ -57,8 +60,16 @@ FOG_DEVICE float row_sum(float s) {
   return s;
 }
 
-// 1 / rms with a gain, correctly rounded; 0 for a vector of zeros (NaN for one that holds a NaN).
-FOG_DEVICE float inv_rms(float sumsq, float cols, float gain) { return sumsq != 0.0f ? gain / __builtin_sqrtf(sumsq / cols) : 0.0f; }
+// gain / rms, half a unit in the last place and a little more: one Newton step on the hardware's reciprocal square root with the residue of r^2 m - 1 to twice the
+// places, which is both shorter and closer than a correctly rounded root and a division.  0 for a vector of zeros, NaN for one that holds a NaN.
+FOG_DEVICE float inv_rms(float sumsq, float inv_cols, float gain) {
+  const float m = sumsq * inv_cols;
+  if (__builtin_expect(!(m >= 0x1p-100f && m <= 0x1p+100f), 0)) return m != 0.0f ? gain / __builtin_sqrtf(m) : 0.0f;
+  const float r = __builtin_amdgcn_rsqf(m);
+  const float h = r * r, l = __builtin_fmaf(r, r, -h);
+  const float e = __builtin_fmaf(-m, l, __builtin_fmaf(-m, h, 1.0f));       // 1 - m r^2
+  return gain * __builtin_fmaf(0.5f * r, e, r);
+}
 
 FOG_DEVICE void unpack8(uint4 v, float (&f)[8]) {
   f[0] = bf16lo(v.x); f[1] = bf16hi(v.x); f[2] = bf16lo(v.y); f[3] = bf16hi(v.y);
@@ -68,6 +79,7 @@ FOG_DEVICE uint4 pack8(const float (&f)[8]) {
   return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
 }
 
+// Runs of eight elements; those of FULL are whole (or not there at all, n == 0).
 template <bool FULL>
 FOG_DEVICE uint4 fetch(const uint16_t* p, int n) {
   if (FULL) return n > 0 ? ld_any_nt16(p) : make_uint4(0, 0, 0, 0);
@@ -88,12 +100,42 @@ FOG_DEVICE void store_half(uint16_t* p, uint4 w, int n) {
   if (FULL ? n > 0 : n >= 8) st_any16(p, w);
   else if (!FULL) st_upto8(p, w, n);
 }
-
-FOG_DEVICE uint2 cast8(const float (&y)[8], float rho, bool e5m2, bool& nan) {
-  if (e5m2)
-    return make_uint2(cvt4_fp8_nan<FOG_E5M2>(y[0] * rho, y[1] * rho, y[2] * rho, y[3] * rho, &nan), cvt4_fp8_nan<FOG_E5M2>(y[4] * rho, y[5] * rho, y[6] * rho, y[7] * rho, &nan));
-  return make_uint2(cvt4_fp8_nan<FOG_E4M3>(y[0] * rho, y[1] * rho, y[2] * rho, y[3] * rho, &nan), cvt4_fp8_nan<FOG_E4M3>(y[4] * rho, y[5] * rho, y[6] * rho, y[7] * rho, &nan));
+// Eight floats at any address of a float.
+FOG_DEVICE void floats8(const float* p, float (&f)[8]) {
+  const uint4 a = ld_any16(p), b = ld_any16(p + 4);
+  f[0] = __uint_as_float(a.x); f[1] = __uint_as_float(a.y); f[2] = __uint_as_float(a.z); f[3] = __uint_as_float(a.w);
+  f[4] = __uint_as_float(b.x); f[5] = __uint_as_float(b.y); f[6] = __uint_as_float(b.z); f[7] = __uint_as_float(b.w);
 }
+// Zeros in the place of the first `skip` of sixteen elements.
+FOG_DEVICE void skip16(float (&a)[8], float (&b)[8], int skip_a, int skip_b) {
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    if (k < skip_a) a[k] = 0.0f;
+    if (k < skip_b) b[k] = 0.0f;
+  }
+}
+
+// Eight numbers to codes.  With CLAMP they are limited to the format first; without it the wave's converts saturate.
+template <bool CLAMP>
+FOG_DEVICE uint2 convert8(const float (&y)[8], bool e5m2) {
+  if (e5m2)
+    return CLAMP ? make_uint2(cvt4_fp8<FOG_E5M2>(y[0], y[1], y[2], y[3]), cvt4_fp8<FOG_E5M2>(y[4], y[5], y[6], y[7]))
+                 : make_uint2(cvt4_fp8_finite<FOG_E5M2>(y[0], y[1], y[2], y[3]), cvt4_fp8_finite<FOG_E5M2>(y[4], y[5], y[6], y[7]));
+  return CLAMP ? make_uint2(cvt4_fp8<FOG_E4M3>(y[0], y[1], y[2], y[3]), cvt4_fp8<FOG_E4M3>(y[4], y[5], y[6], y[7]))
+               : make_uint2(cvt4_fp8_finite<FOG_E4M3>(y[0], y[1], y[2], y[3]), cvt4_fp8_finite<FOG_E4M3>(y[4], y[5], y[6], y[7]));
+}
+// What convert8 does not do, for vectors that hold an infinity or a NaN: infinities become the largest finite number, a NaN a zero of its sign under a
+// code's seven set bits.  (Beside the conversion and not in it: kernels of a few microseconds are as long as their code.)
+FOG_DEVICE uint2 tame8(float (&y)[8]) {
+  uint32_t n[2] = {0u, 0u};
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    if (y[k] != y[k]) n[k >> 2] |= 0x7Fu << (8 * (k & 3));
+    y[k] = y[k] != y[k] ? __builtin_copysignf(0.0f, y[k]) : __builtin_amdgcn_fmed3f(y[k], -FLT_MAX, FLT_MAX);
+  }
+  return make_uint2(n[0], n[1]);
+}
+FOG_DEVICE uint2 with(uint2 q, uint2 n) { return make_uint2(q.x | n.x, q.y | n.y); }
 
 // The turn by (c, s) of eight pairs, or with BACK its transpose.
 template <bool INTER, bool BACK>
@@ -113,21 +155,26 @@ FOG_DEVICE void turn(float (&a)[8], float (&b)[8], const float (&c)[8], const fl
 
 template <int LPR, bool INTER, bool GRAD, bool FULL>
 __global__ __launch_bounds__(kThreads) void rope_kernel(Jobs jobs, Shape sh) {
-  constexpr int TOKENS = kThreads / LPR;        // of a workgroup and trip
-  constexpr int U = GRAD ? 2 : 4;               // heads in flight
+  constexpr int VECTORS = kThreads / LPR;       // of a workgroup at a time
+  constexpr int U = GRAD ? 2 : 1;               // heads in flight
   int j = 0;
   while (j + 1 < jobs.count && (int)blockIdx.x >= jobs.job[j + 1].first) ++j;
   const Job& job = jobs.job[j];
-  const uint32_t at = blockIdx.x - job.first;
-  const int h0 = (int)(at / sh.groups) * sh.segment, h1 = h0 + sh.segment < job.heads ? h0 + sh.segment : job.heads;
+  const uint32_t at = blockIdx.x - job.first, segments = (uint32_t)((job.heads + sh.segment - 1) / sh.segment);
+  const int h0 = (int)(at % segments) * sh.segment, h1 = h0 + sh.segment < job.heads ? h0 + sh.segment : job.heads;
+  const uint32_t vector = threadIdx.x / LPR, tokens = 1u << sh.side;
+  const int slot = (int)(vector >> sh.side), slots = VECTORS >> sh.side;
   const int lane = threadIdx.x % LPR;
   const bool rotate = job.rotate != 0;
   const int half = rotate ? sh.rot >> 1 : 0, turners = (half + 7) >> 3;
   const bool on = lane < turners;
-  int offA, offB, nA, nB;
+  // Where the lane's two runs begin and how long they are.  In the FULL form every run is of eight: the last one of a stretch that eight does not divide
+  // reaches back over elements of the lane in front of it, which gives them the same values; only sums leave those out (skip).
+  int offA, offB, nA, nB, skipA = 0, skipB = 0, first = 8 * lane;        // first: pair
   if (on) {
     const int pairs = half - 8 * lane < 8 ? half - 8 * lane : 8;
-    offA = (INTER ? 16 : 8) * lane;
+    if (FULL) first -= 8 - pairs;
+    offA = (INTER ? 2 : 1) * first;
     offB = INTER ? offA + 8 : offA + half;
     nA = INTER ? (2 * pairs < 8 ? 2 * pairs : 8) : pairs;
     nB = INTER ? 2 * pairs - nA : pairs;
@@ -137,17 +184,37 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(Jobs jobs, Shape sh) {
     const int n = sh.D - offA;
     nA = n < 0 ? 0 : n < 8 ? n : 8;
     nB = n - 8 < 0 ? 0 : n - 8 < 8 ? n - 8 : 8;
+    if (FULL && n > 0 && n < 16) {
+      offB = sh.D - 8;
+      if (sh.D - 2 * half >= 16) offA = sh.D - 16;
+    }
+  }
+  if (FULL && nA + nB > 0) {
+    if (on && !INTER) {
+      skipA = skipB = 8 - nA;
+    } else if (on || sh.D - 2 * half >= 16) {      // sixteen elements in a row, the last ones new
+      const int skip = 16 - (nA + nB);
+      skipA = skip < 8 ? skip : 8;
+      skipB = skip - skipA;
+    } else {
+      skipB = 8 - nB;
+    }
+    nA = nB = 8;
   }
   const float rho = job.q.p ? *job.scale : 0.0f;
   const bool norm = job.gain > 0.0f, e5m2 = job.e5m2 != 0;
-  const float cols = (float)sh.D;
+  if (!GRAD) saturating_converts();      // (the backward converts to bf16, which the mode would saturate too)
   float top = 0.0f;
   bool nan = false;
   uint32_t top_bits = 0u;
-  for (uint32_t group = at % sh.groups; group * (uint64_t)TOKENS < sh.tokens; group += sh.groups) {
-    const uint32_t t = group * TOKENS + threadIdx.x / LPR;
+  for (uint32_t group = at / segments; group * (uint64_t)tokens < sh.tokens; group += sh.groups) {
+    const uint32_t t = group * tokens + (vector & (tokens - 1));
     if (t >= sh.tokens) break;           // (whole vectors: their lanes leave together)
     const uint32_t b = t / sh.S, s = t - b * sh.S;
+    const uint16_t* in = reinterpret_cast<const uint16_t*>(job.in.p) + b * job.in.batch + s * job.in.token;
+    const uint16_t* xin = GRAD && norm ? reinterpret_cast<const uint16_t*>(job.x.p) + b * job.x.batch + s * job.x.token : nullptr;
+    uint8_t* q = job.q.p ? reinterpret_cast<uint8_t*>(job.q.p) + b * job.q.batch + s * job.q.token : nullptr;
+    uint16_t* dx = GRAD && job.dx.p ? reinterpret_cast<uint16_t*>(job.dx.p) + b * job.dx.batch + s * job.dx.token : nullptr;
     bool there = true;
     float c[8], sn[8];
 #pragma unroll
@@ -157,34 +224,28 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(Jobs jobs, Shape sh) {
                                 : sh.pos_bytes == 8 ? reinterpret_cast<const int64_t*>(sh.pos)[t] : (int64_t)reinterpret_cast<const int32_t*>(sh.pos)[t];
       there = p >= 0 && p < sh.positions;
       if (on && there) {
-        const float* row = sh.table + p * sh.rot + 8 * lane;
+        const float* row = sh.table + p * sh.rot + first;
         if (FULL) {
-          const float4 c0 = *reinterpret_cast<const float4*>(row), c1 = *reinterpret_cast<const float4*>(row + 4);
-          const float4 s0 = *reinterpret_cast<const float4*>(row + half), s1 = *reinterpret_cast<const float4*>(row + half + 4);
-          c[0] = c0.x; c[1] = c0.y; c[2] = c0.z; c[3] = c0.w; c[4] = c1.x; c[5] = c1.y; c[6] = c1.z; c[7] = c1.w;
-          sn[0] = s0.x; sn[1] = s0.y; sn[2] = s0.z; sn[3] = s0.w; sn[4] = s1.x; sn[5] = s1.y; sn[6] = s1.z; sn[7] = s1.w;
+          floats8(row, c);
+          floats8(row + half, sn);
         } else {
 #pragma unroll
           for (int k = 0; k < 8; ++k)
-            if (8 * lane + k < half) { c[k] = row[k]; sn[k] = row[half + k]; }
+            if (first + k < half) { c[k] = row[k]; sn[k] = row[half + k]; }
         }
       }
     }
-    const uint16_t* in = reinterpret_cast<const uint16_t*>(job.in.p) + b * job.in.batch + s * job.in.token;
-    const uint16_t* xin = GRAD && norm ? reinterpret_cast<const uint16_t*>(job.x.p) + b * job.x.batch + s * job.x.token : nullptr;
-    uint8_t* q = job.q.p ? reinterpret_cast<uint8_t*>(job.q.p) + b * job.q.batch + s * job.q.token : nullptr;
-    uint16_t* dx = GRAD && job.dx.p ? reinterpret_cast<uint16_t*>(job.dx.p) + b * job.dx.batch + s * job.dx.token : nullptr;
-    for (int h = h0; h < h1; h += U) {
+    for (int h = h0 + slot; h < h1; h += U * slots) {
       uint4 va[U], vb[U], xa[U], xb[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         va[u] = vb[u] = xa[u] = xb[u] = make_uint4(0, 0, 0, 0);
-        if (h + u < h1) {
-          const uint16_t* p = in + (h + u) * job.in.head;
+        if (h + u * slots < h1) {
+          const uint16_t* p = in + (h + u * slots) * job.in.head;
           va[u] = fetch<FULL>(p + offA, nA);
           vb[u] = fetch<FULL>(p + offB, nB);
           if (GRAD && norm) {
-            const uint16_t* x = xin + (h + u) * job.x.head;
+            const uint16_t* x = xin + (h + u * slots) * job.x.head;
             xa[u] = fetch<FULL>(x + offA, nA);
             xb[u] = fetch<FULL>(x + offB, nB);
           }
@@ -192,44 +253,71 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(Jobs jobs, Shape sh) {
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        if (h + u >= h1) break;
+        if (h + u * slots >= h1) break;
         float a[8], e[8];
         unpack8(va[u], a);
         unpack8(vb[u], e);
         if (!GRAD) {
+          float inv = 1.0f;
           if (norm) {
-            float sum = 0.0f;
+            float p[8], r[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) sum = __builtin_fmaf(a[k], a[k], sum);
+            for (int k = 0; k < 8; ++k) { p[k] = a[k]; r[k] = e[k]; }
+            if (FULL && sh.overlap) skip16(p, r, skipA, skipB);
+            float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int k = 0; k < 8; ++k) sum = __builtin_fmaf(e[k], e[k], sum);
-            const float inv = inv_rms(row_sum<LPR>(sum), cols, job.gain);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) { a[k] *= inv; e[k] *= inv; }
+            for (int k = 0; k < 8; ++k) {
+              sum[k & 3] = __builtin_fmaf(p[k], p[k], sum[k & 3]);
+              sum[k & 3] = __builtin_fmaf(r[k], r[k], sum[k & 3]);
+            }
+            inv = inv_rms(row_sum<LPR>((sum[0] + sum[1]) + (sum[2] + sum[3])), sh.inv_cols, job.gain);
           }
+          // the turn is linear: the norm's factor comes behind it, as one number with the scale
           if (on) turn<INTER, false>(a, e, c, sn);
           if (!there) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) a[k] = e[k] = 0.0f;
+            inv = 0.0f;
           }
+          float most = 0.0f;               // (a NaN stays: finite products need neither a clamp nor a NaN test)
 #pragma unroll
-          for (int k = 0; k < 8; ++k) top = fmaxf(top, fmaxf(fabsf(a[k]), fabsf(e[k])));
-          uint8_t* to = q + (h + u) * job.q.head;
-          store_codes<FULL>(to + offA, cast8(a, rho, e5m2, nan), nA);
-          store_codes<FULL>(to + offB, cast8(e, rho, e5m2, nan), nB);
+          for (int k = 0; k < 8; ++k) most = __builtin_elementwise_maximum(most, __builtin_elementwise_maximum(fabsf(a[k]), fabsf(e[k])));
+          float f = inv * rho;
+          if (__builtin_expect(!(fabsf(f) <= FLT_MAX), 0)) {      // a short vector under a large scale: the factors one by one
+#pragma unroll
+            for (int k = 0; k < 8; ++k) { a[k] *= inv; e[k] *= inv; }
+            most *= inv;
+            inv = 1.0f;
+            f = rho;
+          }
+          top = fmaxf(top, most * inv);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) { a[k] *= f; e[k] *= f; }
+          uint2 na = make_uint2(0, 0), ne = na;
+          if (__builtin_expect(!(most * fabsf(f) <= FLT_MAX), 0)) {
+            na = tame8(a);
+            ne = tame8(e);
+            nan |= (na.x | na.y | ne.x | ne.y) != 0u;
+          }
+          uint8_t* to = q + (h + u * slots) * job.q.head;
+          store_codes<FULL>(to + offA, with(convert8<false>(a, e5m2), na), nA);
+          store_codes<FULL>(to + offB, with(convert8<false>(e, e5m2), ne), nB);
         } else {
           if (on) turn<INTER, true>(a, e, c, sn);
           if (norm) {
-            float x0[8], x1[8], xx = 0.0f, xd = 0.0f;
+            float x0[8], x1[8], p[8], r[8], xx = 0.0f, xd = 0.0f;
             unpack8(xa[u], x0);
             unpack8(xb[u], x1);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) { xx = __builtin_fmaf(x0[k], x0[k], xx); xd = __builtin_fmaf(x0[k], a[k], xd); }
+            for (int k = 0; k < 8; ++k) { p[k] = x0[k]; r[k] = x1[k]; }
+            if (FULL && sh.overlap) skip16(p, r, skipA, skipB);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) { xx = __builtin_fmaf(x1[k], x1[k], xx); xd = __builtin_fmaf(x1[k], e[k], xd); }
+            for (int k = 0; k < 8; ++k) { xx = __builtin_fmaf(p[k], p[k], xx); xd = __builtin_fmaf(p[k], a[k], xd); }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) { xx = __builtin_fmaf(r[k], r[k], xx); xd = __builtin_fmaf(r[k], e[k], xd); }
             xx = row_sum<LPR>(xx);
             xd = row_sum<LPR>(xd);
-            const float inv = inv_rms(xx, cols, job.gain), along = xx != 0.0f ? xd / xx : 0.0f;
+            const float inv = inv_rms(xx, sh.inv_cols, job.gain), along = inv != 0.0f ? xd / xx : 0.0f;
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
               a[k] = inv * __builtin_fmaf(-x0[k], along, a[k]);
@@ -238,29 +326,36 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(Jobs jobs, Shape sh) {
           }
           uint4 wa = pack8(a), wb = pack8(e);
           if (!there) wa = wb = make_uint4(0, 0, 0, 0);
-          top_bits = pkmax_abs_bf16(top_bits, wa.x); top_bits = pkmax_abs_bf16(top_bits, wa.y);
-          top_bits = pkmax_abs_bf16(top_bits, wa.z); top_bits = pkmax_abs_bf16(top_bits, wa.w);
-          top_bits = pkmax_abs_bf16(top_bits, wb.x); top_bits = pkmax_abs_bf16(top_bits, wb.y);
-          top_bits = pkmax_abs_bf16(top_bits, wb.z); top_bits = pkmax_abs_bf16(top_bits, wb.w);
+          uint32_t most = 0u;
+          most = pkmax_abs_bf16(most, wa.x); most = pkmax_abs_bf16(most, wa.y); most = pkmax_abs_bf16(most, wa.z); most = pkmax_abs_bf16(most, wa.w);
+          most = pkmax_abs_bf16(most, wb.x); most = pkmax_abs_bf16(most, wb.y); most = pkmax_abs_bf16(most, wb.z); most = pkmax_abs_bf16(most, wb.w);
+          const uint32_t larger = max_of_pair(most);
+          top_bits = top_bits > larger ? top_bits : larger;
           if (dx) {
-            uint16_t* to = dx + (h + u) * job.dx.head;
+            uint16_t* to = dx + (h + u * slots) * job.dx.head;
             store_half<FULL>(to + offA, wa, nA);
             store_half<FULL>(to + offB, wb, nB);
           }
           if (q) {
-            float ra[8], rb[8];
-            unpack8(wa, ra);
-            unpack8(wb, rb);
-            uint8_t* to = q + (h + u) * job.q.head;
-            store_codes<FULL>(to + offA, cast8(ra, rho, e5m2, nan), nA);
-            store_codes<FULL>(to + offB, cast8(rb, rho, e5m2, nan), nB);
+            unpack8(wa, a);
+            unpack8(wb, e);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) { a[k] *= rho; e[k] *= rho; }
+            uint2 na = make_uint2(0, 0), ne = na;
+            if (__builtin_expect(!(__uint_as_float(larger << 16) * fabsf(rho) <= FLT_MAX), 0)) {
+              na = tame8(a);
+              ne = tame8(e);
+            }
+            uint8_t* to = q + (h + u * slots) * job.q.head;
+            store_codes<FULL>(to + offA, with(convert8<true>(a, e5m2), na), nA);
+            store_codes<FULL>(to + offB, with(convert8<true>(e, e5m2), ne), nB);
           }
         }
       }
     }
   }
   if (sh.part) {
-    const uint32_t m = wave_max_u32(GRAD ? max_of_pair(top_bits) << 16 : amax_bits(top, nan));
+    const uint32_t m = wave_max_u32(GRAD ? top_bits << 16 : amax_bits(top, nan));
     __shared__ uint32_t wave[kThreads / 64];
     if ((threadIdx.x & 63) == 0) wave[threadIdx.x >> 6] = m;
     __syncthreads();
@@ -368,18 +463,25 @@ template <bool GRAD>
 fog_status launch(Jobs& jobs, Shape& sh, float* const* amax, bool any_amax, int B, bool inter, void* workspace, hipStream_t s) {
   const int lanes = (sh.rot / 2 + 7) / 8 + (sh.D - sh.rot + 15) / 16, plain = (sh.D + 15) / 16, need = lanes > plain ? lanes : plain;
   const int lpr = need <= 4 ? 4 : need <= 8 ? 8 : need <= 16 ? 16 : need <= 32 ? 32 : 64;
-  const bool full = sh.rot % 16 == 0 && sh.D % 16 == 0 && (reinterpret_cast<uintptr_t>(sh.table) & 15) == 0;
+  // Whole runs of eight everywhere: no stretch (turned pairs, the rest) is shorter than one.
+  bool full = sh.D >= 8 && (sh.rot == 0 || sh.rot >= 16), plain_jobs = false;
+  for (int j = 0; j < jobs.count; ++j) plain_jobs |= !jobs.job[j].rotate;
+  if (sh.rot < sh.D) full = full && sh.D - sh.rot >= 8;
+  sh.overlap = sh.rot % 16 != 0 || (sh.D - sh.rot) % 16 != 0 || (plain_jobs && sh.D % 16 != 0);
   sh.tokens = (uint32_t)((int64_t)B * sh.S);
-  const int64_t groups = ((int64_t)sh.tokens * lpr + kThreads - 1) / kThreads;
-  // Heads of a workgroup: as few as fill the chip, up to eight.
-  const int64_t want = 8 * (int64_t)fog_compute_units();
+  sh.inv_cols = sh.D > 0 ? 1.0f / (float)sh.D : 0.0f;
+  const int vectors = kThreads / lpr;
+  while ((2 << sh.side) <= vectors && (1u << sh.side) < sh.tokens) ++sh.side;
+  const int64_t groups = ((int64_t)sh.tokens + (1 << sh.side) - 1) >> sh.side;
+  // Heads of a workgroup: as few as fill the chip, up to eight for each of its slots.
+  const int64_t want = 8 * (int64_t)fog_compute_units(), slots = vectors >> sh.side;
   auto segments = [&](int64_t segment) {
     int64_t n = 0;
     for (int j = 0; j < jobs.count; ++j) n += (jobs.job[j].heads + segment - 1) / segment;
     return n;
   };
-  int64_t segment = 1;
-  while ((segment < 8 && segments(segment) * groups > want) || segments(segment) > WORDS / 2) segment *= 2;
+  int64_t segment = slots;
+  while ((segment < 8 * slots && segments(segment) * groups > want) || segments(segment) > WORDS / 2) segment *= 2;
   sh.segment = (int)segment;
   const int64_t all = segments(segment), most = all > 0 ? WORDS / all : 1;
   sh.groups = (uint32_t)(groups < most ? groups : most);
