@@ -272,6 +272,16 @@ def test_activation_rows_of_every_alignment(act, alpha, rows, cols, ld, skew):
 
 
 @pytest.mark.parametrize("act,alpha", ACTS)
+@pytest.mark.parametrize("rows,cols,ld,skew", [(1, 5_000_011, 0, 1), (2049, 2051, 0, 3), (1100, 4096, 16, 0), (1030, 4112, 3, 5), (1200, 4099, 1, 0)])
+def test_activation_of_large_tensors(act, alpha, rows, cols, ld, skew):
+    """From some four million elements on, end to end in a length that sixteen does not divide, in rows that it does, and in others."""
+    a = Act(27, act, alpha, rows, cols, ld, skew)
+    a.run()
+    a.check()
+    assert around(a.b_dx, a.dx) and around(a.b_q, a.q)
+
+
+@pytest.mark.parametrize("act,alpha", ACTS)
 @pytest.mark.parametrize("rows", [1, 96])          # 1, 96 times all 65536 - 512 finite numbers: below and above the sizes that a table pays for
 def test_activation_at_every_number(act, alpha, rows):
     """Every finite bf16 number that is not beyond the binary32 range of its slope."""
