@@ -615,7 +615,7 @@ fog_status fog_grad_clip(const fog_grad_job* jobs, int count, const double* sums
  *            where they are given, for steps that are captured once and replayed.  seed : any; the step's number enters the hash too.
  * Tensors of any alignment above their elements'; up to 2^24 of them, 50 to a launch.  The buffers that the call writes must not overlap each other or a
  * gradient.
- * Errors: NULL, SHAPE (count, n, step), ALIGN, UNSUPPORTED (types, states, n above 2^37, a beta outside 0 .. 1 (0.99), eps below the smallest
+ * Errors: NULL, SHAPE (count, n, step), ALIGN, UNSUPPORTED (types, states, n above 2^36, a beta outside 0 .. 1 (0.99), eps below the smallest
  * normal number, values that are not finite, max_norm negative, a master copy of binary32 p, buffers that overlap).
  */
 typedef enum { FOG_STATES_F32 = 0, FOG_STATES_FP8 = 1 } fog_states;

@@ -1,6 +1,7 @@
 // The AdamW step over many tensors, states in binary32 or in FP8 with a scale for each 128 elements.
 //
-// Bound by memory: 28 bytes an element with bf16 weights, bf16 gradients, a binary32 master copy and binary32 states, 16 with FP8 states.
+// Bound by memory: 28 bytes an element with bf16 weights, bf16 gradients, a binary32 master copy and binary32 states, 16 with FP8 states (there the
+// vector ALU is close behind).  Two blocks at 8B scale, 487 M elements: 2335 us (5.8 TB/s) and 1370 us (5.7 TB/s); 49 tensors of 4.8 M: 28 us.
 // As the gradients' norm and clipping: up to BATCH tensors a launch, cut into pieces of PIECE elements, a workgroup for each piece.
 //
 // Every operation on the moments is rounded once to binary32, in the order that the header states (no fused multiply-adds), so that a
@@ -23,7 +24,14 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int BATCH = 50;                // descriptions that fit a launch's arguments
-constexpr int64_t PIECE = 8192;          // elements; a multiple of a scale's 128
+// Elements of a piece, a multiple of a scale's 128.
+constexpr int F32_PIECE = 2048, FP8_PIECE = 4096;
+// Large launches of binary32 states (seven streams an element) are faster with fewer workgroups in flight: beyond MANY pieces (32 M elements) each asks for so much
+// LDS that five fit a compute unit, and keeps four elements a thread in flight instead of eight.  us, without -> with: 4.8 M elements 28.3 -> 30.3, 33.6 M 160.9 ->
+// 160.7, 101 M 487 -> 481, 403 M 2028 -> 1894.  (Pieces of 4096 and 8192 elements: 403 M 2019 and 2105.  FP8 states, whose arithmetic wants the waves: 1136 with
+// pieces of 4096 and sixteen elements in flight, 1167 with 2048 and eight, 1438 with fewer workgroups.)
+constexpr int MANY = 16384;
+constexpr size_t ROOM = 32 << 10;
 constexpr int GROUPS = 1 << 23;          // most workgroups of a launch: grids are counted in threads of 32 bits
 constexpr int TENSORS_MAX = 1 << 24;
 
@@ -43,6 +51,11 @@ struct AdamBatch {
   int count, pieces;
 };
 
+// What a step has in common: worked out on the host where the host knows all of it.
+struct Common {
+  float rate, root;
+  uint32_t key;
+};
 struct AdamStep {
   double lr, log_beta1, log_beta2;
   const float* lr_dev;
@@ -50,7 +63,9 @@ struct AdamStep {
   const double* sumsq;
   int64_t step;
   uint64_t seed;
+  Common common;
   float beta1, beta1c, beta2, beta2c, eps, max_norm;     // c: 1 - beta, from binary64
+  bool plain_eps;                                        // eps is 2^-38 or more
 };
 static_assert(sizeof(AdamBatch) + sizeof(AdamStep) <= 4096, "arguments of a launch");
 
@@ -65,15 +80,15 @@ FOG_DEVICE int tensor_of(const AdamBatch& b, int p) {
 }
 
 // Three rounds of shift and multiplication by odd numbers (the fractions of the golden ratio and of the roots of 2 and 3).
-FOG_DEVICE uint32_t mix(uint32_t h) {
+__host__ __device__ static inline uint32_t mix(uint32_t h) {
   h = (h ^ (h >> 16)) * 0x9E3779B1u;
   h = (h ^ (h >> 15)) * 0x6A09E667u;
   h = (h ^ (h >> 13)) * 0xBB67AE85u;
   return h ^ (h >> 16);
 }
-FOG_DEVICE uint32_t next_key(uint32_t key, uint32_t w) { return mix(key + 0x9E3779B9u + w); }
+__host__ __device__ static inline uint32_t next_key(uint32_t key, uint32_t w) { return mix(key + 0x9E3779B9u + w); }
 
-// The largest of the 16 lanes that hold a block of 128 elements.
+// The largest of the 32 lanes that hold a block of 128 elements.
 template <int CTRL>
 FOG_DEVICE uint32_t dpp_max(uint32_t v) {
   const uint32_t o = (uint32_t)__builtin_amdgcn_mov_dpp((int)v, CTRL, 0xF, 0xF, false);
@@ -83,7 +98,9 @@ FOG_DEVICE uint32_t block_max(uint32_t v) {
   v = dpp_max<0xB1>(v);           // lane ^ 1
   v = dpp_max<0x4E>(v);           // lane ^ 2
   v = dpp_max<0x141>(v);          // the other four of eight
-  return dpp_max<0x140>(v);       // the other eight of sixteen
+  v = dpp_max<0x140>(v);          // the other eight of sixteen
+  const uint32_t o = (uint32_t)__shfl_xor((int)v, 16, 64);
+  return v > o ? v : o;
 }
 
 // k of a block's scale from the bits of its abs-max: floor(log2(FP8MAX / a)), limited to -126 .. 126; 0 where a is zero or not finite.
@@ -105,179 +122,226 @@ FOG_DEVICE float round_by(float y, uint32_t r) {
   float a = fabsf(y);
   const float add = a < LOW ? LOW : 0.0f;
   a = __uint_as_float((__float_as_uint(a + add) + r) & ~((1u << DROP) - 1u)) - add;
-  return __builtin_copysignf(a, y);
+  return FMT == FOG_E4M3 ? __builtin_copysignf(a, y) : a;      // (second moments have no sign)
 }
 
-typedef u32x2 __attribute__((aligned(1))) u32x2_byte;
-// Eight elements from p on, of which n are there; zeros behind them.
-FOG_DEVICE void load8(const float* p, int n, float (&f)[8]) {
-  if (n >= 8) {
-    const uint4 a = ld_any_nt16(p), b = ld_any_nt16(p + 4);
+// A lane takes four elements at a time, so that every load and store of a binary32 tensor covers whole lines: in eights, two instructions each touch half of every
+// line (two blocks at 8B scale 2818 -> 2519 us, 49 small tensors 39 -> 32).
+typedef u32x2 __attribute__((aligned(2))) u32x2_half;
+typedef uint32_t __attribute__((aligned(1))) u32_byte;
+// Four elements from p on, of which n are there; zeros behind them.
+FOG_DEVICE void load4(const float* p, int n, float (&f)[4]) {
+  if (n >= 4) {
+    const uint4 a = ld_any_nt16(p);
     f[0] = __uint_as_float(a.x); f[1] = __uint_as_float(a.y); f[2] = __uint_as_float(a.z); f[3] = __uint_as_float(a.w);
-    f[4] = __uint_as_float(b.x); f[5] = __uint_as_float(b.y); f[6] = __uint_as_float(b.z); f[7] = __uint_as_float(b.w);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = i < n ? p[i] : 0.0f;
+    for (int i = 0; i < 4; ++i) f[i] = i < n ? p[i] : 0.0f;
   }
 }
-FOG_DEVICE void load8(const uint16_t* p, int n, float (&f)[8]) {
-  const uint4 a = n >= 8 ? ld_any_nt16(p) : ld_upto8(p, n);
-  f[0] = bf16lo(a.x); f[1] = bf16hi(a.x); f[2] = bf16lo(a.y); f[3] = bf16hi(a.y);
-  f[4] = bf16lo(a.z); f[5] = bf16hi(a.z); f[6] = bf16lo(a.w); f[7] = bf16hi(a.w);
-}
-FOG_DEVICE uint2 load_codes(const uint8_t* p, int n) {
-  if (n >= 8) {
-    const u32x2 v = __builtin_nontemporal_load(reinterpret_cast<const u32x2_byte*>(p));
-    return make_uint2(v[0], v[1]);
-  }
-  uint32_t w[2] = {0, 0};
+FOG_DEVICE void load4(const uint16_t* p, int n, float (&f)[4]) {
+  if (n >= 4) {
+    const u32x2 a = __builtin_nontemporal_load(reinterpret_cast<const u32x2_half*>(p));
+    f[0] = bf16lo(a[0]); f[1] = bf16hi(a[0]); f[2] = bf16lo(a[1]); f[3] = bf16hi(a[1]);
+  } else {
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (i < n) w[i >> 2] |= (uint32_t)p[i] << (8 * (i & 3));
-  return make_uint2(w[0], w[1]);
+    for (int i = 0; i < 4; ++i) f[i] = i < n ? bf16lo(p[i]) : 0.0f;
+  }
 }
-FOG_DEVICE void store8(float* p, int n, const float (&f)[8]) {
-  if (n >= 8) {
+FOG_DEVICE uint32_t load_codes(const uint8_t* p, int n) {
+  if (n >= 4) return __builtin_nontemporal_load(reinterpret_cast<const u32_byte*>(p));
+  uint32_t w = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (i < n) w |= (uint32_t)p[i] << (8 * i);
+  return w;
+}
+FOG_DEVICE void store4(float* p, int n, const float (&f)[4]) {
+  if (n >= 4) {
     st_any_nt16(p, make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])));
-    st_any_nt16(p + 4, make_uint4(__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7])));
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < 4; ++i)
       if (i < n) p[i] = f[i];
   }
 }
-FOG_DEVICE void store8(uint16_t* p, int n, uint4 w) {
-  if (n >= 8) st_any_nt16(p, w);
-  else st_upto8(p, w, n);
-}
-FOG_DEVICE void store_codes(uint8_t* p, int n, uint2 w) {
-  if (n >= 8) {
+FOG_DEVICE void store4(uint16_t* p, int n, uint2 w) {
+  if (n >= 4) {
     u32x2 v = {w.x, w.y};
-    __builtin_nontemporal_store(v, reinterpret_cast<u32x2_byte*>(p));
+    __builtin_nontemporal_store(v, reinterpret_cast<u32x2_half*>(p));
   } else {
-    st_upto8(p, w, n);
+    st_upto8(p, make_uint4(w.x, w.y, 0u, 0u), n);
   }
+}
+FOG_DEVICE void store_codes(uint8_t* p, int n, uint32_t w) {
+  if (n >= 4) __builtin_nontemporal_store(w, reinterpret_cast<u32_byte*>(p));
+  else st_upto8(p, make_uint2(w, 0u), n);
 }
 
 template <int FMT>
-FOG_DEVICE void decode8(uint2 q, float by, float (&f)[8]) {
-  f32x2 a, b, c, d;
+FOG_DEVICE void decode4(uint32_t q, float by, float (&f)[4]) {
+  f32x2 a, b;
   if (FMT == FOG_E4M3) {
-    a = __builtin_amdgcn_cvt_pk_f32_fp8((int)q.x, false); b = __builtin_amdgcn_cvt_pk_f32_fp8((int)q.x, true);
-    c = __builtin_amdgcn_cvt_pk_f32_fp8((int)q.y, false); d = __builtin_amdgcn_cvt_pk_f32_fp8((int)q.y, true);
+    a = __builtin_amdgcn_cvt_pk_f32_fp8((int)q, false); b = __builtin_amdgcn_cvt_pk_f32_fp8((int)q, true);
   } else {
-    a = __builtin_amdgcn_cvt_pk_f32_bf8((int)q.x, false); b = __builtin_amdgcn_cvt_pk_f32_bf8((int)q.x, true);
-    c = __builtin_amdgcn_cvt_pk_f32_bf8((int)q.y, false); d = __builtin_amdgcn_cvt_pk_f32_bf8((int)q.y, true);
+    a = __builtin_amdgcn_cvt_pk_f32_bf8((int)q, false); b = __builtin_amdgcn_cvt_pk_f32_bf8((int)q, true);
   }
   f[0] = a[0] * by; f[1] = a[1] * by; f[2] = b[0] * by; f[3] = b[1] * by;
-  f[4] = c[0] * by; f[5] = c[1] * by; f[6] = d[0] * by; f[7] = d[1] * by;
 }
 
-// Codes of a block's eight elements of this lane, and the block's scale byte.
+// Codes of this lane's four elements of a block, and the block's scale byte.
 template <int FMT>
-FOG_DEVICE uint2 encode8(const float (&x)[8], const uint32_t (&r)[8], uint32_t& byte) {
+FOG_DEVICE uint32_t encode4(const float (&x)[4], const uint32_t (&r)[4], uint32_t& byte) {
   uint32_t top = 0u;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < 4; ++i) {
     const uint32_t a = __float_as_uint(x[i]) & 0x7FFFFFFFu;
     top = top > a ? top : a;
   }
   const int k = block_exponent<FMT>(block_max(top));
   byte = (uint32_t)(127 - k);
   const float by = __uint_as_float((uint32_t)(127 + k) << 23);
-  float y[8];
+  float y[4];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < 4; ++i) {
     y[i] = round_by<FMT>(x[i] * by, r[i]);
     if (FMT == FOG_E5M2) y[i] = x[i] > 0.0f ? fmaxf(y[i], 1.52587890625e-05f) : y[i];     // the smallest code above zero
   }
-  return make_uint2(cvt4_fp8_finite<FMT>(y[0], y[1], y[2], y[3]), cvt4_fp8_finite<FMT>(y[4], y[5], y[6], y[7]));
+  return cvt4_fp8_finite<FMT>(y[0], y[1], y[2], y[3]);
 }
 
-template <bool FP8>
+__host__ __device__ static inline uint32_t step_key(uint64_t seed, uint64_t t) {
+  return next_key(next_key(next_key(next_key(0u, (uint32_t)seed), (uint32_t)(seed >> 32)), (uint32_t)t), (uint32_t)(t >> 32));
+}
+
+struct Tensor {
+  const void* g;
+  void *p, *m, *v;
+  float* master;
+  uint8_t *ms, *vs;
+  float keep, rate, root, c;
+  uint32_t high, low;      // of the random numbers
+  bool p32, g32;
+};
+
+// Four elements from element i of the tensor on, of which n are there (FULL: all).
+struct Four {
+  float g[4], m[4], v[4], p[4];
+};
+template <bool FP8, bool FULL>
+FOG_DEVICE void load_four(const Tensor& t, int64_t i, int n, Four& f) {
+  if (FULL) n = 4;
+  if (t.g32) load4(reinterpret_cast<const float*>(t.g) + i, n, f.g);
+  else load4(reinterpret_cast<const uint16_t*>(t.g) + i, n, f.g);
+  if (t.master) load4(t.master + i, n, f.p);
+  else if (t.p32) load4(reinterpret_cast<const float*>(t.p) + i, n, f.p);
+  else load4(reinterpret_cast<const uint16_t*>(t.p) + i, n, f.p);
+  if (FP8) {
+    decode4<FOG_E4M3>(load_codes(reinterpret_cast<const uint8_t*>(t.m) + i, n), __uint_as_float((uint32_t)t.ms[i >> 7] << 23), f.m);
+    decode4<FOG_E5M2>(load_codes(reinterpret_cast<const uint8_t*>(t.v) + i, n), __uint_as_float((uint32_t)t.vs[i >> 7] << 23), f.v);
+  } else {
+    load4(reinterpret_cast<const float*>(t.m) + i, n, f.m);
+    load4(reinterpret_cast<const float*>(t.v) + i, n, f.v);
+  }
+}
+template <bool FP8, bool FULL>
+FOG_DEVICE void step_four(const Tensor& t, const AdamStep& s, int64_t i, uint32_t at, int n, Four& f) {
+  if (FULL) n = 4;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float gc = f.g[e] * t.c;
+    f.m[e] = f.m[e] * s.beta1 + gc * s.beta1c;
+    f.v[e] = f.v[e] * s.beta2 + gc * gc * s.beta2c;
+    // Root and quotient by the hardware's instructions, a unit in the last place each.  A second moment below the smallest normal number counts as 0: beside
+    // an eps of 2^-38 and more its root, below 2^-63, does not show.  A smaller eps takes the correctly rounded forms, 25 instructions more.
+    const float d = s.plain_eps ? __builtin_amdgcn_sqrtf(f.v[e]) * t.root + s.eps : __builtin_sqrtf(f.v[e]) * t.root + s.eps;
+    const float u = s.plain_eps ? f.m[e] * t.rate * __builtin_amdgcn_rcpf(d) : f.m[e] * t.rate / d;
+    f.p[e] = f.p[e] * t.keep - u;
+  }
+  uint32_t r[4];
+  if (FP8 || (!t.master && !t.p32)) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r[e] = mix((at + (uint32_t)e) ^ t.high);
+  }
+  if (t.master) store4(t.master + i, n, f.p);
+  if (t.p32) {
+    store4(reinterpret_cast<float*>(t.p) + i, n, f.p);
+  } else {
+    uint2 w;
+    if (t.master) {
+      w = make_uint2(pack_bf16x2(f.p[0], f.p[1]), pack_bf16x2(f.p[2], f.p[3]));
+    } else {
+      // weights without a master copy: up where the sixteen places dropped, plus as many random bits, carry
+      uint32_t h[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) h[e] = f.p[e] != f.p[e] ? 0x7FC0u : (__float_as_uint(f.p[e]) + ((r[e] * 0x9E3779B1u) >> 16)) >> 16;
+      w = make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
+    }
+    store4(reinterpret_cast<uint16_t*>(t.p) + i, n, w);
+  }
+  if (FP8) {
+    uint32_t bm, bv;
+    const uint32_t qm = encode4<FOG_E4M3>(f.m, r, bm), qv = encode4<FOG_E5M2>(f.v, r, bv);
+    store_codes(reinterpret_cast<uint8_t*>(t.m) + i, n, qm);
+    store_codes(reinterpret_cast<uint8_t*>(t.v) + i, n, qv);
+    if ((threadIdx.x & 31) == 0) {
+      t.ms[i >> 7] = (uint8_t)bm;
+      t.vs[i >> 7] = (uint8_t)bv;
+    }
+  } else {
+    store4(reinterpret_cast<float*>(t.m) + i, n, f.m);
+    store4(reinterpret_cast<float*>(t.v) + i, n, f.v);
+  }
+}
+
+// U: fours in flight.
+template <bool FP8, int PIECE, int U>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(AdamBatch b, AdamStep s) {
-  float c = 1.0f;
+  Tensor t;
+  t.c = 1.0f;
   if (s.sumsq) {
     const double norm = __builtin_sqrt(*s.sumsq);
     if (!(norm < __builtin_inf())) return;               // not finite: the step is left out
-    if (norm > (double)s.max_norm) c = (float)((double)s.max_norm / norm);
+    if (norm > (double)s.max_norm) t.c = (float)((double)s.max_norm / norm);
   }
-  int64_t t = s.step_dev ? *s.step_dev : s.step;
-  if (t < 1) t = 1;
-  const double lr = s.lr_dev ? (double)*s.lr_dev : s.lr;
-  // 1 - beta^t without cancellation
-  const float rate = (float)(lr / -expm1((double)t * s.log_beta1)), root = (float)(1.0 / __builtin_sqrt(-expm1((double)t * s.log_beta2)));
-  uint32_t key = 0u;
-  key = next_key(key, (uint32_t)s.seed);
-  key = next_key(key, (uint32_t)(s.seed >> 32));
-  key = next_key(key, (uint32_t)t);
-  key = next_key(key, (uint32_t)((uint64_t)t >> 32));
+  double lr = s.lr;
+  uint32_t key = s.common.key;
+  t.rate = s.common.rate;
+  t.root = s.common.root;
+  if (s.lr_dev || s.step_dev) {
+    int64_t n = s.step_dev ? *s.step_dev : s.step;
+    if (n < 1) n = 1;
+    if (s.lr_dev) lr = (double)*s.lr_dev;
+    t.rate = (float)(lr / -expm1((double)n * s.log_beta1));        // 1 - beta^t without cancellation
+    t.root = (float)(1.0 / __builtin_sqrt(-expm1((double)n * s.log_beta2)));
+    key = step_key(s.seed, (uint64_t)n);
+  }
   for (int piece = blockIdx.x; piece < b.pieces; piece += gridDim.x) {
     const int j = tensor_of(b, piece);
     const int64_t at = (int64_t)(piece - b.first[j]) * PIECE;
     const int64_t left = b.n[j] - at;
     const int n = (int)(left < PIECE ? left : PIECE);
-    const bool p32 = b.p32[j] != 0, g32 = b.g32[j] != 0;
-    float* master = b.master[j];
-    const float keep = (float)(1.0 - lr * (double)b.decay[j]);
-    const uint32_t high = mix((uint32_t)((uint64_t)at >> 32) + next_key(key, (uint32_t)b.number[j]));
-    const uint32_t low = (uint32_t)at;
-    for (int i0 = 8 * (int)threadIdx.x; i0 < ((n + 127) & ~127); i0 += 8 * kThreads) {     // whole blocks: their lanes stay together
-      const int64_t i = at + i0;
-      const int k = n - i0 < 0 ? 0 : n - i0;
-      float g[8], m[8], v[8], p[8];
-      if (g32) load8(reinterpret_cast<const float*>(b.g[j]) + i, k, g);
-      else load8(reinterpret_cast<const uint16_t*>(b.g[j]) + i, k, g);
-      if (master) load8(master + i, k, p);
-      else if (p32) load8(reinterpret_cast<const float*>(b.p[j]) + i, k, p);
-      else load8(reinterpret_cast<const uint16_t*>(b.p[j]) + i, k, p);
-      if (FP8) {
-        decode8<FOG_E4M3>(load_codes(reinterpret_cast<const uint8_t*>(b.m[j]) + i, k), __uint_as_float((uint32_t)b.ms[j][i >> 7] << 23), m);
-        decode8<FOG_E5M2>(load_codes(reinterpret_cast<const uint8_t*>(b.v[j]) + i, k), __uint_as_float((uint32_t)b.vs[j][i >> 7] << 23), v);
-      } else {
-        load8(reinterpret_cast<const float*>(b.m[j]) + i, k, m);
-        load8(reinterpret_cast<const float*>(b.v[j]) + i, k, v);
-      }
+    t.g = b.g[j]; t.p = b.p[j]; t.m = b.m[j]; t.v = b.v[j]; t.master = b.master[j]; t.ms = b.ms[j]; t.vs = b.vs[j];
+    t.p32 = b.p32[j] != 0; t.g32 = b.g32[j] != 0;
+    t.keep = (float)(1.0 - lr * (double)b.decay[j]);
+    t.high = mix((uint32_t)((uint64_t)at >> 32) + next_key(key, (uint32_t)b.number[j]));
+    t.low = (uint32_t)at;
+    if (n == PIECE) {
+#pragma unroll 1
+      for (int i0 = 4 * (int)threadIdx.x; i0 < PIECE; i0 += 4 * kThreads * U) {
+        Four f[U];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float gc = g[e] * c;
-        m[e] = m[e] * s.beta1 + gc * s.beta1c;
-        v[e] = v[e] * s.beta2 + gc * gc * s.beta2c;
-        p[e] = p[e] * keep - m[e] * rate / (__builtin_sqrtf(v[e]) * root + s.eps);
-      }
-      uint32_t r[8];
-      if (FP8 || (!master && !p32)) {
+        for (int u = 0; u < U; ++u) load_four<FP8, true>(t, at + i0 + 4 * kThreads * u, 4, f[u]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) r[e] = mix((low + (uint32_t)(i0 + e)) ^ high);
+        for (int u = 0; u < U; ++u) step_four<FP8, true>(t, s, at + i0 + 4 * kThreads * u, t.low + (uint32_t)(i0 + 4 * kThreads * u), 4, f[u]);
       }
-      if (master) store8(master + i, k, p);
-      if (p32) {
-        store8(reinterpret_cast<float*>(b.p[j]) + i, k, p);
-      } else {
-        uint4 w;
-        if (master) {
-          w = make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7]));
-        } else {
-          // weights without a master copy: up where the sixteen places dropped, plus as many random bits, carry
-          uint32_t h[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) h[e] = p[e] != p[e] ? 0x7FC0u : (__float_as_uint(p[e]) + ((r[e] * 0x9E3779B1u) >> 16)) >> 16;
-          w = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
-        }
-        store8(reinterpret_cast<uint16_t*>(b.p[j]) + i, k, w);
-      }
-      if (FP8) {
-        uint32_t bm, bv;
-        const uint2 qm = encode8<FOG_E4M3>(m, r, bm), qv = encode8<FOG_E5M2>(v, r, bv);
-        store_codes(reinterpret_cast<uint8_t*>(b.m[j]) + i, k, qm);
-        store_codes(reinterpret_cast<uint8_t*>(b.v[j]) + i, k, qv);
-        if ((threadIdx.x & 15) == 0) {
-          b.ms[j][i >> 7] = (uint8_t)bm;
-          b.vs[j][i >> 7] = (uint8_t)bv;
-        }
-      } else {
-        store8(reinterpret_cast<float*>(b.m[j]) + i, k, m);
-        store8(reinterpret_cast<float*>(b.v[j]) + i, k, v);
+    } else {
+      const int whole = (n + 127) & ~127;                // whole blocks: their lanes stay together
+#pragma unroll 1
+      for (int i0 = 4 * (int)threadIdx.x; i0 < whole; i0 += 4 * kThreads) {
+        Four f;
+        load_four<FP8, false>(t, at + i0, n - i0, f);
+        step_four<FP8, false>(t, s, at + i0, t.low + (uint32_t)i0, n - i0, f);
       }
     }
   }
@@ -290,7 +354,7 @@ fog_status check_jobs(const fog_adamw_job* jobs, int count, bool fp8) {
     const fog_adamw_job& j = jobs[i];
     if (j.n < 0) return FOG_ERR_SHAPE;
     if ((j.p_type != FOG_BF16 && j.p_type != FOG_F32) || (j.g_type != FOG_BF16 && j.g_type != FOG_F32)) return FOG_ERR_UNSUPPORTED;
-    if (j.n > ((int64_t)1 << 37)) return FOG_ERR_UNSUPPORTED;      // a batch of such tensors has fewer than 2^31 pieces
+    if (j.n > ((int64_t)1 << 36)) return FOG_ERR_UNSUPPORTED;      // a batch of such tensors has fewer than 2^31 pieces
     if (!(std::fabs(j.weight_decay) <= FLT_MAX) || (j.master && j.p_type == FOG_F32)) return FOG_ERR_UNSUPPORTED;
     if (j.n == 0) continue;
     if (!j.p || !j.g || !j.m || !j.v || (fp8 && (!j.m_scale || !j.v_scale))) return FOG_ERR_NULL;
@@ -331,14 +395,21 @@ extern "C" fog_status fog_adamw(const fog_adamw_job* jobs, int count, fog_states
   s.lr_dev = lr_dev; s.step_dev = step_dev; s.sumsq = sumsq; s.step = step; s.seed = seed;
   s.beta1 = (float)beta1; s.beta1c = (float)(1.0 - beta1); s.beta2 = (float)beta2; s.beta2c = (float)(1.0 - beta2);
   s.eps = (float)eps; s.max_norm = max_norm;
+  s.plain_eps = eps >= 0x1p-38;
+  s.common = {0.0f, 0.0f, 0u};
+  if (!lr_dev && !step_dev)
+    s.common = {(float)(lr / -std::expm1((double)step * s.log_beta1)), (float)(1.0 / std::sqrt(-std::expm1((double)step * s.log_beta2))), step_key(seed, (uint64_t)step)};
   AdamBatch b;
+  const int64_t piece = fp8 ? FP8_PIECE : F32_PIECE;
   bool launched = false;
   b.count = b.pieces = 0;
   auto flush = [&]() {
     if (b.count == 0) return;
     const int groups = b.pieces < GROUPS ? b.pieces : GROUPS;
-    if (fp8) adamw_kernel<true><<<groups, kThreads, 0, (hipStream_t)stream>>>(b, s);
-    else     adamw_kernel<false><<<groups, kThreads, 0, (hipStream_t)stream>>>(b, s);
+    hipStream_t st = (hipStream_t)stream;
+    if (fp8)                   adamw_kernel<true, FP8_PIECE, 4><<<groups, kThreads, 0, st>>>(b, s);
+    else if (b.pieces <= MANY) adamw_kernel<false, F32_PIECE, 2><<<groups, kThreads, 0, st>>>(b, s);
+    else                       adamw_kernel<false, F32_PIECE, 1><<<groups, kThreads, ROOM, st>>>(b, s);
     launched = true;
     b.count = b.pieces = 0;
   };
@@ -350,7 +421,7 @@ extern "C" fog_status fog_adamw(const fog_adamw_job* jobs, int count, fog_states
     b.p[a] = j.p; b.g[a] = j.g; b.master[a] = j.master; b.m[a] = j.m; b.v[a] = j.v; b.ms[a] = j.m_scale; b.vs[a] = j.v_scale;
     b.n[a] = j.n; b.first[a] = b.pieces; b.number[a] = i; b.decay[a] = j.weight_decay;
     b.p32[a] = j.p_type == FOG_F32; b.g32[a] = j.g_type == FOG_F32;
-    b.pieces += (int)((j.n + PIECE - 1) / PIECE);
+    b.pieces += (int)((j.n + piece - 1) / piece);
   }
   flush();
   return launched ? fog_launch_status() : FOG_OK;

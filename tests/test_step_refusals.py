@@ -37,7 +37,7 @@ def adamw(lib, jobs=None, states=0, lr=1e-3, lr_dev=None, beta1=0.9, beta2=0.95,
     (ALIGN, dict(p=P + 1)), (ALIGN, dict(g=P + 1)), (ALIGN, dict(master=P + 2)), (ALIGN, dict(m=P + 2)), (ALIGN, dict(v=P + 1)),
     (ALIGN, dict(p=P + 2, p_type=F, master=None)), (ALIGN, dict(g=P + 2, g_type=F)),
     (UNSUPPORTED, dict(p_type=2)), (UNSUPPORTED, dict(g_type=-1)), (UNSUPPORTED, dict(p_type=F)), (UNSUPPORTED, dict(weight_decay=NAN)),
-    (UNSUPPORTED, dict(weight_decay=INF)), (UNSUPPORTED, dict(n=(1 << 37) + 1))])
+    (UNSUPPORTED, dict(weight_decay=INF)), (UNSUPPORTED, dict(n=(1 << 36) + 1))])
 def test_adamw_job(lib, status, change):
     assert adamw(lib, [job(**change)]) == status
     assert adamw(lib, [job(n=0), job(**change)]) == status
