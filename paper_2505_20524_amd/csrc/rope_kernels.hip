@@ -21,15 +21,28 @@ constexpr int JOBS = FOG_ROPE_JOBS_MAX;
 constexpr int HEADS_MAX = 1 << 24;
 
 struct Job {
-  fog_heads in, x, dx, q;                // in: x of the forward, dy of the backward; x, dx: backward only
+  fog_heads in, q;                       // in: x of the forward, dy of the backward
   const float* scale;
   int heads, first;                      // first: number of the job's first workgroup
   float gain;
   uint8_t rotate, e5m2;
 };
+struct Back {
+  fog_heads x, dx;
+};
+// (A launch costs the host by its arguments: for Q, K and V of a decoding step, room for eight jobs of both directions in 1.4 KB took 8.1 us a call, eight of one in
+// 0.9 KB 6.1.  So calls of up to FEW jobs have a form of their own.)
+constexpr int FEW = 4;
+template <bool GRAD, int N>
 struct Jobs {
-  Job job[JOBS];
+  Job job[N];
   int count;
+};
+template <int N>
+struct Jobs<true, N> {
+  Job job[N];
+  int count;
+  Back back[N];
 };
 struct Shape {
   const float* table;
@@ -42,7 +55,7 @@ struct Shape {
   int D, rot, segment, pos_bytes;        // segment: heads of a workgroup
   int side;                              // log2 of the tokens that a workgroup takes side by side; its other vectors are more of their heads
 };
-static_assert(sizeof(Jobs) + sizeof(Shape) <= 4096, "arguments of a launch");
+static_assert(sizeof(Jobs<true, JOBS>) + sizeof(Shape) <= 4096, "arguments of a launch");
 
 template <int CTRL>
 FOG_DEVICE float dpp_add(float s) {
@@ -153,8 +166,8 @@ FOG_DEVICE void turn(float (&a)[8], float (&b)[8], const float (&c)[8], const fl
   }
 }
 
-template <int LPR, bool INTER, bool GRAD, bool FULL>
-__global__ __launch_bounds__(kThreads) void rope_kernel(Jobs jobs, Shape sh) {
+template <int LPR, bool INTER, bool GRAD, bool FULL, int N>
+__global__ __launch_bounds__(kThreads) void rope_kernel(Jobs<GRAD, N> jobs, Shape sh) {
   constexpr int VECTORS = kThreads / LPR;       // of a workgroup at a time
   constexpr int U = GRAD ? 2 : 1;               // heads in flight
   int j = 0;
@@ -212,9 +225,17 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(Jobs jobs, Shape sh) {
     if (t >= sh.tokens) break;           // (whole vectors: their lanes leave together)
     const uint32_t b = t / sh.S, s = t - b * sh.S;
     const uint16_t* in = reinterpret_cast<const uint16_t*>(job.in.p) + b * job.in.batch + s * job.in.token;
-    const uint16_t* xin = GRAD && norm ? reinterpret_cast<const uint16_t*>(job.x.p) + b * job.x.batch + s * job.x.token : nullptr;
     uint8_t* q = job.q.p ? reinterpret_cast<uint8_t*>(job.q.p) + b * job.q.batch + s * job.q.token : nullptr;
-    uint16_t* dx = GRAD && job.dx.p ? reinterpret_cast<uint16_t*>(job.dx.p) + b * job.dx.batch + s * job.dx.token : nullptr;
+    const uint16_t* xin = nullptr;
+    uint16_t* dx = nullptr;
+    int64_t x_head = 0, dx_head = 0;
+    if constexpr (GRAD) {
+      const Back& back = jobs.back[j];
+      if (norm) xin = reinterpret_cast<const uint16_t*>(back.x.p) + b * back.x.batch + s * back.x.token;
+      if (back.dx.p) dx = reinterpret_cast<uint16_t*>(back.dx.p) + b * back.dx.batch + s * back.dx.token;
+      x_head = back.x.head;
+      dx_head = back.dx.head;
+    }
     bool there = true;
     float c[8], sn[8];
 #pragma unroll
@@ -245,7 +266,7 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(Jobs jobs, Shape sh) {
           va[u] = fetch<FULL>(p + offA, nA);
           vb[u] = fetch<FULL>(p + offB, nB);
           if (GRAD && norm) {
-            const uint16_t* x = xin + (h + u * slots) * job.x.head;
+            const uint16_t* x = xin + (h + u * slots) * x_head;
             xa[u] = fetch<FULL>(x + offA, nA);
             xb[u] = fetch<FULL>(x + offB, nB);
           }
@@ -332,7 +353,7 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(Jobs jobs, Shape sh) {
           const uint32_t larger = max_of_pair(most);
           top_bits = top_bits > larger ? top_bits : larger;
           if (dx) {
-            uint16_t* to = dx + (h + u * slots) * job.dx.head;
+            uint16_t* to = dx + (h + u * slots) * dx_head;
             store_half<FULL>(to + offA, wa, nA);
             store_half<FULL>(to + offB, wb, nB);
           }
@@ -460,7 +481,7 @@ fog_status check_call(int count, const void* jobs, int B, int S, int D, int rot,
 }
 
 template <bool GRAD>
-fog_status launch(Jobs& jobs, Shape& sh, float* const* amax, bool any_amax, int B, bool inter, void* workspace, hipStream_t s) {
+fog_status launch(Jobs<GRAD, JOBS>& jobs, Shape& sh, float* const* amax, bool any_amax, int B, bool inter, void* workspace, hipStream_t s) {
   const int lanes = (sh.rot / 2 + 7) / 8 + (sh.D - sh.rot + 15) / 16, plain = (sh.D + 15) / 16, need = lanes > plain ? lanes : plain;
   const int lpr = need <= 4 ? 4 : need <= 8 ? 8 : need <= 16 ? 16 : need <= 32 ? 32 : 64;
   // Whole runs of eight everywhere: no stretch (turned pairs, the rest) is shorter than one.
@@ -497,11 +518,22 @@ fog_status launch(Jobs& jobs, Shape& sh, float* const* amax, bool any_amax, int 
   for (int j = jobs.count; j <= JOBS; ++j) tops.first[j] = next;
   sh.part = any_amax ? reinterpret_cast<uint32_t*>(workspace) : nullptr;
   if (next > 0 && sh.tokens > 0 && sh.D > 0) {
-#define FOG_ROPE2(L, I, F) rope_kernel<L, I, GRAD, F><<<next, kThreads, 0, s>>>(jobs, sh)
-#define FOG_ROPE(L)                                             \
-  do {                                                          \
-    if (inter) { if (full) FOG_ROPE2(L, true, true); else FOG_ROPE2(L, true, false); }    \
-    else       { if (full) FOG_ROPE2(L, false, true); else FOG_ROPE2(L, false, false); }  \
+    Jobs<GRAD, FEW> few;
+    if (jobs.count <= FEW) {
+      few.count = jobs.count;
+      for (int j = 0; j < FEW; ++j) {
+        few.job[j] = jobs.job[j];
+        if constexpr (GRAD) few.back[j] = jobs.back[j];
+      }
+    }
+#define FOG_ROPE(L)                                                                                                        \
+  do {                                                                                                                     \
+    if (!full)                   { if (inter) rope_kernel<L, true, GRAD, false, JOBS><<<next, kThreads, 0, s>>>(jobs, sh);  \
+                                   else rope_kernel<L, false, GRAD, false, JOBS><<<next, kThreads, 0, s>>>(jobs, sh); }     \
+    else if (jobs.count <= FEW)  { if (inter) rope_kernel<L, true, GRAD, true, FEW><<<next, kThreads, 0, s>>>(few, sh);     \
+                                   else rope_kernel<L, false, GRAD, true, FEW><<<next, kThreads, 0, s>>>(few, sh); }        \
+    else                         { if (inter) rope_kernel<L, true, GRAD, true, JOBS><<<next, kThreads, 0, s>>>(jobs, sh);   \
+                                   else rope_kernel<L, false, GRAD, true, JOBS><<<next, kThreads, 0, s>>>(jobs, sh); }      \
   } while (0)
     if (lpr == 4) FOG_ROPE(4);
     else if (lpr == 8) FOG_ROPE(8);
@@ -509,7 +541,6 @@ fog_status launch(Jobs& jobs, Shape& sh, float* const* amax, bool any_amax, int 
     else if (lpr == 32) FOG_ROPE(32);
     else FOG_ROPE(64);
 #undef FOG_ROPE
-#undef FOG_ROPE2
   } else {
     for (int j = 0; j <= JOBS; ++j) tops.first[j] = 0;
     if (!any_amax) return FOG_OK;
@@ -542,7 +573,7 @@ extern "C" fog_status fog_rope_quantize(const fog_rope_job* jobs, int count, int
                                         void* stream) {
   const fog_status st = check_call(count, jobs, B, S, D, rot, layout, table, positions, pos, pos_bytes, offset);
   if (st != FOG_OK) return st;
-  Jobs all = {};
+  Jobs<false, JOBS> all = {};
   Call call;
   float* amax[JOBS] = {};
   bool any_amax = false;
@@ -578,7 +609,7 @@ extern "C" fog_status fog_rope_grad(const fog_rope_grad_job* jobs, int count, in
                                     int64_t positions, const void* pos, int pos_bytes, int64_t offset, void* workspace, size_t workspace_bytes, void* stream) {
   const fog_status st = check_call(count, jobs, B, S, D, rot, layout, table, positions, pos, pos_bytes, offset);
   if (st != FOG_OK) return st;
-  Jobs all = {};
+  Jobs<true, JOBS> all = {};
   Call call;
   float* amax[JOBS] = {};
   bool any_amax = false;
@@ -600,7 +631,7 @@ extern "C" fog_status fog_rope_grad(const fog_rope_grad_job* jobs, int count, in
       if (s != FOG_OK) return s;
     }
     Job& to = all.job[j];
-    to.in = in.dy; to.x = in.x; to.dx = in.dx; to.q = in.q; to.scale = in.scale; to.heads = empty ? 0 : in.heads; to.gain = in.gain;
+    to.in = in.dy; all.back[j] = {in.x, in.dx}; to.q = in.q; to.scale = in.scale; to.heads = empty ? 0 : in.heads; to.gain = in.gain;
     to.rotate = in.rotate && rot > 0; to.e5m2 = in.fmt == FOG_E5M2;
     amax[j] = in.amax;
     any_amax |= in.amax != nullptr;

@@ -1,0 +1,310 @@
+"""GPU: a whole training step of one block from the library's calls alone, products and what lies between them: forward, backward, the gradients' norm and the update.
+Against float64 autograd of the block without casts, the new operators stage by stage, in a captured graph, and on two streams at once."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import bf16, fp8, grads, rope
+from paper_2505_20524_amd import fog
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+BF = torch.bfloat16
+
+
+def u8(*shape):
+    return torch.zeros(shape, dtype=torch.uint8, device="cuda")
+
+
+def half(*shape):
+    return torch.zeros(shape, dtype=BF, device="cuda")
+
+
+def f32(*shape):
+    return torch.zeros(shape, device="cuda")
+
+
+class Cast:
+    """Codes of a tensor with the scale that its abs-max of the last step gives."""
+
+    def __init__(self, fmt, *shape):
+        self.fmt, self.q, self.amax, self.scale, self.inv = fmt, u8(*shape), f32(1), torch.ones(1, device="cuda"), torch.ones(1, device="cuda")
+
+    def next(self, stream):
+        fog.scale(self.amax, self.fmt, self.scale, self.inv, stream=stream)
+
+    def value(self):
+        return fp8.decode(self.q.cpu().numpy(), self.fmt) / float(self.scale.item())
+
+
+class Block:
+    """x1 = x0 + norm(attention(x0)), x2 = x1 + norm(feed-forward(x1)), loss = <x2, G>; grouped queries, QK norm, rotary positions, xIELU."""
+
+    def __init__(self, seed, B=2, S=128, hidden=256, H=4, Hkv=2, inner=512, states=fog.STATES_F32):
+        g = torch.Generator(device="cuda")
+        g.manual_seed(seed)
+        D, T, W = 128, B * S, (H + 2 * Hkv) * 128
+        self.gen, self.B, self.S, self.T, self.H, self.Hkv, self.D, self.hidden, self.inner, self.width = g, B, S, T, H, Hkv, D, hidden, inner, W
+        self.soft, self.alpha = 1.0 / math.sqrt(D), (0.8, 0.6)
+        shapes = {"qkv": (W, hidden), "o": (hidden, H * D), "up": (inner, hidden), "down": (hidden, inner)}
+        normal = lambda std, *s: torch.randn(s, device="cuda", generator=g) * std  # noqa: E731
+        self.master = {k: normal(1.0 / math.sqrt(s[1]), *s) for k, s in shapes.items()}
+        self.w = {k: m.to(BF) for k, m in self.master.items()}
+        self.wq, self.wjit = {k: Cast(fog.E4M3, *s) for k, s in shapes.items()}, u8(fog.quantize_jit_workspace())
+        self.gamma = {k: torch.rand(hidden, device="cuda", generator=g) + 0.5 for k in (1, 2)}
+        self.x0, self.G = half(T, hidden), half(T, hidden)
+        self.new_batch()
+        self.table = f32(S, D)
+        fog.rope_table(self.table)
+        heads = {"q": H, "k": Hkv, "v": Hkv}
+        # forward
+        self.x0q, self.x1q, self.aq, self.Oq = Cast(fog.E4M3, T, hidden), Cast(fog.E4M3, T, hidden), Cast(fog.E4M3, T, inner), Cast(fog.E4M3, B, S, H, D)
+        self.qkv, self.y1, self.x1, self.u, self.y2, self.x2 = half(T, W), half(T, hidden), half(T, hidden), half(T, inner), half(T, hidden), half(T, hidden)
+        self.hq = {k: Cast(fog.E4M3, B, n, S, D) for k, n in heads.items()}
+        self.O, self.lse, self.rho_p, self.rho_ds, self.amax_ds = half(B, H, S, D), f32(B, H, S), torch.full((1,), 448.0, device="cuda"), torch.ones(1, device="cuda"), f32(1)
+        # backward
+        self.dy2, self.du, self.dy1 = Cast(fog.E5M2, T, hidden), Cast(fog.E5M2, T, inner), Cast(fog.E5M2, T, hidden)
+        self.dO8, self.dqkv = Cast(fog.E5M2, B, H, S, D), Cast(fog.E5M2, B, S, W)
+        self.da, self.dx1b, self.G1, self.dOt, self.dO, self.dx0b = half(T, inner), half(T, hidden), half(T, hidden), half(T, H * D), half(B, H, S, D), half(T, hidden)
+        self.dh = {k: half(B, n, S, D) for k, n in heads.items()}
+        self.dw, self.dgamma, self.dalpha = {k: half(*s) for k, s in shapes.items()}, {k: f32(hidden) for k in (1, 2)}, f32(2)
+        at, first, view = {}, 0, lambda t: t.view(B, S, H + 2 * Hkv, D)  # noqa: E731
+        for k, n in heads.items():
+            at[k], first = slice(first, first + n), first + n
+        gain = {"q": 1.0, "k": 1.0, "v": 0.0}
+        self.rope = fog.make_rope_jobs([dict(x=view(self.qkv)[:, :, at[k]], q=c.q.transpose(1, 2), scale=c.scale, amax=c.amax, gain=gain[k], rotate=k != "v")
+                                        for k, c in self.hq.items()])
+        self.rope_back = fog.make_rope_grad_jobs([dict(dy=self.dh[k].transpose(1, 2), x=view(self.qkv)[:, :, at[k]], q=view(self.dqkv.q)[:, :, at[k]], scale=self.dqkv.scale,
+                                                       amax=self.dqkv.amax, gain=gain[k], rotate=k != "v") for k in heads])
+        # attention's result to the next projection's operand and its gradient back: the change of layout with the cast, without positions
+        self.o_out = fog.make_rope_jobs([dict(x=self.O.transpose(1, 2), q=self.Oq.q, scale=self.Oq.scale, amax=self.Oq.amax, rotate=False)])
+        self.o_back = fog.make_rope_grad_jobs([dict(dy=self.dOt.view(B, S, H, D), dx=self.dO.transpose(1, 2), q=self.dO8.q.transpose(1, 2), scale=self.dO8.scale,
+                                                    amax=self.dO8.amax, rotate=False)])
+        need = [fog.fp8_gemm_workspace(*a) for n, k in shapes.values() for a in ((fog.NT, T, n, k), (fog.NN, T, k, n), (fog.TN, n, k, T))]
+        self.ws = u8(max(need + [fog.rope_workspace(), fog.postnorm_residual_grad_workspace(T, hidden), fog.act_grad_workspace(), fog.fp8_attn_workspace(B, H, S, D, True, H_kv=Hkv)]))
+        # update
+        self.grads = [*self.dw.values(), *self.dgamma.values()]
+        self.norm_jobs, self.sumsq, self.ws_norm = fog.make_grad_jobs(self.grads), torch.zeros(1, dtype=torch.float64, device="cuda"), u8(fog.grad_sumsq_workspace(len(self.grads)))
+        self.step, self.state = torch.zeros(1, dtype=torch.int64, device="cuda"), []
+        items = []
+        for k, m in list(self.master.items()) + list(self.gamma.items()):
+            n, weights = m.numel(), k in self.w
+            st = dict(m=f32(n), v=f32(n)) if states == fog.STATES_F32 else dict(m=u8(n), v=u8(n), m_scale=u8(-(-n // 128)), v_scale=u8(-(-n // 128)))
+            self.state.append(st)
+            items.append(dict(st, p=self.w[k] if weights else m, master=m if weights else None, g=self.dw[k] if weights else self.dgamma[k], weight_decay=0.1 if weights else 0.0))
+        self.jobs = fog.make_adamw_jobs(items)
+        self.casts = [self.x1q, self.aq, self.Oq, *self.hq.values(), self.dy2, self.du, self.dy1, self.dO8, self.dqkv]
+
+    def new_batch(self):
+        self.x0.copy_(torch.randn(self.x0.shape, device="cuda", generator=self.gen))
+        self.G.copy_(torch.randn(self.G.shape, device="cuda", generator=self.gen) * 1e-3)
+
+    def gemm(self, layout, a, b, out, stream):
+        M, N = out.shape
+        two = lambda c: c.q.view(-1, c.q.shape[-1]) if c.q.dim() == 2 or c is self.dqkv else c.q.view(self.T, -1)  # noqa: E731
+        A, Bm = two(a), two(b)
+        K = A.shape[0] if layout == fog.TN else A.shape[1]
+        fog.fp8_gemm(layout, M, N, K, A, a.fmt, a.inv, Bm, b.fmt, b.inv, out, workspace=self.ws, stream=stream)
+
+    def passes(self, stream=None):
+        """Forward and backward."""
+        k, w, E4 = dict(stream=stream), self.wq, fog.E4M3
+        jit = lambda x, c: fog.quantize_jit(x, E4, c.amax, c.scale, c.inv, self.wjit, q=c.q, **k)  # noqa: E731
+        for n in self.w:
+            jit(self.w[n], w[n])
+        jit(self.x0, self.x0q)
+        self.gemm(fog.NT, self.x0q, w["qkv"], self.qkv, stream)
+        fog.rope_quantize(self.rope, self.table, self.ws, **k)
+        h = self.hq
+        attn = (self.B, self.H, self.S, self.D, self.soft, True, h["q"].q, h["k"].q, h["v"].q, h["q"].inv, h["k"].inv, h["v"].inv)
+        fog.fp8_attn_fwd(*attn, self.rho_p, self.O, self.lse, H_kv=self.Hkv, **k)
+        fog.rope_quantize(self.o_out, None, self.ws, **k)
+        self.gemm(fog.NT, self.Oq, w["o"], self.y1, stream)
+        fog.postnorm_residual_quantize(self.x0, self.y1, self.gamma[1], E4, self.x1q.scale, self.x1, q=self.x1q.q, amax_out=self.x1q.amax, **k)
+        self.gemm(fog.NT, self.x1q, w["up"], self.u, stream)
+        fog.xielu_quantize(self.u, *self.alpha, E4, self.aq.scale, self.aq.q, amax_out=self.aq.amax, **k)
+        self.gemm(fog.NT, self.aq, w["down"], self.y2, stream)
+        fog.postnorm_residual_quantize(self.x1, self.y2, self.gamma[2], E4, self.rho_p, self.x2, **k)
+
+        def back(dres, y, which, cast, **more):
+            fog.postnorm_residual_grad(dres, y, self.gamma[which], fog.E5M2, cast.scale, self.dgamma[which], self.ws, q=cast.q, amax_out=cast.amax, **more, **k)
+        back(self.G, self.y2, 2, self.dy2)
+        self.gemm(fog.NN, self.dy2, w["down"], self.da, stream)
+        self.gemm(fog.TN, self.dy2, self.aq, self.dw["down"], stream)
+        fog.xielu_grad(self.u, self.da, *self.alpha, fog.E5M2, self.du.scale, self.ws, q=self.du.q, amax_out=self.du.amax, dalpha=self.dalpha, **k)
+        self.gemm(fog.NN, self.du, w["up"], self.dx1b, stream)
+        self.gemm(fog.TN, self.du, self.x1q, self.dw["up"], stream)
+        back(self.G, self.y1, 1, self.dy1, dbranch=self.dx1b, dstream=self.G1)
+        self.gemm(fog.NN, self.dy1, w["o"], self.dOt, stream)
+        self.gemm(fog.TN, self.dy1, self.Oq, self.dw["o"], stream)
+        fog.rope_grad(self.o_back, None, self.ws, **k)
+        fog.fp8_attn_bwd(*attn, self.O, self.dO, self.dO8.q, self.dO8.inv, self.lse, self.rho_p, self.rho_ds, self.dh["q"], self.dh["k"], self.dh["v"], amax_ds=self.amax_ds,
+                         workspace=self.ws, H_kv=self.Hkv, **k)
+        fog.rope_grad(self.rope_back, self.table, self.ws, **k)
+        self.gemm(fog.NN, self.dqkv, w["qkv"], self.dx0b, stream)
+        self.gemm(fog.TN, self.dqkv, self.x0q, self.dw["qkv"], stream)
+
+    def scales(self, stream=None):
+        """Delayed scaling with a history of one: the next step's scales from this step's maxima."""
+        for c in self.casts:
+            c.next(stream)
+        fog.scale(self.amax_ds, fog.E5M2, self.rho_ds, None, stream=stream)
+
+    def update(self, stream=None):
+        fog.grad_sumsq(self.norm_jobs, self.sumsq, self.ws_norm, stream=stream)
+        fog.adamw(self.jobs, 1e-3, self.step, seed=17, sumsq=self.sumsq, max_norm=0.05, stream=stream)
+
+    def run(self, stream=None):
+        self.passes(stream)
+        self.update(stream)
+        self.scales(stream)
+
+    def outputs(self):
+        return [t.clone() for t in [self.x2, self.dx0b, self.G1, self.dalpha, self.sumsq, *self.grads, *self.master.values(), *self.w.values(), *self.gamma.values(),
+                                    *[t for s in self.state for t in s.values()], *[c.scale for c in self.casts]]]
+
+
+def reference(b):
+    """float64 autograd of the same block without any cast."""
+    d = lambda t: t.detach().double().cpu()  # noqa: E731
+    w = {k: d(t).requires_grad_() for k, t in b.w.items()}
+    gamma = {k: d(t).requires_grad_() for k, t in b.gamma.items()}
+    alpha = torch.tensor(b.alpha, dtype=torch.float64, requires_grad=True)
+    x0 = d(b.x0).requires_grad_()
+    B, S, H, Hkv, D = b.B, b.S, b.H, b.Hkv, b.D
+    rms = lambda x: x / x.square().mean(-1, keepdim=True).sqrt()  # noqa: E731
+    qkv = (x0 @ w["qkv"].t()).view(B, S, H + 2 * Hkv, D).transpose(1, 2)
+    M = torch.from_numpy(np.stack([rope.matrix(r, D, rope.HALF) for r in rope.table(range(S), D)]))
+    turn = lambda x: torch.einsum("bhsd,sed->bhse", rms(x), M)  # noqa: E731
+    q, k, v = turn(qkv[:, :H]), turn(qkv[:, H:H + Hkv]), qkv[:, H + Hkv:]
+    k, v = (t.repeat_interleave(H // Hkv, 1) for t in (k, v))
+    score = (q @ k.transpose(2, 3)) * b.soft
+    score = score.masked_fill(torch.ones(S, S, dtype=torch.bool).triu(1), -math.inf)
+    y1 = (torch.softmax(score, -1) @ v).transpose(1, 2).reshape(B * S, H * D) @ w["o"].t()
+    x1 = x0 + gamma[1] * rms(y1)
+    u = x1 @ w["up"].t()
+    a = torch.where(u > 0, alpha[0] * u * u + 0.5 * u, alpha[1] * (torch.expm1(u.clamp(max=0)) - u) + 0.5 * u)
+    x2 = x1 + gamma[2] * rms(a @ w["down"].t())
+    (x2 * d(b.G)).sum().backward()
+    return x2.detach(), x0.grad, {k: t.grad for k, t in w.items()}, {k: t.grad for k, t in gamma.items()}, alpha.grad
+
+
+def check_e5m2(got, want, cast):
+    """Codes' values against what was cast: half a step, and what the rounding to bfloat16 in between moves it (2^-8 of a value, of which a step is a quarter to an eighth).
+    Under the scale of the last step's maximum the largest values saturate."""
+    scale = float(cast.scale.item())
+    want = np.clip(want * scale, -57344.0, 57344.0)
+    step = np.maximum(np.exp2(np.floor(np.log2(np.maximum(np.abs(want), 1e-300)))) * 0.25, 2.0 ** -16)
+    assert np.all(np.abs(got * scale - want) <= (0.5 + 2.0 ** -5) * step)
+
+
+def off(got, want):
+    got, want = got.double().cpu(), want.double()
+    return float((got - want).norm() / want.norm())
+
+
+def test_gradients_of_the_whole_block():
+    """A cast to E4M3 moves a tensor by some 2.6 % of its norm (a rounding error that is even over half a step of 2^-4 to 2^-3 of a value), one to E5M2 by 5.2 %; the forward
+    result goes through 9 casts, the first projection's gradient through those and 9 more (6 of them to E5M2).  As if independent: 8 % and 16 %.  Held to twice that."""
+    b = Block(1)
+    b.passes()
+    b.scales()
+    b.passes()
+    torch.cuda.synchronize()
+    x2, dx0, dw, dgamma, dalpha = reference(b)
+    forward, backward = 2 * math.sqrt(9) * 0.026, 2 * math.sqrt(12 * 0.026 ** 2 + 6 * 0.052 ** 2)
+    assert off(b.x2, x2) < forward
+    assert off(b.G1.float() + b.dx0b.float(), dx0) < backward
+    for k in dw:
+        assert off(b.dw[k], dw[k]) < backward, k
+    for k in dgamma:
+        assert off(b.dgamma[k], dgamma[k]) < backward, k
+    # sums of T * inner terms of either sign, of which the errors keep their share: by the terms' norm
+    assert off(b.dalpha, dalpha) < 1.0
+
+
+def test_every_stage_between_the_products():
+    """Each operator on the tensors as they occur, against the oracle."""
+    b = Block(2)
+    for _ in range(2):
+        b.run()
+        b.new_batch()
+    b.passes()
+    torch.cuda.synchronize()
+    h64 = lambda t: t.double().cpu().numpy()  # noqa: E731
+    B, S, H, Hkv, D = b.B, b.S, b.H, b.Hkv, b.D
+    x, first, tab, pos = h64(b.qkv).reshape(B, S, H + 2 * Hkv, D), 0, h64(b.table), np.arange(S)[None].repeat(B, 0)
+    dx = np.zeros_like(x)
+    for k, n in (("q", H), ("k", Hkv), ("v", Hkv)):
+        part = x[:, :, first:first + n]
+        on, gain = (tab, 1.0) if k != "v" else (None, 0.0)
+        y, size = rope.forward(part, on, pos, rope.HALF, gain)
+        s = float(b.hq[k].scale.item())
+        e = 19.2 * U * size if gain else 0.0
+        lo, hi = (fp8.decode(fp8.encode_sat(((y + d) * s).astype(np.float32), fp8.E4M3), fp8.E4M3) for d in (-e, e))
+        got = fp8.decode(b.hq[k].q.cpu().numpy(), fp8.E4M3).transpose(0, 2, 1, 3)
+        assert np.all((got >= lo) & (got <= hi)), k
+        dy = h64(b.dh[k]).transpose(0, 2, 1, 3)
+        dx[:, :, first:first + n] = rope.backward(dy, part if gain else None, on, pos, rope.HALF, gain)[0]
+        first += n
+    check_e5m2(b.dqkv.value().reshape(x.shape), dx, b.dqkv)
+    assert np.array_equal(b.Oq.q.cpu().numpy(), fp8.encode_sat(h64(b.O).transpose(0, 2, 1, 3).astype(np.float32) * np.float32(b.Oq.scale.item()), fp8.E4M3))
+    assert torch.equal(b.dO.transpose(1, 2).reshape(b.T, -1), b.dOt)
+    for G, y, which, cast in ((b.G1, b.y1, 1, b.dy1), (b.G, b.y2, 2, b.dy2)):
+        dy, dgamma, _, terms = grads.postnorm(h64(G), h64(y), h64(b.gamma[which]))
+        check_e5m2(cast.value(), dy, cast)
+        assert np.all(np.abs(h64(b.dgamma[which]) - dgamma) <= 100 * U * terms)
+    assert np.array_equal(h64(b.G1), bf16.f64_round((h64(b.G).astype(np.float32) + h64(b.dx1b).astype(np.float32)).astype(np.float64)))
+    s, _, (g0, g1) = grads.xielu(h64(b.u), *[float(np.float32(a)) for a in b.alpha])
+    check_e5m2(b.du.value(), h64(b.da) * s, b.du)
+    for got, g in zip(b.dalpha.tolist(), (g0, g1)):
+        assert abs(got - (h64(b.da) * g).sum()) <= 80 * U * np.abs(h64(b.da) * g).sum()
+
+
+@pytest.mark.parametrize("states", [fog.STATES_F32, fog.STATES_FP8])
+def test_steps_in_a_graph(states):
+    """Whole steps, the update's number and the scales among them, captured once and replayed on new batches with eager work between: the eager steps' bits."""
+    a, c = Block(3, states=states), Block(3, states=states)
+    for b in (a, c):
+        b.step.fill_(1)
+        b.run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.step.add_(1)
+        c.run()
+    for i in range(4):
+        for b in (a, c):
+            b.new_batch()
+        a.step.add_(1)
+        a.run()
+        torch.cuda.synchronize()
+        c.x2.fill_(3.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, want in zip(c.outputs(), a.outputs()):
+            assert torch.equal(got, want), i
+    assert a.step.item() == 5 and all(bool(torch.isfinite(t).all()) for t in a.master.values())
+
+
+def test_steps_on_two_streams():
+    blocks, want = [Block(4), Block(5, B=1, S=192, H=2, Hkv=1)], []
+    alone = [Block(4), Block(5, B=1, S=192, H=2, Hkv=1)]
+    for b in alone:
+        for t in range(1, 4):
+            b.step.fill_(t)
+            b.run()
+        want.append(b.outputs())
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in blocks]
+    for t in range(1, 4):
+        for b, s in zip(blocks, streams):
+            with torch.cuda.stream(s):
+                b.step.fill_(t)
+            b.run(stream=s)
+    torch.cuda.synchronize()
+    for b, w in zip(blocks, want):
+        assert all(torch.equal(x, y) for x, y in zip(b.outputs(), w))
