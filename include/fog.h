@@ -256,7 +256,8 @@ fog_status fog_rmsnorm_quantize(const void* x_bf16, int64_t rows, int64_t cols, 
  *   table : [positions, rot] floats, a row the cosines of the pairs, then their sines: fog_rope_table, or any other.  c^2 + s^2 need not be 1.
  *   pos : B * S positions of pos_bytes (4 or 8) bytes, signed; NULL: token s of every sequence has position offset + s.  A token whose position is no row of the
  *         table (padding) has y = 0 in the jobs that are turned.
- *   D up to FOG_ROPE_DIM_MAX, rot even, up to D; rows of any alignment.  Multiples of 16 for both, with a 16-byte aligned table, are the fastest.
+ *   D up to FOG_ROPE_DIM_MAX, rot even, up to D (0: nothing is turned and positions are not looked at); vectors of any alignment.  Stretches (the turned pairs, the
+ *         rest of a vector) of eight elements and more are the fastest.
  *   workspace : fog_rope_workspace() bytes (64 KB), 4-byte aligned, where a job has an amax; contents on entry do not matter.  Calls that may overlap in
  *         time need a workspace each.
  * Errors: NULL, SHAPE (count, sizes, strides), ALIGN, WORKSPACE, UNSUPPORTED (format, layout, odd rot, D, B * S above 2^31 - 1, heads above 2^24, pos_bytes, gain
@@ -267,7 +268,9 @@ fog_status fog_rmsnorm_quantize(const void* x_bf16, int64_t rows, int64_t cols, 
  * rounded once to bfloat16.  dx receives it, q its cast (of the ROUNDED value, as fog_quantize of a stored dx would give); either may have p == NULL.
  * amax = max |dx|, the rounded.  Padding has dx = 0 where it is turned.  Jobs that write ranges of one matrix (the gradient of the projection's result, one operand of
  * its products) name one scale and one amax.
- * A sum of squares is held in binary32: vectors beyond 10^18 lose their norm, in either direction.
+ * An input may repeat (strides of 0); the gradient of each of its appearances is one of its own.  Jobs without positions and norm change the layout alone, with the
+ * cast: attention's result into the next projection's operand, that projection's gradient into attention's.
+ * A sum of squares is held in binary32: vectors beyond 10^18 lose their norm in either direction, vectors below 10^-22 count as zeros.
  */
 #define FOG_ROPE_JOBS_MAX 8
 #define FOG_ROPE_DIM_MAX 1008
@@ -397,7 +400,7 @@ fog_status fog_postnorm_residual_quantize(const void* x_bf16, int64_t ldx, const
  *   amax_out : NULL or one float, overwritten.
  *   workspace : fog_postnorm_residual_grad_workspace(rows, cols) bytes, 4-byte aligned, where dgamma or amax_out is given; contents on entry do not matter.  Calls
  *             that may overlap in time need a workspace each.
- * Rows of any alignment, up to 32768 columns.  A sum of squares is held in binary32: rows beyond 10^18 lose their norm, as in the forward.
+ * Rows of any alignment, up to 32768 columns.  A sum of squares is held in binary32: rows beyond 10^18 lose their norm, as in the forward; rows below 10^-22 count as zeros.
  * Errors: NULL, SHAPE, ALIGN, WORKSPACE, UNSUPPORTED (format, cols, results that meet an input or each other).
  */
 fog_status fog_postnorm_residual_grad(const void* dres_bf16, int64_t ld_dres, const void* dbranch_bf16, int64_t ld_dbranch, const void* y_bf16,

@@ -414,10 +414,9 @@ __global__ __launch_bounds__(kThreads) void rope_top_kernel(Tops t, const uint32
 }
 
 // cos and sin of every position and pair from binary64 angles: far positions turn 10^5 times and more.  A thread keeps its pair's frequency for
-// sixteen positions.
+// sixteen positions and more.
 constexpr int TABLE_ROWS = 64;
 __global__ __launch_bounds__(kThreads) void rope_table_kernel(fog_rope_scaling sc, int64_t first, int64_t positions, int half, float* __restrict__ table) {
-  const int64_t p0 = (int64_t)blockIdx.x * TABLE_ROWS;
   for (int i = threadIdx.x & 63; i < half; i += 64) {
     double f = exp2(-(double)i / (double)half * log2(sc.base));
     if (sc.factor != 1.0) {
@@ -428,14 +427,15 @@ __global__ __launch_bounds__(kThreads) void rope_table_kernel(fog_rope_scaling s
       }
       f = f * ((1.0 - keep) / sc.factor + keep);
     }
-    for (int r = threadIdx.x >> 6; r < TABLE_ROWS; r += kThreads / 64) {
-      if (p0 + r >= positions) break;
-      double s, c;
-      sincos((double)(first + p0 + r) * f, &s, &c);
-      float* row = table + (p0 + r) * 2 * half;
-      row[i] = (float)(c * sc.amplitude);
-      row[half + i] = (float)(s * sc.amplitude);
-    }
+    for (int64_t p0 = (int64_t)blockIdx.x * TABLE_ROWS; p0 < positions; p0 += (int64_t)gridDim.x * TABLE_ROWS)
+      for (int r = threadIdx.x >> 6; r < TABLE_ROWS; r += kThreads / 64) {
+        if (p0 + r >= positions) break;
+        double s, c;
+        sincos((double)(first + p0 + r) * f, &s, &c);
+        float* row = table + (p0 + r) * 2 * half;
+        row[i] = (float)(c * sc.amplitude);
+        row[half + i] = (float)(s * sc.amplitude);
+      }
   }
 }
 
@@ -562,7 +562,8 @@ extern "C" fog_status fog_rope_table(const fog_rope_scaling* scaling, int64_t fi
   if (positions == 0 || rot == 0) return FOG_OK;
   if (!table) return FOG_ERR_NULL;
   if (reinterpret_cast<uintptr_t>(table) & 3) return FOG_ERR_ALIGN;
-  rope_table_kernel<<<(int)((positions + TABLE_ROWS - 1) / TABLE_ROWS), kThreads, 0, (hipStream_t)stream>>>(sc, first, positions, rot / 2, table);
+  const int64_t blocks = (positions + TABLE_ROWS - 1) / TABLE_ROWS;
+  rope_table_kernel<<<(int)(blocks < (1 << 20) ? blocks : 1 << 20), kThreads, 0, (hipStream_t)stream>>>(sc, first, positions, rot / 2, table);
   return fog_launch_status();
 }
 

@@ -323,6 +323,8 @@ def make_rope_grad_jobs(items):
 
 def _rope(name, jobs, table, workspace, layout, positions, offset, stream):
     rows, rot = (0, 0) if table is None else table.shape
+    if table is None and any(job.rotate for job in jobs):
+        raise ValueError("a table is needed: without one, nothing is turned (rotate=False)")
     if table is not None and (table.dtype != torch.float32 or not table.is_contiguous()):
         raise ValueError("table: a contiguous float32 matrix is needed, got %s with strides %s" % (table.dtype, table.stride()))
     B, S, D = jobs.shape or (0, 0, rot)

@@ -174,6 +174,19 @@ def test_postnorm_rows_of_zeros_and_of_nan():
     assert bool(torch.isnan(n.dgamma).all())            # x / NaN: every column of the row
 
 
+@pytest.mark.parametrize("value", [1e-30, 1e-23, 3e17])
+def test_postnorm_of_very_short_and_long_rows(value):
+    n = Norm(16, 20, 700)
+    n.y.mul_(value)
+    n.y[3, 5], n.y[4] = 0.0, 0.0
+    n.run()
+    assert bool(torch.isfinite(n.dy).all()) and bool(torch.isfinite(n.dgamma).all()) and math.isfinite(n.amax.item())
+    if value == 1e-30:
+        assert bool((n.dy == 0).all()) and bool((n.dgamma == 0).all())
+    if value == 3e17:
+        n.check()
+
+
 @pytest.mark.parametrize("rows,cols", [(0, 300), (5, 0), (0, 0)])
 def test_postnorm_of_nothing(rows, cols):
     n = Norm(14, rows, cols)

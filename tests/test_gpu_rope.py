@@ -377,6 +377,26 @@ def test_a_step_in_a_graph_and_on_two_streams():
         assert all(torch.equal(a, b) for a, b in zip(x.outputs(), w))
 
 
+@pytest.mark.parametrize("value", [1e-20, 1e-23, 1e-30, 3e17])
+def test_very_short_and_long_vectors(value):
+    """A norm whose squares still show, and vectors whose squares vanish: zeros in both directions, no infinity and no NaN beside them."""
+    x, q, amax, dx = (normal(16, 2, 5, 2, 128).double() * value).bfloat16(), u8(2, 5, 2, 128), one(-1), normal(0, 2, 5, 2, 128)
+    x[0, 0, 0, 3], x[0, 1] = 0.0, 0.0
+    table = make_table(5, 128)
+    fog.rope_quantize(fog.make_rope_jobs([dict(x=x, q=q, scale=one(1e9 if value == 1e-30 else 30.0), amax=amax, gain=1.0)]), table, room())
+    assert math.isfinite(amax.item()) and not np.isnan(fp8.decode(q.cpu().numpy(), fog.E4M3)).any()
+    dy = normal(17, 2, 5, 2, 128)
+    fog.rope_grad(fog.make_rope_grad_jobs([dict(dy=dy, x=x, dx=dx, amax=amax, gain=1.0)]), table, room())
+    assert bool(torch.isfinite(dx).all())
+    if value in (3e17, 1e-30):
+        y, _ = rope.forward(h64(x), h64(table), pos_of(2, 5, None), fog.HALF, 1.0)
+        got = fp8.decode(q.cpu().numpy(), fog.E4M3)
+        if value == 1e-30:
+            assert not got.any() and bool((dx == 0).all())
+        else:       # half a step of a code
+            assert np.all(np.abs(got / 30.0 - y) <= 2.0 ** -4 * 1.01 * np.abs(y) + 2.0 ** -10 / 30)
+
+
 @pytest.mark.parametrize("rot", [2, 20, 128, 600])
 @pytest.mark.parametrize("first,positions", [(0, 1), (0, 130), (1_000_000, 65), (-40, 80), ((1 << 40), 3)])
 @pytest.mark.parametrize("scaling", [{}, dict(base=5e5), dict(factor=4.0), dict(factor=8.0, low=1.0, high=32.0, original=4096.0, amplitude=1.25)])

@@ -203,6 +203,8 @@ def test_rope_bindings_look_at_types_and_shapes():
             fog.make_rope_jobs([{**good, **bad}])
     with pytest.raises(ValueError):
         fog.make_rope_jobs([good, dict(x=x[:1], q=q[:1], scale=s)])
+    with pytest.raises(ValueError):
+        fog.rope_quantize(fog.make_rope_jobs([good]), None)          # to be turned, by no table
     assert ctypes.sizeof(fog.RopeJob) == 96 and ctypes.sizeof(fog.RopeGradJob) == 160
 
 
