@@ -574,15 +574,23 @@ def grad_clip(jobs, sumsq, max_norm, norm=None, stream=None):
 
 
 def _vector(t, what, n):
-    """A contiguous vector of n floats, or None."""
-    if t is not None and (t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous()):
+    """Pointer of a contiguous vector of n floats that may be missing."""
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous():
         raise ValueError("%s: %d contiguous float32 numbers are needed, got %s of %s with strides %s" % (what, n, tuple(t.shape), t.dtype, t.stride()))
-    return _ptr(t)
+    return t.data_ptr()
 
 
 def _some(t, what, rows, cols, types):
     """Pointer and leading dimension of a matrix that may be missing."""
-    return (None, 0) if t is None else (t.data_ptr(), _matrix(t, what, rows, cols, types))
+    if t is None:
+        return None, 0
+    if t.shape == (rows, cols) and t.dtype in types:          # (the usual case at half the cost)
+        ld, step = t.stride()
+        if step == 1 and ld >= cols:
+            return t.data_ptr(), ld
+    return t.data_ptr(), _matrix(t, what, rows, cols, types)
 
 
 def postnorm_residual_grad(dres, y, gamma, fmt, scale_t, dgamma, workspace, dbranch=None, dstream=None, dy=None, q=None, amax_out=None, accumulate=False, stream=None):
