@@ -1,7 +1,10 @@
 // Rotary positions between the projection and attention: the QK norm, the turn by the token's position, the FP8 cast and the change from the projection's
 // layout to the heads that attention reads, in one pass; and the way back.
 //
-// Bound by memory: forward 2 bytes read and 1 written an element, backward 2 (4 with the norm) and 1 or 3.
+// Bound by memory: forward 2 bytes read and 1 written an element, backward 2 (4 with the norm) and 1 or 3.  Q and K of 2 x 4096 tokens, 32 and 8 heads of 128, and V:
+// forward 31 us and 4 us for the launch behind it that takes the maxima together (50 M elements, 4.9 TB/s), backward with the norm 50 us (4.8 TB/s) and 5; 24 single tokens:
+// 5 us and 2, less than a call takes on the host.  (That launch stands in for a zeroed word and an atomic from each of some thousand workgroups.  A call by one
+// workgroup, without it, was slower even at the smallest sizes: 13 us.)
 //
 // A token's vector of one head (D elements) belongs to LPR lanes, a wave takes 64 / LPR tokens and walks some heads of them, so that the cosines
 // and sines, 16 of them a lane, are loaded once for all of these.  A lane holds two runs of eight elements: in the half layout eight elements and their
