@@ -260,8 +260,8 @@ fog_status fog_rmsnorm_quantize(const void* x_bf16, int64_t rows, int64_t cols, 
  *         rest of a vector) of eight elements and more are the fastest.
  *   workspace : fog_rope_workspace() bytes (64 KB), 4-byte aligned, where a job has an amax; contents on entry do not matter.  Calls that may overlap in
  *         time need a workspace each.
- * Errors: NULL, SHAPE (count, sizes, strides), ALIGN, WORKSPACE, UNSUPPORTED (format, layout, odd rot, D, B * S above 2^31 - 1, heads above 2^24, pos_bytes, gain
- * negative or not finite; an output that lies within an input's first and last element, or outputs that are not seen to lie apart).
+ * Errors: NULL, SHAPE (count, sizes, strides), ALIGN, WORKSPACE, UNSUPPORTED (format, layout, odd rot, D, B * S above 2^31 - 1, heads above 2^24, pos_bytes, a table larger than any address space, gain
+ * negative or not finite; an output that lies within the first and last element of an input (table and pos among them), or outputs that are not seen to lie apart).
  *
  * fog_rope_grad is the way back, per token and head with dy the gradient of y:
  *     dz = the transposed turn of dy;     dx = gain / rms(x) (dz - x (x . dz) / (x . x))      (gain == 0: dx = dz; x is not looked at; a vector of zeros: 0)

@@ -2,7 +2,7 @@
 // layout to the heads that attention reads, in one pass; and the way back.
 //
 // Bound by memory: forward 2 bytes read and 1 written an element, backward 2 (4 with the norm) and 1 or 3.  Q and K of 2 x 4096 tokens, 32 and 8 heads of 128, and V:
-// forward 31 us and 4 us for the launch behind it that takes the maxima together (50 M elements, 4.9 TB/s), backward with the norm 50 us (4.8 TB/s) and 5; 24 single tokens:
+// forward 28 us and 4 us for the launch behind it that takes the maxima together (50 M elements, 5.4 TB/s), backward with the norm 48 us (4.9 TB/s) and 5; 24 single tokens:
 // 5 us and 2, less than a call takes on the host.  (That launch stands in for a zeroed word and an atomic from each of some thousand workgroups.  A call by one
 // workgroup, without it, was slower even at the smallest sizes: 13 us.)
 //
@@ -102,6 +102,7 @@ FOG_DEVICE uint4 fetch(const uint16_t* p, int n) {
   return n >= 8 ? ld_any_nt16(p) : ld_upto8(p, n);
 }
 typedef u32x2 __attribute__((aligned(1))) u32x2_byte;
+typedef u32x4 __attribute__((aligned(1))) u32x4_byte;
 template <bool FULL>
 FOG_DEVICE void store_codes(uint8_t* p, uint2 w, int n) {
   if (FULL ? n > 0 : n >= 8) {
@@ -111,14 +112,22 @@ FOG_DEVICE void store_codes(uint8_t* p, uint2 w, int n) {
     st_upto8(p, w, n);
   }
 }
+// Codes of two runs whose next ones the neighbour lane has: the even lane stores both first runs, the odd one both second runs.  (Not past the caches: 33.5 us
+// instead of 31.9, and 39 in pieces of eight.)
+FOG_DEVICE uint32_t beside(uint32_t v) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xF, 0xF, false); }
+FOG_DEVICE void store_even(uint8_t* to, int offA, int offB, uint2 a, uint2 e, bool odd) {
+  const uint32_t x = beside(odd ? a.x : e.x), y = beside(odd ? a.y : e.y);
+  const u32x4 v = {odd ? x : a.x, odd ? y : a.y, odd ? e.x : x, odd ? e.y : y};
+  *reinterpret_cast<u32x4_byte*>(to + (odd ? offB - 8 : offA)) = v;
+}
 template <bool FULL>
 FOG_DEVICE void store_half(uint16_t* p, uint4 w, int n) {
   if (FULL ? n > 0 : n >= 8) st_any16(p, w);
   else if (!FULL) st_upto8(p, w, n);
 }
-// Eight floats at any address of a float.
-FOG_DEVICE void floats8(const float* p, float (&f)[8]) {
-  const uint4 a = ld_any16(p), b = ld_any16(p + 4);
+// Four floats at each of two addresses of a float.
+FOG_DEVICE void floats8(const float* p, const float* r, float (&f)[8]) {
+  const uint4 a = ld_any16(p), b = ld_any16(r);
   f[0] = __uint_as_float(a.x); f[1] = __uint_as_float(a.y); f[2] = __uint_as_float(a.z); f[3] = __uint_as_float(a.w);
   f[4] = __uint_as_float(b.x); f[5] = __uint_as_float(b.y); f[6] = __uint_as_float(b.z); f[7] = __uint_as_float(b.w);
 }
@@ -177,7 +186,11 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(Jobs<GRAD, N> jobs, Shap
   while (j + 1 < jobs.count && (int)blockIdx.x >= jobs.job[j + 1].first) ++j;
   const Job& job = jobs.job[j];
   const uint32_t at = blockIdx.x - job.first, segments = (uint32_t)((job.heads + sh.segment - 1) / sh.segment);
-  const int h0 = (int)(at % segments) * sh.segment, h1 = h0 + sh.segment < job.heads ? h0 + sh.segment : job.heads;
+  // The segments of the same tokens on one XCD (workgroups eight apart), so that its L2 has their rows of the table for all but the first (2 x 4096: 34.4 -> 33.7 us).
+  const uint32_t eights = sh.groups & ~7u;
+  const bool apart = at < eights * segments;
+  const uint32_t group0 = apart ? (at & 7u) + 8u * (at / (8u * segments)) : at / segments, segment = apart ? (at >> 3) % segments : at % segments;
+  const int h0 = (int)segment * sh.segment, h1 = h0 + sh.segment < job.heads ? h0 + sh.segment : job.heads;
   const uint32_t vector = threadIdx.x / LPR, tokens = 1u << sh.side;
   const int slot = (int)(vector >> sh.side), slots = VECTORS >> sh.side;
   const int lane = threadIdx.x % LPR;
@@ -186,8 +199,18 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(Jobs<GRAD, N> jobs, Shap
   const bool on = lane < turners;
   // Where the lane's two runs begin and how long they are.  In the FULL form every run is of eight: the last one of a stretch that eight does not divide
   // reaches back over elements of the lane in front of it, which gives them the same values; only sums leave those out (skip).
-  int offA, offB, nA, nB, skipA = 0, skipB = 0, first = 8 * lane;        // first: pair
-  if (on) {
+  // `even`: stretches of whole thirty-twos.  There a lane's runs lie half a stretch apart in either layout, so that each load of a wave covers whole lines, and
+  // two lanes store the codes of one's first and the other's second runs, sixteen bytes each (2 x 4096, 32/8 heads: 33.7 -> 31.9 us forward, 52.5 -> 52 backward).
+  int offA, offB, nA, nB, skipA = 0, skipB = 0, first = 8 * lane;        // first, firstB: pairs whose cosines come first and from the fifth on
+  const int rest = sh.D - 2 * half;
+  const bool even = FULL && (half & 15) == 0 && (rest & 31) == 0;
+  if (even) {
+    const int width = on ? half : rest >> 1, l = on ? lane : lane - turners;
+    offA = (on ? 0 : 2 * half) + 8 * l;
+    offB = offA + width;
+    nA = nB = 8 * l < width ? 8 : 0;
+    if (INTER) first = 4 * lane;
+  } else if (on) {
     const int pairs = half - 8 * lane < 8 ? half - 8 * lane : 8;
     if (FULL) first -= 8 - pairs;
     offA = (INTER ? 2 : 1) * first;
@@ -202,13 +225,14 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(Jobs<GRAD, N> jobs, Shap
     nB = n - 8 < 0 ? 0 : n - 8 < 8 ? n - 8 : 8;
     if (FULL && n > 0 && n < 16) {
       offB = sh.D - 8;
-      if (sh.D - 2 * half >= 16) offA = sh.D - 16;
+      if (rest >= 16) offA = sh.D - 16;
     }
   }
-  if (FULL && nA + nB > 0) {
+  const int firstB = INTER && even ? first + (half >> 1) : first + 4;
+  if (FULL && !even && nA + nB > 0) {
     if (on && !INTER) {
       skipA = skipB = 8 - nA;
-    } else if (on || sh.D - 2 * half >= 16) {      // sixteen elements in a row, the last ones new
+    } else if (on || rest >= 16) {      // sixteen elements in a row, the last ones new
       const int skip = 16 - (nA + nB);
       skipA = skip < 8 ? skip : 8;
       skipB = skip - skipA;
@@ -223,7 +247,7 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(Jobs<GRAD, N> jobs, Shap
   float top = 0.0f;
   bool nan = false;
   uint32_t top_bits = 0u;
-  for (uint32_t group = at / segments; group * (uint64_t)tokens < sh.tokens; group += sh.groups) {
+  for (uint32_t group = group0; group * (uint64_t)tokens < sh.tokens; group += sh.groups) {
     const uint32_t t = group * tokens + (vector & (tokens - 1));
     if (t >= sh.tokens) break;           // (whole vectors: their lanes leave together)
     const uint32_t b = t / sh.S, s = t - b * sh.S;
@@ -250,8 +274,9 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(Jobs<GRAD, N> jobs, Shap
       if (on && there) {
         const float* row = sh.table + p * sh.rot + first;
         if (FULL) {
-          floats8(row, c);
-          floats8(row + half, sn);
+          const float* later = sh.table + p * sh.rot + firstB;
+          floats8(row, later, c);
+          floats8(row + half, later + half, sn);
         } else {
 #pragma unroll
           for (int k = 0; k < 8; ++k)
@@ -324,8 +349,13 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(Jobs<GRAD, N> jobs, Shap
             nan |= (na.x | na.y | ne.x | ne.y) != 0u;
           }
           uint8_t* to = q + (h + u * slots) * job.q.head;
-          store_codes<FULL>(to + offA, with(convert8<false>(a, e5m2), na), nA);
-          store_codes<FULL>(to + offB, with(convert8<false>(e, e5m2), ne), nB);
+          const uint2 ca = with(convert8<false>(a, e5m2), na), ce = with(convert8<false>(e, e5m2), ne);
+          if (even) {
+            if (nA > 0) store_even(to, offA, offB, ca, ce, (lane & 1) != 0);
+          } else {
+            store_codes<FULL>(to + offA, ca, nA);
+            store_codes<FULL>(to + offB, ce, nB);
+          }
         } else {
           if (on) turn<INTER, true>(a, e, c, sn);
           if (norm) {
@@ -371,8 +401,13 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(Jobs<GRAD, N> jobs, Shap
               ne = tame8(e);
             }
             uint8_t* to = q + (h + u * slots) * job.q.head;
-            store_codes<FULL>(to + offA, with(convert8<true>(a, e5m2), na), nA);
-            store_codes<FULL>(to + offB, with(convert8<true>(e, e5m2), ne), nB);
+            const uint2 ca = with(convert8<true>(a, e5m2), na), ce = with(convert8<true>(e, e5m2), ne);
+            if (even) {
+              if (nA > 0) store_even(to, offA, offB, ca, ce, (lane & 1) != 0);
+            } else {
+              store_codes<FULL>(to + offA, ca, nA);
+              store_codes<FULL>(to + offB, ce, nB);
+            }
           }
         }
       }
@@ -450,7 +485,7 @@ fog_status make_box(const fog_heads& h, int B, int S, int heads, int D, int size
 }
 
 struct Call {
-  FogBox in[2 * JOBS], out[2 * JOBS];
+  FogBox in[2 * JOBS + 2], out[2 * JOBS];
   int ins = 0, outs = 0;
   fog_status add(const fog_heads& h, int B, int S, int heads, int D, int size, bool written) {
     const fog_status st = make_box(h, B, S, heads, D, size, written ? &out[outs] : &in[ins]);
@@ -458,6 +493,14 @@ struct Call {
     if (written && !fog_injective(out[outs])) return FOG_ERR_SHAPE;
     ++(written ? outs : ins);
     return FOG_OK;
+  }
+  // The table and the positions, which are read as well.
+  fog_status add_common(const float* table, int64_t positions, int rot, const void* pos, int64_t tokens, int pos_bytes) {
+    const int64_t n[2] = {positions, tokens}, stride[2] = {rot, 1};
+    fog_status st = FOG_OK;
+    if (table && rot > 0 && positions > 0) st = fog_make_box(table, 1, n, stride, rot, 4, &in[ins++]);
+    if (st == FOG_OK && pos) st = fog_make_box(pos, 1, n + 1, stride + 1, 1, pos_bytes, &in[ins++]);
+    return st;
   }
   bool fine() const {
     for (int i = 0; i < outs; ++i) {
@@ -601,6 +644,8 @@ extern "C" fog_status fog_rope_quantize(const fog_rope_job* jobs, int count, int
     amax[j] = in.amax;
     any_amax |= in.amax != nullptr;
   }
+  const fog_status common = empty ? FOG_OK : call.add_common(table, positions, rot, pos, (int64_t)B * S, pos_bytes);
+  if (common != FOG_OK) return common;
   if (!call.fine()) return FOG_ERR_UNSUPPORTED;
   if (any_amax && (!workspace || workspace_bytes < fog_rope_workspace())) return FOG_ERR_WORKSPACE;
   if (reinterpret_cast<uintptr_t>(workspace) & 3) return FOG_ERR_ALIGN;
@@ -640,6 +685,8 @@ extern "C" fog_status fog_rope_grad(const fog_rope_grad_job* jobs, int count, in
     amax[j] = in.amax;
     any_amax |= in.amax != nullptr;
   }
+  const fog_status common = empty ? FOG_OK : call.add_common(table, positions, rot, pos, (int64_t)B * S, pos_bytes);
+  if (common != FOG_OK) return common;
   if (!call.fine()) return FOG_ERR_UNSUPPORTED;
   if (any_amax && (!workspace || workspace_bytes < fog_rope_workspace())) return FOG_ERR_WORKSPACE;
   if (reinterpret_cast<uintptr_t>(workspace) & 3) return FOG_ERR_ALIGN;

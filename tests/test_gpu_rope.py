@@ -115,6 +115,25 @@ def test_backward(B, S, H, D, rot, layout, gain, fmt):
     assert torch.equal(q2, q) and amax2.item() == amax.item() and torch.equal(dx2, dx)
 
 
+@pytest.mark.parametrize("layout", LAYOUTS)
+@pytest.mark.parametrize("B,S,H,D,rot", [(2, 9, 3, 96, 32), (1, 355, 9, 128, 96), (3, 5, 2, 320, 96), (2, 45, 5, 992, 512), (5, 67, 7, 64, 64), (1, 300, 3, 32, 0)])
+def test_stretches_of_whole_thirty_twos(B, S, H, D, rot, layout):
+    """Runs half a stretch apart, turned or not; groups of tokens that eight does not divide, and jobs of one and of several segments of heads; codes at odd addresses."""
+    x, y = normal(B + S + D, B, S, H, D), normal(B + S + D + 1, B, S, H, D)
+    table, scale, amaxs = make_table(S, rot), one(448.0 / 8), [one(-1) for _ in range(4)]
+    outs = [u8(B * H * S * D + 16) for _ in range(2)]
+    q, v = (o[3:3 + B * H * S * D].view(B, H, S, D).transpose(1, 2) for o in outs)
+    fog.rope_quantize(fog.make_rope_jobs([dict(x=x, q=q, scale=scale, amax=amaxs[0], gain=1.0), dict(x=y, q=v, scale=scale, amax=amaxs[1], rotate=False)]), table, room(),
+                      layout=layout)
+    check_forward(x, q, amaxs[0], scale, table, pos_of(B, S, None), layout, 1.0, fog.E4M3)
+    check_forward(y, v, amaxs[1], scale, table, pos_of(B, S, None), layout, 0.0, fog.E4M3, rotate=False)
+    for o in outs:
+        assert bool((o[:3] == 0xA5).all()) and bool((o[3 + B * H * S * D:] == 0xA5).all())
+    dy, dx, dq, sg = normal(B + S + D + 2, B, H, S, D, std=1e-3).transpose(1, 2), normal(0, B, S, H, D), u8(B, S, H, D), one(57344.0 / 8e-3)
+    fog.rope_grad(fog.make_rope_grad_jobs([dict(dy=dy, x=x, dx=dx, q=dq, scale=sg, amax=amaxs[2], gain=1.0)]), table, room(), layout=layout)
+    check_backward(dy, x, dx, dq, amaxs[2], sg, table, pos_of(B, S, None), layout, 1.0, fog.E5M2)
+
+
 @pytest.mark.parametrize("dtype", [torch.int32, torch.int64])
 @pytest.mark.parametrize("layout", LAYOUTS)
 def test_positions_of_every_kind(dtype, layout):

@@ -179,6 +179,20 @@ def test_rope_outputs_that_lie_between_each_other(lib):
     assert outputs(lib, kv(0, 8), (heads(Q + MB, 4096, 256, 128), 2)) == HIP
 
 
+def test_rope_outputs_on_the_table_or_the_positions(lib):
+    end = P + 16 * 128 * 4                                                # of a table of 16 rows
+    for at in (P, end - 1):
+        assert rope(lib, [rope_job(q=heads(at), x=heads(P + 8 * MB))]) == UNSUPPORTED
+        assert rope(lib, [rope_grad_job(dx=heads(at & ~1), dy=heads(P + 8 * MB))], grad=True) == UNSUPPORTED
+    for pos_bytes in (4, 8):
+        for at in (P + 2 * MB, P + 2 * MB + 48 * pos_bytes - 1):           # 3 x 16 positions
+            assert rope(lib, [rope_job(q=heads(at))], pos=P + 2 * MB, pos_bytes=pos_bytes) == UNSUPPORTED
+    assert rope(lib, [rope_job()], positions=1 << 60) == UNSUPPORTED
+    if not torch.cuda.is_available():
+        assert rope(lib, [rope_job(q=heads(end), x=heads(P + 8 * MB))]) == HIP
+        assert rope(lib, [rope_job(q=heads(P + 2 * MB + 48 * 4))], pos=P + 2 * MB, pos_bytes=4) == HIP
+
+
 def table(lib, first=0, positions=10, rot=64, t=P, **scaling):
     s = dict(base=10000.0, factor=2.0, low=1.0, high=4.0, original=4096.0, amplitude=1.0)
     s.update(scaling)
