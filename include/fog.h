@@ -422,7 +422,8 @@ size_t fog_postnorm_residual_grad_workspace(int64_t rows, int64_t cols);
  *   amax_out : NULL or one float, overwritten.
  *   workspace : fog_act_grad_workspace() bytes (40 KB), 8-byte aligned, where dalpha or amax_out is given; contents on entry do not matter.  Calls that may overlap in
  *             time need a workspace each.
- * Rows of any length and alignment.  f' is within 2^-19 of its terms' size (GeLU: and x^2 2^-23, tanh: and |alpha x| 2^-22).
+ * Rows of any length and alignment.  f' is within 2^-19 of its terms' size (GeLU: and x^2 2^-23, tanh: and |alpha x| 2^-22).  A term of the
+ * xIELU's second sum whose |x| is at most 2^-24 may count as 0.
  * Errors: NULL, SHAPE, ALIGN, WORKSPACE, UNSUPPORTED (format, alpha as in the producers, rows * cols above 2^47, results that meet an input or each other).
  */
 fog_status fog_xielu_grad(const void* x_bf16, int64_t ldx, const void* dy_bf16, int64_t ld_dy, int64_t rows, int64_t cols, float alpha_p, float alpha_n,

@@ -46,13 +46,12 @@ FOG_DEVICE Entry entry(float t, float p0) {
   return {4.0f * e * r * r, 0.0f};
 }
 
-// f'(x), and the parameters' sums of one element.  (The bounds that the xIELU's entries are held to are true of the functions; they give what an entry of a table
-// does not know, the function beyond the table's ends.  The maxima and minima let a NaN through.)
+// f'(x), and the parameters' sums of one element.  (The bounds that the xIELU's entries are held to, e^x - 1 >= x and e^x - 1 - x >= -1 - x, are true of the functions;
+// they give what an entry of a table does not know, the function beyond the table's ends.  The maxima and minima let a NaN through.)
 template <int ACT>
 FOG_DEVICE float slope(float x, float d, Entry v, float p0, float p1, float& t0, float& t1) {
   if (ACT == ACT_XIELU) {
-    const float e = __builtin_elementwise_maximum(v.f, x);                               // e^x - 1 >= x
-    const float curve = __builtin_elementwise_minimum(__builtin_elementwise_maximum(v.g, -1.0f - x), 0.5f * x * x);   // -1 - x <= e^x - 1 - x <= x^2 / 2
+    const float e = __builtin_elementwise_maximum(v.f, x), curve = __builtin_elementwise_maximum(v.g, -1.0f - x);
     const bool up = x > 0.0f;
     const float xu = up ? x : 0.0f, dn = up ? 0.0f : d;
     t0 = __builtin_fmaf(d * xu, xu, t0);
@@ -69,7 +68,7 @@ FOG_DEVICE float slope(float x, float d, Entry v, float p0, float p1, float& t0,
 
 // ---------------------------------------------------------------- large tensors: the entries of a bf16 magnitude from a table in LDS
 // (As the producers have it.)  Magnitudes (bf16 patterns) lo .. hi; smaller ones take the entry of lo, larger ones that of hi.
-//   xIELU  2^-24 .. 32      GeLU  2^-24 .. 14: 1/2 and 0 outside      tanh  1 below |alpha| t = 2^-13, 0 from 64 on
+//   xIELU  2^-24 .. 32 (up to 2^-24 the second sum's term counts as 0)      GeLU  2^-24 .. 14: 1/2 and 0 outside      tanh  1 below |alpha| t = 2^-13, 0 from 64 on
 struct Window { int lo, hi; };
 template <int ACT>
 __device__ constexpr Window window_of(uint32_t p0_bits) {
@@ -85,17 +84,22 @@ template <int ACT>
 struct Table {
   static constexpr int BYTES = ACT == ACT_XIELU ? 8 : 4;
   const char* at;          // entry of magnitude b at byte BYTES (b - lo)
-  uint32_t lo, hi;         // the window as float patterns
-  __device__ __forceinline__ Entry operator()(float x) const {
-    uint32_t b = __float_as_uint(x) & 0x7FFFFFFFu;                   // (clamped as integers: a NaN's pattern is above hi)
-    b = b < lo ? lo : b > hi ? hi : b;
-    const char* p = at + ((b - lo) >> (BYTES == 8 ? 13 : 14));
+  us2 lo, hi;              // the window, twice
+  // Where the entries of a pair of numbers lie, 16 bits each: four instructions on both (one by one eight; with the bounds of the slope 124 -> 119 us).
+  __device__ __forceinline__ uint32_t places(uint32_t w) const {
+    us2 b = __builtin_bit_cast(us2, w & 0x7FFF7FFFu);                // (clamped as integers: a NaN's pattern is above hi)
+    b = __builtin_elementwise_min(__builtin_elementwise_max(b, lo), hi);
+    return __builtin_bit_cast(uint32_t, (us2)((b - lo) << (unsigned short)(BYTES == 8 ? 3 : 2)));
+  }
+  __device__ __forceinline__ Entry entry_at(uint32_t place) const {
+    const char* p = at + place;
     if (BYTES == 8) {
       const float2 v = *reinterpret_cast<const float2*>(p);
       return {v.x, v.y};
     }
     return {*reinterpret_cast<const float*>(p), 0.0f};
   }
+  __device__ __forceinline__ Entry operator()(float x) const { return entry_at(places(__float_as_uint(x) >> 16) & 0xFFFFu); }
 };
 
 struct Args {
@@ -234,54 +238,62 @@ __global__ __launch_bounds__(kThreads) void act_grad_kernel(Args a) {
   leave<kThreads>(a, s0, s1, top);
 }
 
-// Rows of whole sixteens, or one row of any length: a thread takes sixteen elements at a time, the next ones' loads under way, and looks the entries up.
-// One workgroup a compute unit fills its table once.  Whole calls, 8192 x 14336 / 4096 x 4096: xIELU 142 -> 119 / 28.7 -> 23.4 us against entries that are computed
-// in chunks of eight, GeLU 123 -> 115; without any activation (dx = dy x) 112 / 20: the rest is memory and two launches.
-template <int ACT, int FMT>
+// Rows of whole sixteens, or one row of any length (FLAT): a wave takes 1024 elements at a time, in two halves so that each of its loads covers whole lines, and
+// looks the entries up; two lanes store the codes of one's first and the other's second eight, sixteen bytes each.  Whole calls of xIELU, 8192 x 14336, from a graph:
+// 123 us with sixteen elements in a row a lane and the next ones' loads under way, 114 like this (110 to 115 with three workgroups of 512 threads a compute unit and
+// spilled registers, 115 with the loads under way); 104 without the function: the rest is memory and two launches.  One workgroup a compute unit fills its table once.
+// Against entries that are computed in chunks of eight, 8192 x 14336 / 4096 x 4096 (an earlier form of this kernel): xIELU 142 -> 119 / 28.7 -> 23.4 us, GeLU 123 -> 115.
+FOG_DEVICE uint32_t beside(uint32_t v) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xF, 0xF, false); }
+template <int ACT, int FMT, bool FLAT>
 __global__ __launch_bounds__(kTableThreads) void act_grad_table_kernel(Args a) {
   __shared__ __attribute__((aligned(16))) char table[kTableMax * Table<ACT>::BYTES];
-  const int64_t per_row = a.cols / 16, total = a.rows * per_row, stride = (int64_t)gridDim.x * kTableThreads;
-  auto offset = [&](int64_t i, int64_t ld) {
-    if (a.rows == 1) return i * 16;
-    const int64_t r = total <= 0xFFFFFFFF ? (int64_t)((uint32_t)i / (uint32_t)per_row) : i / per_row;
-    return r * ld + (i - r * per_row) * 16;
-  };
-  int64_t i = (int64_t)blockIdx.x * kTableThreads + threadIdx.x;
-  uint4 x[2], d[2], nx[2], nd[2];
-  auto load = [&](int64_t i, uint4 (&x)[2], uint4 (&d)[2]) {
-    if (i < total) {
-      const uint16_t *px = a.x + offset(i, a.ldx), *pd = a.dy + offset(i, a.ld_dy);
-      x[0] = ld_any_nt16(px); x[1] = ld_any_nt16(px + 8);
-      d[0] = ld_any_nt16(pd); d[1] = ld_any_nt16(pd + 8);
-    }
-  };
-  x[0] = x[1] = d[0] = d[1] = make_uint4(0, 0, 0, 0);
-  load(i, x, d);
+  constexpr int WAVES = kTableThreads / 64;
   const Window win = window_of<ACT>(__float_as_uint(a.p0));
   for (int b = win.lo + (int)threadIdx.x; b <= win.hi; b += kTableThreads) {
-    const Entry v = entry<ACT>(__uint_as_float((uint32_t)b << 16), a.p0);
+    Entry v = entry<ACT>(__uint_as_float((uint32_t)b << 16), a.p0);
+    if (ACT == ACT_XIELU && b == win.lo) v.g = 0.0f;                 // zeros, among others
     float* to = reinterpret_cast<float*>(table) + (b - win.lo) * (Table<ACT>::BYTES / 4);
     to[0] = v.f;
     if (Table<ACT>::BYTES == 8) to[1] = v.g;
   }
   const float rho = a.q ? *a.scale : 0.0f;
-  const Table<ACT> look = {table, (uint32_t)win.lo << 16, (uint32_t)win.hi << 16};
+  const unsigned short lo = (unsigned short)win.lo, hi = (unsigned short)win.hi;
+  const Table<ACT> look = {table, {lo, lo}, {hi, hi}};
   double s0 = 0.0, s1 = 0.0;
   uint32_t top = 0u;
   __syncthreads();
-  while (i < total) {
-    const int64_t next = i + stride;
-    nx[0] = nx[1] = nd[0] = nd[1] = make_uint4(0, 0, 0, 0);
-    load(next, nx, nd);
-    uint4 o[2];
+  // Chunks of eight elements: pairs of them are whole, so that a lane and its neighbour are there or not together.
+  const int64_t chunks = 2 * (a.cols / 16), total = a.rows * chunks;
+  const uint32_t lane = threadIdx.x & 63;
+  const bool odd = (lane & 1) != 0;
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  int64_t i = 128 * ((int64_t)blockIdx.x * WAVES + wave);            // the wave's first chunk: scalar, and with it the addresses of FLAT but for the lane's place
+  auto at = [&](auto* base, uint32_t k, int64_t ld) {
+    if (FLAT) return (base + 8 * i) + 8 * k;
+    const int64_t j = i + k, r = total <= 0xFFFFFFFF ? (int64_t)((uint32_t)j / (uint32_t)chunks) : j / chunks;
+    return base + r * ld + 8 * (j - r * chunks);
+  };
+  for (; i < total; i += 128 * (int64_t)gridDim.x * WAVES) {
+    const uint32_t left = total - i < 128 ? (uint32_t)(total - i) : 128u;
+    uint4 x[2], d[2], o[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      x[h] = d[h] = make_uint4(0, 0, 0, 0);
+      if (lane + 64 * h < left) {
+        x[h] = ld_any_nt16(at(a.x, lane + 64 * h, a.ldx));
+        d[h] = ld_any_nt16(at(a.dy, lane + 64 * h, a.ld_dy));
+      }
+    }
     uint32_t most = 0u;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       float f[8], g[8], t0 = 0.0f, t1 = 0.0f;
       unpack8(x[h], f);
       unpack8(d[h], g);
+      const uint32_t place[4] = {look.places(x[h].x), look.places(x[h].y), look.places(x[h].z), look.places(x[h].w)};
 #pragma unroll
-      for (int k = 0; k < 8; ++k) g[k] *= slope<ACT>(f[k], g[k], look(f[k]), a.p0, a.p1, t0, t1);
+      for (int k = 0; k < 8; ++k)
+        g[k] *= slope<ACT>(f[k], g[k], look.entry_at(k & 1 ? place[k >> 1] >> 16 : place[k >> 1] & 0xFFFFu), a.p0, a.p1, t0, t1);
       if (ACT != ACT_GELU) s0 += (double)t0;
       if (ACT == ACT_XIELU) s1 += (double)t1;
       o[h] = pack8(g);
@@ -289,21 +301,19 @@ __global__ __launch_bounds__(kTableThreads) void act_grad_table_kernel(Args a) {
     }
     top = larger(top, most);
     if (a.dx) {
-      uint16_t* to = a.dx + offset(i, a.ld_dx);
-      st_any_nt16(to, o[0]);
-      st_any_nt16(to + 8, o[1]);
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        if (lane + 64 * h < left) st_any_nt16(at(a.dx, lane + 64 * h, a.ld_dx), o[h]);
     }
     if (a.q) {
       const bool fine = fits<FMT>(most, rho);
-      const uint2 lo = cast8<FMT>(o[0], rho, fine), hi = cast8<FMT>(o[1], rho, fine);
-      st_any_nt16(a.q + offset(i, a.ldq), make_uint4(lo.x, lo.y, hi.x, hi.y));
+      const uint2 u = cast8<FMT>(o[0], rho, fine), w = cast8<FMT>(o[1], rho, fine);
+      const uint32_t p = beside(odd ? u.x : w.x), r = beside(odd ? u.y : w.y), k = odd ? lane + 63 : lane;
+      if (k < left) st_any_nt16(at(a.q, k, a.ldq), make_uint4(odd ? p : u.x, odd ? r : u.y, odd ? w.x : p, odd ? w.y : r));
     }
-#pragma unroll
-    for (int h = 0; h < 2; ++h) { x[h] = nx[h]; d[h] = nd[h]; }
-    i = next;
   }
-  if (blockIdx.x == 0 && threadIdx.x < 2 && a.rows == 1)          // what sixteen does not divide
-    work<ACT, FMT>(a, fetch(a, 2 * total + threadIdx.x, a.chunks), rho, look, s0, s1, top);
+  if (FLAT && blockIdx.x == 0 && threadIdx.x < 2)          // what sixteen does not divide
+    work<ACT, FMT>(a, fetch(a, total + threadIdx.x, a.chunks), rho, look, s0, s1, top);
   leave<kTableThreads>(a, s0, s1, top);
 }
 
@@ -377,8 +387,12 @@ fog_status act_grad(const void* x_bf16, int64_t ldx, const void* dy_bf16, int64_
     const bool table = chunks >= 2 * (int64_t)cus * kTableThreads && cus <= GROUPS && (a.rows == 1 || a.cols % 16 == 0);
     groups = table ? cus : (int)(want < GROUPS ? want : GROUPS);
     if (table) {
-      if (fmt == FOG_E4M3) act_grad_table_kernel<ACT, FOG_E4M3><<<groups, kTableThreads, 0, s>>>(a);
-      else                 act_grad_table_kernel<ACT, FOG_E5M2><<<groups, kTableThreads, 0, s>>>(a);
+#define FOG_TABLE(FLAT)                                                                                                        \
+  (fmt == FOG_E4M3 ? act_grad_table_kernel<ACT, FOG_E4M3, FLAT><<<groups, kTableThreads, 0, s>>>(a)                            \
+                   : act_grad_table_kernel<ACT, FOG_E5M2, FLAT><<<groups, kTableThreads, 0, s>>>(a))
+      if (a.rows == 1) FOG_TABLE(true);
+      else FOG_TABLE(false);
+#undef FOG_TABLE
     } else {
       if (fmt == FOG_E4M3) act_grad_kernel<ACT, FOG_E4M3><<<groups, kThreads, 0, s>>>(a);
       else                 act_grad_kernel<ACT, FOG_E5M2><<<groups, kThreads, 0, s>>>(a);

@@ -294,6 +294,19 @@ def test_activation_of_large_tensors(act, alpha, rows, cols, ld, skew):
     assert around(a.b_dx, a.dx) and around(a.b_q, a.q)
 
 
+@pytest.mark.parametrize("rows", [3, 900])          # below and above the sizes that a table pays for
+def test_xielu_sums_of_zeros_and_of_very_small_numbers(rows):
+    """Exactly nothing from zeros; from numbers of at most 2^-24 their squares' half, or nothing."""
+    a = Act(28, "xielu", (0.8, 0.6), rows, 8192)
+    a.x[:, ::2], a.x[:, 1::2] = 0.0, -0.0
+    a.run()
+    assert a.dalpha.tolist() == [0.0, 0.0]
+    a.x.fill_(-(2.0 ** -25))
+    a.run()
+    assert a.dalpha[0].item() == 0.0 and abs(a.dalpha[1].item()) <= 1.01 * 2.0 ** -51 * np.abs(h64(a.d)).sum()
+    assert bool((a.dx == (a.d.float() * 0.5).to(BF)).all())
+
+
 @pytest.mark.parametrize("act,alpha", ACTS)
 @pytest.mark.parametrize("rows", [1, 96])          # 1, 96 times all 65536 - 512 finite numbers: below and above the sizes that a table pays for
 def test_activation_at_every_number(act, alpha, rows):
