@@ -102,7 +102,6 @@ FOG_DEVICE uint4 fetch(const uint16_t* p, int n) {
   return n >= 8 ? ld_any_nt16(p) : ld_upto8(p, n);
 }
 typedef u32x2 __attribute__((aligned(1))) u32x2_byte;
-typedef u32x4 __attribute__((aligned(1))) u32x4_byte;
 template <bool FULL>
 FOG_DEVICE void store_codes(uint8_t* p, uint2 w, int n) {
   if (FULL ? n > 0 : n >= 8) {
@@ -112,13 +111,12 @@ FOG_DEVICE void store_codes(uint8_t* p, uint2 w, int n) {
     st_upto8(p, w, n);
   }
 }
-// Codes of two runs whose next ones the neighbour lane has: the even lane stores both first runs, the odd one both second runs.  (Not past the caches: 33.5 us
-// instead of 31.9, and 39 in pieces of eight.)
+// Codes of two runs whose next ones the neighbour lane has: the even lane stores both first runs, the odd one both second runs.  Written through: without, the next
+// launch waits for what the caches still have to write back (31.6 -> 30.3 us forward, 51.6 -> 50.3 backward); past the caches 33.5 us, and 39 in pieces of eight.
 FOG_DEVICE uint32_t beside(uint32_t v) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xF, 0xF, false); }
 FOG_DEVICE void store_even(uint8_t* to, int offA, int offB, uint2 a, uint2 e, bool odd) {
   const uint32_t x = beside(odd ? a.x : e.x), y = beside(odd ? a.y : e.y);
-  const u32x4 v = {odd ? x : a.x, odd ? y : a.y, odd ? e.x : x, odd ? e.y : y};
-  *reinterpret_cast<u32x4_byte*>(to + (odd ? offB - 8 : offA)) = v;
+  st_through16(to + (odd ? offB - 8 : offA), odd ? make_uint4(x, y, e.x, e.y) : make_uint4(a.x, a.y, x, y));
 }
 template <bool FULL>
 FOG_DEVICE void store_half(uint16_t* p, uint4 w, int n) {
@@ -200,7 +198,7 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(Jobs<GRAD, N> jobs, Shap
   // Where the lane's two runs begin and how long they are.  In the FULL form every run is of eight: the last one of a stretch that eight does not divide
   // reaches back over elements of the lane in front of it, which gives them the same values; only sums leave those out (skip).
   // `even`: stretches of whole thirty-twos.  There a lane's runs lie half a stretch apart in either layout, so that each load of a wave covers whole lines, and
-  // two lanes store the codes of one's first and the other's second runs, sixteen bytes each (2 x 4096, 32/8 heads: 33.7 -> 31.9 us forward, 52.5 -> 52 backward).
+  // two lanes store the codes of one's first and the other's second runs, sixteen bytes each (2 x 4096, 32/8 heads: 33.7 -> 31.6 us forward, 52.5 -> 51.6 backward).
   int offA, offB, nA, nB, skipA = 0, skipB = 0, first = 8 * lane;        // first, firstB: pairs whose cosines come first and from the fifth on
   const int rest = sh.D - 2 * half;
   const bool even = FULL && (half & 15) == 0 && (rest & 31) == 0;
