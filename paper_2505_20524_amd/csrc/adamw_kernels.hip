@@ -244,7 +244,7 @@ FOG_DEVICE void load_four(const Tensor& t, int64_t i, int n, Four& f) {
     load4(reinterpret_cast<const float*>(t.v) + i, n, f.v);
   }
 }
-template <bool FP8, bool FULL>
+template <bool FP8, bool FULL, bool PLAIN>
 FOG_DEVICE void step_four(const Tensor& t, const AdamStep& s, int64_t i, uint32_t at, int n, Four& f) {
   if (FULL) n = 4;
 #pragma unroll
@@ -253,9 +253,12 @@ FOG_DEVICE void step_four(const Tensor& t, const AdamStep& s, int64_t i, uint32_
     f.m[e] = f.m[e] * s.beta1 + gc * s.beta1c;
     f.v[e] = f.v[e] * s.beta2 + gc * gc * s.beta2c;
     // Root and quotient by the hardware's instructions, a unit in the last place each.  A second moment below the smallest normal number counts as 0: beside
-    // an eps of 2^-38 and more its root, below 2^-63, does not show.  A smaller eps takes the correctly rounded forms, 25 instructions more.
-    const float d = s.plain_eps ? __builtin_amdgcn_sqrtf(f.v[e]) * t.root + s.eps : __builtin_sqrtf(f.v[e]) * t.root + s.eps;
-    const float u = s.plain_eps ? f.m[e] * t.rate * __builtin_amdgcn_rcpf(d) : f.m[e] * t.rate / d;
+    // an eps of 2^-38 and more its root, below 2^-63, does not show.  A smaller eps takes the correctly rounded forms, 25 instructions more, which the compiler
+    // evaluates beside the others where the eps decides in the kernel.  FP8 states have kernels for either (two blocks at 8B scale 1450 -> 1405 us); binary32 states,
+    // whose arithmetic hides behind memory, are a little faster with both (2335 us, not 2380).
+    const bool plain = PLAIN || s.plain_eps;
+    const float d = plain ? __builtin_amdgcn_sqrtf(f.v[e]) * t.root + s.eps : __builtin_sqrtf(f.v[e]) * t.root + s.eps;
+    const float u = plain ? f.m[e] * t.rate * __builtin_amdgcn_rcpf(d) : f.m[e] * t.rate / d;
     f.p[e] = f.p[e] * t.keep - u;
   }
   uint32_t r[4];
@@ -295,7 +298,7 @@ FOG_DEVICE void step_four(const Tensor& t, const AdamStep& s, int64_t i, uint32_
 }
 
 // U: fours in flight.
-template <bool FP8, int PIECE, int U>
+template <bool FP8, int PIECE, int U, bool PLAIN>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(AdamBatch b, AdamStep s) {
   Tensor t;
   t.c = 1.0f;
@@ -333,7 +336,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(AdamBatch b, AdamStep s
 #pragma unroll
         for (int u = 0; u < U; ++u) load_four<FP8, true>(t, at + i0 + 4 * kThreads * u, 4, f[u]);
 #pragma unroll
-        for (int u = 0; u < U; ++u) step_four<FP8, true>(t, s, at + i0 + 4 * kThreads * u, t.low + (uint32_t)(i0 + 4 * kThreads * u), 4, f[u]);
+        for (int u = 0; u < U; ++u) step_four<FP8, true, PLAIN>(t, s, at + i0 + 4 * kThreads * u, t.low + (uint32_t)(i0 + 4 * kThreads * u), 4, f[u]);
       }
     } else {
       const int whole = (n + 127) & ~127;                // whole blocks: their lanes stay together
@@ -341,7 +344,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(AdamBatch b, AdamStep s
       for (int i0 = 4 * (int)threadIdx.x; i0 < whole; i0 += 4 * kThreads) {
         Four f;
         load_four<FP8, false>(t, at + i0, n - i0, f);
-        step_four<FP8, false>(t, s, at + i0, t.low + (uint32_t)i0, n - i0, f);
+        step_four<FP8, false, PLAIN>(t, s, at + i0, t.low + (uint32_t)i0, n - i0, f);
       }
     }
   }
@@ -407,9 +410,10 @@ extern "C" fog_status fog_adamw(const fog_adamw_job* jobs, int count, fog_states
     if (b.count == 0) return;
     const int groups = b.pieces < GROUPS ? b.pieces : GROUPS;
     hipStream_t st = (hipStream_t)stream;
-    if (fp8)                   adamw_kernel<true, FP8_PIECE, 4><<<groups, kThreads, 0, st>>>(b, s);
-    else if (b.pieces <= MANY) adamw_kernel<false, F32_PIECE, 2><<<groups, kThreads, 0, st>>>(b, s);
-    else                       adamw_kernel<false, F32_PIECE, 1><<<groups, kThreads, ROOM, st>>>(b, s);
+    if (fp8 && s.plain_eps)    adamw_kernel<true, FP8_PIECE, 4, true><<<groups, kThreads, 0, st>>>(b, s);
+    else if (fp8)              adamw_kernel<true, FP8_PIECE, 4, false><<<groups, kThreads, 0, st>>>(b, s);
+    else if (b.pieces <= MANY) adamw_kernel<false, F32_PIECE, 2, false><<<groups, kThreads, 0, st>>>(b, s);
+    else                       adamw_kernel<false, F32_PIECE, 1, false><<<groups, kThreads, ROOM, st>>>(b, s);
     launched = true;
     b.count = b.pieces = 0;
   };
