@@ -1,7 +1,7 @@
 // The gradients of the activations, on the way back between the two products of the feed-forward half (tanh: in front of attention): dx = dy f'(x), its cast for
 // the products, and the sums that the activation's own parameters get.
 //
-// Bound by memory: 4 bytes read and 1 (3 with dx) written an element.  xIELU of 8192 x 14336: a call takes 119 to 123 us (4.9 TB/s; 112 without the function itself),
+// Bound by memory: 4 bytes read and 1 (3 with dx) written an element.  xIELU of 8192 x 14336: a call takes 113 us (5.2 TB/s; 104 without the function itself),
 // 5 of them the launch that joins the workgroups' sums in a fixed order; GeLU of 333 x 2736: 5 us and 2, less than a call takes on the host.
 #include <cfloat>
 

@@ -2,8 +2,8 @@
 // layout to the heads that attention reads, in one pass; and the way back.
 //
 // Bound by memory: forward 2 bytes read and 1 written an element, backward 2 (4 with the norm) and 1 or 3.  Q and K of 2 x 4096 tokens, 32 and 8 heads of 128, and V:
-// forward 28 us and 4 us for the launch behind it that takes the maxima together (50 M elements, 5.4 TB/s), backward with the norm 48 us (4.9 TB/s) and 5; 24 single tokens:
-// 5 us and 2, less than a call takes on the host.  (That launch stands in for a zeroed word and an atomic from each of some thousand workgroups.  A call by one
+// a whole call of the forward 31 to 32.5 us (50 M elements, 4.9 TB/s), of which some 4 are the launch behind it that takes the maxima together, backward with the norm 50.5 us
+// (4.7 TB/s); 24 single tokens: 5 us and 2, less than a call takes on the host.  (That launch stands in for a zeroed word and an atomic from each of some thousand workgroups.  A call by one
 // workgroup, without it, was slower even at the smallest sizes: 13 us.)
 //
 // A token's vector of one head (D elements) belongs to LPR lanes, a wave takes 64 / LPR tokens and walks some heads of them, so that the cosines
@@ -431,20 +431,22 @@ struct Tops {
   int first[JOBS + 1];
   uint8_t same[JOBS];      // jobs that name the result of job j
 };
-__global__ __launch_bounds__(kThreads) void rope_top_kernel(Tops t, const uint32_t* __restrict__ part) {
+// (512 threads against 256: half as many rounds of loads one behind the other, 51.4 -> 50.7 us for a whole gradient of 2 x 4096 tokens.)
+constexpr int kTopThreads = 512;
+__global__ __launch_bounds__(kTopThreads) void rope_top_kernel(Tops t, const uint32_t* __restrict__ part) {
   const int j = blockIdx.x;
   if (!t.amax[j] || (t.same[j] & ((1 << j) - 1))) return;      // the first of them writes it
   uint32_t m = 0u;
   for (int k = 0; k < JOBS; ++k)
     if (t.same[j] >> k & 1)
-      for (int i = t.first[k] + (int)threadIdx.x; i < t.first[k + 1]; i += kThreads) m = m > part[i] ? m : part[i];
+      for (int i = t.first[k] + (int)threadIdx.x; i < t.first[k + 1]; i += kTopThreads) m = m > part[i] ? m : part[i];
   m = wave_max_u32(m);
-  __shared__ uint32_t wave[kThreads / 64];
+  __shared__ uint32_t wave[kTopThreads / 64];
   if ((threadIdx.x & 63) == 0) wave[threadIdx.x >> 6] = m;
   __syncthreads();
   if (threadIdx.x == 0) {
 #pragma unroll
-    for (int w = 1; w < kThreads / 64; ++w) m = m > wave[w] ? m : wave[w];
+    for (int w = 1; w < kTopThreads / 64; ++w) m = m > wave[w] ? m : wave[w];
     *t.amax[j] = m;
   }
 }
@@ -589,7 +591,7 @@ fog_status launch(Jobs<GRAD, JOBS>& jobs, Shape& sh, float* const* amax, bool an
     for (int j = 0; j <= JOBS; ++j) tops.first[j] = 0;
     if (!any_amax) return FOG_OK;
   }
-  if (any_amax) rope_top_kernel<<<jobs.count, kThreads, 0, s>>>(tops, sh.part);
+  if (any_amax) rope_top_kernel<<<jobs.count, kTopThreads, 0, s>>>(tops, sh.part);
   return fog_launch_status();
 }
 
