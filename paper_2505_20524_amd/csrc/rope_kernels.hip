@@ -2,8 +2,8 @@
 // layout to the heads that attention reads, in one pass; and the way back.
 //
 // Bound by memory: forward 2 bytes read and 1 written an element, backward 2 (4 with the norm) and 1 or 3.  Q and K of 2 x 4096 tokens, 32 and 8 heads of 128, and V:
-// a whole call of the forward 31 to 32.5 us (50 M elements, 4.9 TB/s), of which some 4 are the launch behind it that takes the maxima together, backward with the norm 50.5 us
-// (4.7 TB/s); 24 single tokens: 5 us and 2, less than a call takes on the host.  (That launch stands in for a zeroed word and an atomic from each of some thousand workgroups.  A call by one
+// a whole call of the forward 31 to 32.5 us (50 M elements, 4.9 TB/s), of which some 4 are the launch behind it that takes the maxima together, backward with the norm 49.5 us
+// (4.8 TB/s); 24 single tokens: 5 us and 2, less than a call takes on the host.  (That launch stands in for a zeroed word and an atomic from each of some thousand workgroups.  A call by one
 // workgroup, without it, was slower even at the smallest sizes: 13 us.)
 //
 // A token's vector of one head (D elements) belongs to LPR lanes, a wave takes 64 / LPR tokens and walks some heads of them, so that the cosines
@@ -176,10 +176,14 @@ FOG_DEVICE void turn(float (&a)[8], float (&b)[8], const float (&c)[8], const fl
   }
 }
 
-template <int LPR, bool INTER, bool GRAD, bool FULL, int N>
+// What the runs of a call look like: of any length; whole (FULL); half a stretch apart in stretches of whole thirty-twos (EVEN).  Kernels of their own: with EVEN a
+// choice in the FULL ones, 24 tokens took 6.5 us from a graph instead of 6.05, the gradient of 1 x 333 8.45 instead of 7.8, of 2 x 4096 50.6 instead of 49.3.
+enum { ANY, FULL_RUNS, EVEN_RUNS };
+template <int LPR, bool INTER, bool GRAD, int FORM, int N>
 __global__ __launch_bounds__(kThreads) void rope_kernel(Jobs<GRAD, N> jobs, Shape sh) {
   constexpr int VECTORS = kThreads / LPR;       // of a workgroup at a time
   constexpr int U = GRAD ? 2 : 1;               // heads in flight
+  constexpr bool FULL = FORM != ANY, EVEN = FORM == EVEN_RUNS;
   int j = 0;
   while (j + 1 < jobs.count && (int)blockIdx.x >= jobs.job[j + 1].first) ++j;
   const Job& job = jobs.job[j];
@@ -197,12 +201,10 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(Jobs<GRAD, N> jobs, Shap
   const bool on = lane < turners;
   // Where the lane's two runs begin and how long they are.  In the FULL form every run is of eight: the last one of a stretch that eight does not divide
   // reaches back over elements of the lane in front of it, which gives them the same values; only sums leave those out (skip).
-  // `even`: stretches of whole thirty-twos.  There a lane's runs lie half a stretch apart in either layout, so that each load of a wave covers whole lines, and
-  // two lanes store the codes of one's first and the other's second runs, sixteen bytes each (2 x 4096, 32/8 heads: 33.7 -> 31.6 us forward, 52.5 -> 51.6 backward).
+  // EVEN: a lane's runs lie half a stretch apart in either layout, so that each load of a wave covers whole lines, and two lanes store the codes of one's first and the other's second runs, sixteen bytes each (2 x 4096, 32/8 heads: 33.7 -> 31.6 us forward, 52.5 -> 51.6 backward).
   int offA, offB, nA, nB, skipA = 0, skipB = 0, first = 8 * lane;        // first, firstB: pairs whose cosines come first and from the fifth on
   const int rest = sh.D - 2 * half;
-  const bool even = FULL && (half & 15) == 0 && (rest & 31) == 0;
-  if (even) {
+  if (EVEN) {
     const int width = on ? half : rest >> 1, l = on ? lane : lane - turners;
     offA = (on ? 0 : 2 * half) + 8 * l;
     offB = offA + width;
@@ -226,8 +228,8 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(Jobs<GRAD, N> jobs, Shap
       if (rest >= 16) offA = sh.D - 16;
     }
   }
-  const int firstB = INTER && even ? first + (half >> 1) : first + 4;
-  if (FULL && !even && nA + nB > 0) {
+  const int firstB = INTER && EVEN ? first + (half >> 1) : first + 4;
+  if (FULL && !EVEN && nA + nB > 0) {
     if (on && !INTER) {
       skipA = skipB = 8 - nA;
     } else if (on || rest >= 16) {      // sixteen elements in a row, the last ones new
@@ -310,7 +312,7 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(Jobs<GRAD, N> jobs, Shap
             float p[8], r[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) { p[k] = a[k]; r[k] = e[k]; }
-            if (FULL && sh.overlap) skip16(p, r, skipA, skipB);
+            if (FORM == FULL_RUNS && sh.overlap) skip16(p, r, skipA, skipB);
             float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
@@ -348,7 +350,7 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(Jobs<GRAD, N> jobs, Shap
           }
           uint8_t* to = q + (h + u * slots) * job.q.head;
           const uint2 ca = with(convert8<false>(a, e5m2), na), ce = with(convert8<false>(e, e5m2), ne);
-          if (even) {
+          if (EVEN) {
             if (nA > 0) store_even(to, offA, offB, ca, ce, (lane & 1) != 0);
           } else {
             store_codes<FULL>(to + offA, ca, nA);
@@ -362,7 +364,7 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(Jobs<GRAD, N> jobs, Shap
             unpack8(xb[u], x1);
 #pragma unroll
             for (int k = 0; k < 8; ++k) { p[k] = x0[k]; r[k] = x1[k]; }
-            if (FULL && sh.overlap) skip16(p, r, skipA, skipB);
+            if (FORM == FULL_RUNS && sh.overlap) skip16(p, r, skipA, skipB);
 #pragma unroll
             for (int k = 0; k < 8; ++k) { xx = __builtin_fmaf(p[k], p[k], xx); xd = __builtin_fmaf(p[k], a[k], xd); }
 #pragma unroll
@@ -400,7 +402,7 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(Jobs<GRAD, N> jobs, Shap
             }
             uint8_t* to = q + (h + u * slots) * job.q.head;
             const uint2 ca = with(convert8<true>(a, e5m2), na), ce = with(convert8<true>(e, e5m2), ne);
-            if (even) {
+            if (EVEN) {
               if (nA > 0) store_even(to, offA, offB, ca, ce, (lane & 1) != 0);
             } else {
               store_codes<FULL>(to + offA, ca, nA);
@@ -534,6 +536,7 @@ fog_status launch(Jobs<GRAD, JOBS>& jobs, Shape& sh, float* const* amax, bool an
   bool full = sh.D >= 8 && (sh.rot == 0 || sh.rot >= 16), plain_jobs = false;
   for (int j = 0; j < jobs.count; ++j) plain_jobs |= !jobs.job[j].rotate;
   if (sh.rot < sh.D) full = full && sh.D - sh.rot >= 8;
+  const bool even = full && sh.rot % 32 == 0 && sh.D % 32 == 0;      // (then in jobs that are not turned, too)
   sh.overlap = sh.rot % 16 != 0 || (sh.D - sh.rot) % 16 != 0 || (plain_jobs && sh.D % 16 != 0);
   sh.tokens = (uint32_t)((int64_t)B * sh.S);
   sh.inv_cols = sh.D > 0 ? 1.0f / (float)sh.D : 0.0f;
@@ -574,12 +577,14 @@ fog_status launch(Jobs<GRAD, JOBS>& jobs, Shape& sh, float* const* amax, bool an
     }
 #define FOG_ROPE(L)                                                                                                        \
   do {                                                                                                                     \
-    if (!full)                   { if (inter) rope_kernel<L, true, GRAD, false, JOBS><<<next, kThreads, 0, s>>>(jobs, sh);  \
-                                   else rope_kernel<L, false, GRAD, false, JOBS><<<next, kThreads, 0, s>>>(jobs, sh); }     \
-    else if (jobs.count <= FEW)  { if (inter) rope_kernel<L, true, GRAD, true, FEW><<<next, kThreads, 0, s>>>(few, sh);     \
-                                   else rope_kernel<L, false, GRAD, true, FEW><<<next, kThreads, 0, s>>>(few, sh); }        \
-    else                         { if (inter) rope_kernel<L, true, GRAD, true, JOBS><<<next, kThreads, 0, s>>>(jobs, sh);   \
-                                   else rope_kernel<L, false, GRAD, true, JOBS><<<next, kThreads, 0, s>>>(jobs, sh); }      \
+    if (!full)                  FOG_ROPE_FORM(L, ANY, JOBS, jobs);                                                          \
+    else if (jobs.count <= FEW) { if (even) FOG_ROPE_FORM(L, EVEN_RUNS, FEW, few); else FOG_ROPE_FORM(L, FULL_RUNS, FEW, few); }       \
+    else                        { if (even) FOG_ROPE_FORM(L, EVEN_RUNS, JOBS, jobs); else FOG_ROPE_FORM(L, FULL_RUNS, JOBS, jobs); }   \
+  } while (0)
+#define FOG_ROPE_FORM(L, FORM, N, args)                                                                                     \
+  do {                                                                                                                      \
+    if (inter) rope_kernel<L, true, GRAD, FORM, N><<<next, kThreads, 0, s>>>(args, sh);                                     \
+    else rope_kernel<L, false, GRAD, FORM, N><<<next, kThreads, 0, s>>>(args, sh);                                          \
   } while (0)
     if (lpr == 4) FOG_ROPE(4);
     else if (lpr == 8) FOG_ROPE(8);
@@ -587,6 +592,7 @@ fog_status launch(Jobs<GRAD, JOBS>& jobs, Shape& sh, float* const* amax, bool an
     else if (lpr == 32) FOG_ROPE(32);
     else FOG_ROPE(64);
 #undef FOG_ROPE
+#undef FOG_ROPE_FORM
   } else {
     for (int j = 0; j <= JOBS; ++j) tops.first[j] = 0;
     if (!any_amax) return FOG_OK;
