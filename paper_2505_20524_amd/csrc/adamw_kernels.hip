@@ -1,6 +1,7 @@
 // The AdamW step over many tensors, states in binary32 or in FP8 with a scale for each 128 elements.
 //
-// Bound by memory: 28 bytes an element with bf16 weights, bf16 gradients, a binary32 master copy and binary32 states, 16 with FP8 states.  Two blocks at 8B scale, 487 M elements: 2300 to 2340 us (5.9 TB/s) and 1330 to 1410 us (5.7 TB/s); 49 tensors of 4.8 M: 27 us.
+// Bound by memory: 28 bytes an element with bf16 weights, bf16 gradients, a binary32 master copy and binary32 states, 16 with FP8 states.
+// Two blocks at 8B scale, 487 M elements: 2300 to 2340 us (5.9 TB/s) and 1330 to 1410 us (5.7 TB/s); 49 tensors of 4.8 M: 27 us.
 // As the gradients' norm and clipping: up to BATCH tensors a launch, cut into pieces of PIECE elements, a workgroup for each piece.
 //
 // Every operation on the moments is rounded once to binary32, in the order that the header states (no fused multiply-adds), so that a

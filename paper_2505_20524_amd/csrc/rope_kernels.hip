@@ -2,8 +2,8 @@
 // layout to the heads that attention reads, in one pass; and the way back.
 //
 // Bound by memory: forward 2 bytes read and 1 written an element, backward 2 (4 with the norm) and 1 or 3.  Q and K of 2 x 4096 tokens, 32 and 8 heads of 128, and V:
-// a whole call of the forward 31 to 32.5 us (50 M elements, 4.9 TB/s), of which some 4 are the launch behind it that takes the maxima together, backward with the norm 49.5 us
-// (4.8 TB/s); 24 single tokens: 5 us and 2, less than a call takes on the host.  (That launch stands in for a zeroed word and an atomic from each of some thousand workgroups.  A call by one
+// a whole call of the forward 31 to 32.5 us (50 M elements, 4.9 TB/s), of which some 4 are the launch behind it that takes the maxima together, backward with the
+// norm 49.5 us (4.8 TB/s); 24 single tokens: 5 us and 2, less than a call takes on the host.  (That launch stands in for a zeroed word and an atomic from each of some thousand workgroups.  A call by one
 // workgroup, without it, was slower even at the smallest sizes: 13 us.)
 //
 // A token's vector of one head (D elements) belongs to LPR lanes, a wave takes 64 / LPR tokens and walks some heads of them, so that the cosines
@@ -201,7 +201,8 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(Jobs<GRAD, N> jobs, Shap
   const bool on = lane < turners;
   // Where the lane's two runs begin and how long they are.  In the FULL form every run is of eight: the last one of a stretch that eight does not divide
   // reaches back over elements of the lane in front of it, which gives them the same values; only sums leave those out (skip).
-  // EVEN: a lane's runs lie half a stretch apart in either layout, so that each load of a wave covers whole lines, and two lanes store the codes of one's first and the other's second runs, sixteen bytes each (2 x 4096, 32/8 heads: 33.7 -> 31.6 us forward, 52.5 -> 51.6 backward).
+  // EVEN: a lane's runs lie half a stretch apart in either layout, so that each load of a wave covers whole lines, and two lanes
+  // store the codes of one's first and the other's second runs, sixteen bytes each (2 x 4096, 32/8 heads: 33.7 -> 31.6 us forward, 52.5 -> 51.6 backward).
   int offA, offB, nA, nB, skipA = 0, skipB = 0, first = 8 * lane;        // first, firstB: pairs whose cosines come first and from the fifth on
   const int rest = sh.D - 2 * half;
   if (EVEN) {
