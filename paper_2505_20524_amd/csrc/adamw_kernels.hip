@@ -112,7 +112,7 @@ FOG_DEVICE int block_exponent(uint32_t a) {
   return k < -126 ? -126 : k > 126 ? 126 : k;
 }
 
-// One of the two codes beside y, as a number: the places that the format drops, plus as many random bits, carry or do not.  Below the smallest
+// One of the two codes beside y (which is no NaN), as a number: the places that the format drops, plus as many random bits, carry or do not.  Below the smallest
 // normal number, where the format's steps stay equal, that number is added first: then the steps of the sum are those of the format.
 template <int FMT>
 FOG_DEVICE float round_by(float y, uint32_t r) {
@@ -198,7 +198,8 @@ FOG_DEVICE uint32_t encode4(const float (&x)[4], const uint32_t (&r)[4], uint32_
     const uint32_t a = __float_as_uint(x[i]) & 0x7FFFFFFFu;
     top = top > a ? top : a;
   }
-  const int k = block_exponent<FMT>(block_max(top));
+  top = block_max(top);
+  const int k = block_exponent<FMT>(top);
   byte = (uint32_t)(127 - k);
   const float by = __uint_as_float((uint32_t)(127 + k) << 23);
   float y[4];
@@ -206,6 +207,12 @@ FOG_DEVICE uint32_t encode4(const float (&x)[4], const uint32_t (&r)[4], uint32_
   for (int i = 0; i < 4; ++i) {
     y[i] = round_by<FMT>(x[i] * by, r[i]);
     if (FMT == FOG_E5M2) y[i] = x[i] > 0.0f ? fmaxf(y[i], 1.52587890625e-05f) : y[i];     // the smallest code above zero
+  }
+  // A NaN whose upper bits are set carries into the sign and would come out of round_by as a zero: NaNs take their own way, in blocks that hold one (a comparison
+  // for each block; beside every rounding it would be one for each element).
+  if (__builtin_expect(top > 0x7F800000u, 0)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = x[i] != x[i] ? x[i] : y[i];
   }
   return cvt4_fp8_finite<FMT>(y[0], y[1], y[2], y[3]);
 }

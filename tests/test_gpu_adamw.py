@@ -234,6 +234,25 @@ def test_a_moment_that_is_not_finite_shows_and_spoils_its_block_only(states):
         assert math.isnan(x.m[200].item()) and math.isnan(x.v[200].item())
 
 
+@pytest.mark.parametrize("pattern", [0x7FC0, 0x7FFF, 0xFFC0, 0xFFFF, 0x7F81])
+@pytest.mark.parametrize("seed", range(6))
+def test_a_nan_of_any_pattern_stays_one_in_fp8_states(pattern, seed):
+    """Whatever the NaN's other bits and the random ones: both states keep it, in this step and in the ones after."""
+    x, y = Tensor(gen(15), 1000, fog.STATES_FP8), Tensor(gen(15), 1000, fog.STATES_FP8)
+    at = [3, 77, 400, 999]                                   # two in one block, one that is alone, one in the last, ragged block
+    x.g.view(torch.int16)[at] = pattern - (1 << 16 if pattern >= 1 << 15 else 0)
+    for t in range(5, 8):
+        for z in (x, y):
+            fog.adamw(fog.make_adamw_jobs([z.item()]), 1e-2, t, seed=seed)
+        for state, fmt in ((x.m, fp8.E4M3), (x.v, fp8.E5M2)):
+            assert np.isnan(fp8.decode(host(state), fmt)[at]).all(), (t, fmt)
+        assert bool(torch.isnan(x.master[at]).all()) and bool(torch.isnan(x.p[at]).all())
+        x.g.copy_(y.g)                                       # from here on finite gradients
+    for name in ("p", "m", "v"):
+        a, b = x.item()[name], y.item()[name]
+        assert torch.equal(a[128:384], b[128:384]) and torch.equal(a[512:896], b[512:896]), name
+
+
 @pytest.mark.parametrize("states", STATES)
 def test_rate_and_step_in_device_memory(states):
     """The numbers of the host and those of the device give the same bits."""
