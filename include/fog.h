@@ -418,7 +418,8 @@ size_t fog_postnorm_residual_grad_workspace(int64_t rows, int64_t cols);
  *   x_bf16, dy_bf16 : [rows, cols] bfloat16, leading dimensions.   scale : one float; may be NULL without q.
  *   dx_bf16, q : either may be NULL; [rows, cols], leading dimensions.  dx may lie in the place of x or dy (the same address and leading dimension); otherwise no
  *             result may meet an input or the other result.
- *   dalpha : NULL, or two floats (xIELU) or one (tanh), overwritten (accumulate == 0) or added to; joined in binary64 in a fixed order, the same bits on every run.
+ *   dalpha : NULL, or two floats (xIELU) or one (tanh), overwritten (accumulate == 0) or added to; joined in binary64 in a fixed order, the same bits on every run.  What is
+ *             not finite in x or dy shows in the sum that the element belongs to, and in that one alone.
  *   amax_out : NULL or one float, overwritten.
  *   workspace : fog_act_grad_workspace() bytes (40 KB), 8-byte aligned, where dalpha or amax_out is given; contents on entry do not matter.  Calls that may overlap in
  *             time need a workspace each.

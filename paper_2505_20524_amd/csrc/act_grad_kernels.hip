@@ -53,9 +53,10 @@ FOG_DEVICE float slope(float x, float d, Entry v, float p0, float p1, float& t0,
   if (ACT == ACT_XIELU) {
     const float e = __builtin_elementwise_maximum(v.f, x), curve = __builtin_elementwise_maximum(v.g, -1.0f - x);
     const bool up = x > 0.0f;
-    const float xu = up ? x : 0.0f, dn = up ? 0.0f : d;
-    t0 = __builtin_fmaf(d * xu, xu, t0);
-    t1 = __builtin_fmaf(dn, curve, t1);
+    // (The sums are chosen, not their terms: a zero in the place of a factor makes a NaN beside an infinity in the other.)
+    const float u0 = __builtin_fmaf(d * x, x, t0), u1 = __builtin_fmaf(d, curve, t1);
+    t0 = up ? u0 : t0;
+    t1 = up ? t1 : u1;
     return up ? __builtin_fmaf(p0 + p0, x, 0.5f) : __builtin_fmaf(p1, e, 0.5f);
   }
   if (ACT == ACT_GELU) {

@@ -385,6 +385,26 @@ def test_activation_of_numbers_that_are_not_finite(act, alpha, rows):
     assert (a.q[1, 5].item() & 0x7F) == 0x7F and (a.q[2, 9].item() & 0x7F) == 0x7F
 
 
+INF, NAN = float("inf"), float("nan")
+
+
+@pytest.mark.parametrize("rows,cols,ld", [(3, 8192, 0), (900, 8192, 0), (1100, 4099, 1)])          # computed, from a table, and rows that no table takes
+@pytest.mark.parametrize("x,d,which", [
+    (INF, 1e-3, 0), (1.5, INF, 0), (1.5, -INF, 0), (1.5, NAN, 0), (INF, 0.0, 0), (INF, INF, 0), (3e38, INF, 0),
+    (-INF, 1e-3, 1), (-1.5, INF, 1), (-1.5, -INF, 1), (-1.5, NAN, 1), (-INF, 0.0, 1), (0.0, INF, 1), (-0.0, NAN, 1), (-3e38, INF, 1), (NAN, 1e-3, 1)])
+def test_what_is_not_finite_shows_in_its_own_sum(rows, cols, ld, x, d, which):
+    """Numbers above zero belong to the first of the xIELU's sums, the others to the second: the one that they do not belong to is what it is without them."""
+    a = Act(29, "xielu", (0.8, 0.6), rows, cols, ld)
+    x64, d64 = h64(a.x), h64(a.d)
+    for r, c in ((0, 0), (1, 513), (2, cols - 1), (rows - 1, 7)):
+        a.x[r, c], a.d[r, c], x64[r, c], d64[r, c] = x, d, 0.0, 0.0
+    a.run()
+    assert not math.isfinite(a.dalpha[which].item())
+    g = grads.xielu(x64, *[float(np.float32(v)) for v in a.alpha])[2][1 - which]
+    terms = d64 * g
+    assert abs(a.dalpha[1 - which].item() - terms.sum()) <= 1.01 * 40 * U * np.abs(terms).sum() + 2 * U * abs(terms.sum()) + 2.0 ** -120
+
+
 @pytest.mark.parametrize("act,alpha", [ACTS[0], ACTS[2], ACTS[3]])
 @pytest.mark.parametrize("rows,cols", [(0, 300), (5, 0)])
 def test_activation_of_nothing(act, alpha, rows, cols):
