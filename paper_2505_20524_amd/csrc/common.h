@@ -166,6 +166,16 @@ FOG_DEVICE void st_any_nt16(void* p, uint4 v) {
   u32x4 w = {v.x, v.y, v.z, v.w};
   __builtin_nontemporal_store(w, reinterpret_cast<u32x4_any*>(p));
 }
+// Codes, which may begin at any byte.
+typedef u32x4 __attribute__((aligned(1))) u32x4_byte;
+FOG_DEVICE void st_any16(uint8_t* p, uint4 v) {
+  u32x4 w = {v.x, v.y, v.z, v.w};
+  *reinterpret_cast<u32x4_byte*>(p) = w;
+}
+FOG_DEVICE void st_any_nt16(uint8_t* p, uint4 v) {
+  u32x4 w = {v.x, v.y, v.z, v.w};
+  __builtin_nontemporal_store(w, reinterpret_cast<u32x4_byte*>(p));
+}
 // Eight 16-bit elements from p on of which n are there; zeros behind them.
 FOG_DEVICE uint4 ld_upto8(const uint16_t* p, int n) {
   uint32_t w[4] = {0, 0, 0, 0};
