@@ -602,7 +602,8 @@ fog_status fog_grad_clip(const fog_grad_job* jobs, int count, const double* sums
  * The AdamW step (decoupled weight decay) over many tensors:
  *     gc = g c,   m = beta1 m + (1 - beta1) gc,   v = beta2 v + (1 - beta2) gc gc,
  *     p  = p (1 - lr weight_decay) - m rate / (sqrt(v) root + eps),     rate = lr / (1 - beta1^t),  root = 1 / sqrt(1 - beta2^t),
- * binary32, every operation rounded once, products of three from the left (m and v are the same bits in any evaluation that does so).
+ * binary32, every operation rounded once, products of three from the left (m, v and with binary32 states p are the same bits in any evaluation that does so).  FP8 states
+ * with an eps of 2^-38 and more: root and quotient are off by up to a unit in the last place each, and a v below the smallest normal number counts as 0 in the root.
  *   c : without sumsq 1; else the factor of fog_grad_clip for *sumsq and max_norm, so that the gradients need not be clipped before.  A sum
  *       that is not finite leaves the whole step out: nothing is written.
  *   states : FOG_STATES_F32  m, v are n floats each.

@@ -65,7 +65,6 @@ struct AdamStep {
   uint64_t seed;
   Common common;
   float beta1, beta1c, beta2, beta2c, eps, max_norm;     // c: 1 - beta, from binary64
-  bool plain_eps;                                        // eps is 2^-38 or more
 };
 static_assert(sizeof(AdamBatch) + sizeof(AdamStep) <= 4096, "arguments of a launch");
 
@@ -251,7 +250,7 @@ FOG_DEVICE void load_four(const Tensor& t, int64_t i, int n, Four& f) {
     load4(reinterpret_cast<const float*>(t.v) + i, n, f.v);
   }
 }
-template <bool FP8, bool FULL, bool PLAIN>
+template <bool FP8, bool FULL, bool NEAR>
 FOG_DEVICE void step_four(const Tensor& t, const AdamStep& s, int64_t i, uint32_t at, int n, Four& f) {
   if (FULL) n = 4;
 #pragma unroll
@@ -259,13 +258,12 @@ FOG_DEVICE void step_four(const Tensor& t, const AdamStep& s, int64_t i, uint32_
     const float gc = f.g[e] * t.c;
     f.m[e] = f.m[e] * s.beta1 + gc * s.beta1c;
     f.v[e] = f.v[e] * s.beta2 + gc * gc * s.beta2c;
-    // Root and quotient by the hardware's instructions, a unit in the last place each.  A second moment below the smallest normal number counts as 0: beside
-    // an eps of 2^-38 and more its root, below 2^-63, does not show.  A smaller eps takes the correctly rounded forms, 25 instructions more, which the compiler
-    // evaluates beside the others where the eps decides in the kernel.  FP8 states have kernels for either (two blocks at 8B scale 1450 -> 1405 us); binary32 states,
-    // whose arithmetic hides behind memory, are a little faster with both (2335 us, not 2380).
-    const bool plain = PLAIN || s.plain_eps;
-    const float d = plain ? __builtin_amdgcn_sqrtf(f.v[e]) * t.root + s.eps : __builtin_sqrtf(f.v[e]) * t.root + s.eps;
-    const float u = plain ? f.m[e] * t.rate * __builtin_amdgcn_rcpf(d) : f.m[e] * t.rate / d;
+    // Root and quotient are rounded correctly, at 25 instructions more than the hardware's own, which are off by up to a unit in the last place each.  With binary32
+    // states these hide behind memory (two blocks at 8B scale 2310 us a step either way).  With FP8 states they do not (1450 us, not 1340), and a unit of 2^-23 is
+    // nothing beside moments in steps of 2^-3 and 2^-2: NEAR takes the hardware's there.  A second moment below the smallest normal number then counts as 0: beside
+    // an eps of 2^-38 and more its root, below 2^-63, does not show; FP8 states with a smaller eps have the kernel without NEAR.
+    const float u = NEAR ? f.m[e] * t.rate * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(f.v[e]) * t.root + s.eps)
+                         : f.m[e] * t.rate / (__builtin_sqrtf(f.v[e]) * t.root + s.eps);
     f.p[e] = f.p[e] * t.keep - u;
   }
   uint32_t r[4];
@@ -304,8 +302,8 @@ FOG_DEVICE void step_four(const Tensor& t, const AdamStep& s, int64_t i, uint32_
   }
 }
 
-// U: fours in flight.
-template <bool FP8, int PIECE, int U, bool PLAIN>
+// U: fours in flight.  NEAR: root and quotient by the hardware's instructions.
+template <bool FP8, int PIECE, int U, bool NEAR>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(AdamBatch b, AdamStep s) {
   Tensor t;
   t.c = 1.0f;
@@ -343,7 +341,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(AdamBatch b, AdamStep s
 #pragma unroll
         for (int u = 0; u < U; ++u) load_four<FP8, true>(t, at + i0 + 4 * kThreads * u, 4, f[u]);
 #pragma unroll
-        for (int u = 0; u < U; ++u) step_four<FP8, true, PLAIN>(t, s, at + i0 + 4 * kThreads * u, t.low + (uint32_t)(i0 + 4 * kThreads * u), 4, f[u]);
+        for (int u = 0; u < U; ++u) step_four<FP8, true, NEAR>(t, s, at + i0 + 4 * kThreads * u, t.low + (uint32_t)(i0 + 4 * kThreads * u), 4, f[u]);
       }
     } else {
       const int whole = (n + 127) & ~127;                // whole blocks: their lanes stay together
@@ -351,7 +349,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(AdamBatch b, AdamStep s
       for (int i0 = 4 * (int)threadIdx.x; i0 < whole; i0 += 4 * kThreads) {
         Four f;
         load_four<FP8, false>(t, at + i0, n - i0, f);
-        step_four<FP8, false, PLAIN>(t, s, at + i0, t.low + (uint32_t)i0, n - i0, f);
+        step_four<FP8, false, NEAR>(t, s, at + i0, t.low + (uint32_t)i0, n - i0, f);
       }
     }
   }
@@ -405,7 +403,6 @@ extern "C" fog_status fog_adamw(const fog_adamw_job* jobs, int count, fog_states
   s.lr_dev = lr_dev; s.step_dev = step_dev; s.sumsq = sumsq; s.step = step; s.seed = seed;
   s.beta1 = (float)beta1; s.beta1c = (float)(1.0 - beta1); s.beta2 = (float)beta2; s.beta2c = (float)(1.0 - beta2);
   s.eps = (float)eps; s.max_norm = max_norm;
-  s.plain_eps = eps >= 0x1p-38;
   s.common = {0.0f, 0.0f, 0u};
   if (!lr_dev && !step_dev)
     s.common = {(float)(lr / -std::expm1((double)step * s.log_beta1)), (float)(1.0 / std::sqrt(-std::expm1((double)step * s.log_beta2))), step_key(seed, (uint64_t)step)};
@@ -417,7 +414,7 @@ extern "C" fog_status fog_adamw(const fog_adamw_job* jobs, int count, fog_states
     if (b.count == 0) return;
     const int groups = b.pieces < GROUPS ? b.pieces : GROUPS;
     hipStream_t st = (hipStream_t)stream;
-    if (fp8 && s.plain_eps)    adamw_kernel<true, FP8_PIECE, 4, true><<<groups, kThreads, 0, st>>>(b, s);
+    if (fp8 && eps >= 0x1p-38) adamw_kernel<true, FP8_PIECE, 4, true><<<groups, kThreads, 0, st>>>(b, s);
     else if (fp8)              adamw_kernel<true, FP8_PIECE, 4, false><<<groups, kThreads, 0, st>>>(b, s);
     else if (b.pieces <= MANY) adamw_kernel<false, F32_PIECE, 2, false><<<groups, kThreads, 0, st>>>(b, s);
     else                       adamw_kernel<false, F32_PIECE, 1, false><<<groups, kThreads, ROOM, st>>>(b, s);

@@ -264,6 +264,32 @@ def test_rate_and_step_in_device_memory(states):
         assert torch.equal(bits(a), bits(b)), k
 
 
+def parameters(p, m, v, lr, t, beta1, beta2, eps, decay):
+    """The parameters after the step in binary32, each operation rounded once: p keep - m rate / (sqrt(v) root + eps)."""
+    f = np.float32
+    keep, rate = f(1 - lr * float(f(decay))), f(lr / -math.expm1(t * math.log(beta1)))
+    root = f(1 / math.sqrt(-math.expm1(t * math.log(beta2))))
+    p, m, v = (np.asarray(a).astype(f) for a in (p, m, v))
+    return p * keep - m * rate / (np.sqrt(v) * root + f(eps))
+
+
+@pytest.mark.parametrize("states,eps", [(fog.STATES_F32, e) for e in (1e-4, 1e-8, 2.0 ** -39, 1e-30)] + [(fog.STATES_FP8, e) for e in (2.0 ** -39, 1e-30)])
+@pytest.mark.parametrize("p,master", [(B, True), (F, False)])
+def test_every_operation_on_the_parameters_is_rounded_once(states, eps, p, master):
+    """Bit for bit: root, quotient and all else as binary32 arithmetic gives them, over many binades of the second moment."""
+    x = Tensor(gen(17), 20000, states, p=p, g=F, master=master)
+    x.g.mul_(torch.exp2(-(torch.arange(20000, device="cuda") // 128 % 50).float()))
+    if states == fog.STATES_F32:
+        x.m.mul_(torch.exp2(-(torch.arange(20000, device="cuda") // 128 % 50).float()))
+        x.v.mul_(torch.exp2(-2 * (torch.arange(20000, device="cuda") // 128 % 50).float()))
+    before, g, m, v = x.values()
+    fog.adamw(fog.make_adamw_jobs([x.item()]), 1e-2, 9, eps=eps, seed=3)
+    m, v = adamw.moments(m, v, g, np.float32(1), 0.9, 0.95)
+    want = parameters(before, m, v, 1e-2, 9, 0.9, 0.95, eps, x.decay)
+    got = (x.master if master else x.p).cpu().numpy()
+    assert np.array_equal(got, want), (int((got != want).sum()), np.flatnonzero(got != want)[:5])
+
+
 @pytest.mark.parametrize("states", STATES)
 def test_steps_in_a_graph(states):
     """Captured once with its rate and step in device memory, replayed over several steps with eager work between: the eager steps' bits."""
