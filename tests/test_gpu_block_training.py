@@ -226,6 +226,28 @@ def test_gradients_of_the_whole_block():
     assert off(b.dalpha, dalpha) < 1.0
 
 
+@pytest.mark.parametrize("which", [0, 1])
+def test_gradient_of_an_alpha_whose_terms_add_up(which):
+    """The gradient of the result along its own derivative after one alpha, so that the terms of that alpha's sum do not cancel: the sum is the derivative's square norm, and
+    off by no more than a gradient through as many casts is by its norm.  (On gradients of either sign the sum's own size is no measure.)"""
+    b = Block(6)
+    h, alpha, ends = 1e-4, b.alpha, []
+    for sign in (1, -1):
+        b.alpha = tuple(a + sign * h * (i == which) for i, a in enumerate(alpha))
+        ends.append(reference(b)[0])
+    b.alpha = alpha
+    along = (ends[0] - ends[1]) / (2 * h)
+    b.G.copy_(along * (1e-3 / along.square().mean().sqrt()))
+    b.passes()
+    b.scales()
+    b.passes()
+    torch.cuda.synchronize()
+    want = float(reference(b)[4][which])
+    assert want > 0.99 * 1e-3 / float(along.square().mean().sqrt()) * float(along.square().sum())          # (the derivative: up to its difference and G's rounding)
+    # as above: 9 casts forward, and on the way back to the activation the second norm's gradient to E5M2 and the weight (one more to E4M3 to spare): held to twice that
+    assert abs(b.dalpha[which].item() - want) < 2 * math.sqrt(11 * 0.026 ** 2 + 0.052 ** 2) * want
+
+
 def test_every_stage_between_the_products():
     """Each operator on the tensors as they occur, against the oracle."""
     b = Block(2)
