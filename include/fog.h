@@ -24,6 +24,9 @@
  *   - Errors are returned as fog_status; nothing is thrown and nothing aborts.
  *     Argument errors are detected on the host before anything is launched, so a
  *     failing call has no effect on device memory.
+ *   - What a call writes, workspaces included, lies apart from all else that it reads or writes, unless the call allows
+ *     a result in the place of an input.  Where a call's errors name overlaps, its matrices and tensors are looked at;
+ *     single numbers (abs-max, scales, sums, steps) and workspaces are not, in any call.
  *   - FP8 codes are OCP E4M3 / E5M2 bytes.  The casts (fog_quantize and its variants, the fused
  *     producers) give a NaN input the NaN code 0x7F with the input's sign and saturate infinities; the
  *     abs-max of a tensor that holds a NaN is NaN (and its scale therefore 1).  The GEMM and attention
@@ -248,7 +251,9 @@ fog_status fog_rmsnorm_quantize(const void* x_bf16, int64_t rows, int64_t cols, 
  *     z = gain x / rms(x)                     (as fog_rmsnorm_quantize; gain == 0: z = x)
  *     y_a = z_a c_i - z_b s_i,  y_b = z_b c_i + z_a s_i      for the pairs i of the first `rot` elements, the others stay:
  *         FOG_ROPE_HALF         (a, b) = (i, i + rot / 2)          FOG_ROPE_INTERLEAVED  (a, b) = (2i, 2i + 1)
- *     q = sat_rne_fmt( fl32( y * scale ) ),   amax = max |y| over the job      (binary32; y is not stored)
+ *     q = sat_rne_fmt( fl32( y * scale ) ),   amax = max |y| over the job      (binary32)
+ * y is never stored, and under a norm never formed: gain / rms(x) and the scale follow the turn as one factor.  Codes agree with a float64 evaluation except where scale * y
+ * lies within about 2^-19 (without a norm 2^-21; what is not turned: nowhere) of its terms' size of a rounding boundary.
  *   jobs : HOST array of `count` (0 .. FOG_ROPE_JOBS_MAX) tensors of B sequences of S tokens, typically Q, K and V; read before the call returns.
  *     x, q  : element (b, s, h, d) at p + b batch + s token + h head + d, strides in elements, any that are not negative (and under which no
  *             vector of q meets another): ranges of the projection's columns, [B, heads, S, D], rows of a cache.   x bfloat16, q codes.
@@ -265,8 +270,8 @@ fog_status fog_rmsnorm_quantize(const void* x_bf16, int64_t rows, int64_t cols, 
  *
  * fog_rope_grad is the way back, per token and head with dy the gradient of y:
  *     dz = the transposed turn of dy;     dx = gain / rms(x) (dz - x (x . dz) / (x . x))      (gain == 0: dx = dz; x is not looked at; a vector of zeros: 0)
- * rounded once to bfloat16.  dx receives it, q its cast (of the ROUNDED value, as fog_quantize of a stored dx would give); either may have p == NULL.
- * amax = max |dx|, the rounded.  Padding has dx = 0 where it is turned.  Jobs that write ranges of one matrix (the gradient of the projection's result, one operand of
+ * in binary32, within about 2^-18 of its terms' size, and rounded once to bfloat16.  dx receives it, q its cast (of the ROUNDED value, as fog_quantize of a stored dx
+ * would give); either may have p == NULL.  amax = max |dx|, the rounded.  Padding has dx = 0 where it is turned.  Jobs that write ranges of one matrix (the gradient of the projection's result, one operand of
  * its products) name one scale and one amax.
  * An input may repeat (strides of 0); the gradient of each of its appearances is one of its own.  Jobs without positions and norm change the layout alone, with the
  * cast: attention's result into the next projection's operand, that projection's gradient into attention's.
@@ -395,8 +400,8 @@ fog_status fog_postnorm_residual_quantize(const void* x_bf16, int64_t ldx, const
  *     dgamma = sum over the rows of G y / rms(y),        amax_out = max |dy|   (dy, q, amax_out: of the rounded value)
  *   dres_bf16, dbranch_bf16, y_bf16 : [rows, cols] bfloat16, leading dimensions ld_*.   gamma : [cols] floats.   scale : one float; may be NULL without q.
  *   dstream_bf16, dy_bf16, q : each may be NULL; [rows, cols], leading dimensions.  One may lie in the place of an input of its type (the same address and leading
- *             dimension); otherwise no result may meet an input or another result.
- *   dgamma : NULL, or [cols] floats, overwritten (accumulate == 0) or added to.  Sums in a fixed order, the same bits on every run.
+ *             dimension); otherwise no result, dgamma among them, may meet an input or another result.
+ *   dgamma : NULL, or [cols] floats, overwritten (accumulate == 0) or added to.  Sums in binary32 in a fixed order, the same bits on every run.
  *   amax_out : NULL or one float, overwritten.
  *   workspace : fog_postnorm_residual_grad_workspace(rows, cols) bytes, 4-byte aligned, where dgamma or amax_out is given; contents on entry do not matter.  Calls
  *             that may overlap in time need a workspace each.
@@ -416,10 +421,10 @@ size_t fog_postnorm_residual_grad_workspace(int64_t rows, int64_t cols);
  *   GeLU:   f' = Phi(x) + x phi(x), phi the normal density
  *   tanh:   f' = alpha (1 - tanh^2(alpha x));                                         dalpha = sum of dy x (1 - tanh^2(alpha x))
  *   x_bf16, dy_bf16 : [rows, cols] bfloat16, leading dimensions.   scale : one float; may be NULL without q.
- *   dx_bf16, q : either may be NULL; [rows, cols], leading dimensions.  dx may lie in the place of x or dy (the same address and leading dimension); otherwise no
- *             result may meet an input or the other result.
- *   dalpha : NULL, or two floats (xIELU) or one (tanh), overwritten (accumulate == 0) or added to; joined in binary64 in a fixed order, the same bits on every run.  What is
- *             not finite in x or dy shows in the sum that the element belongs to, and in that one alone.
+ *   dx_bf16, q : either may be NULL; [rows, cols], leading dimensions.  dx may lie in the place of x or dy (the same address and leading dimension); otherwise neither
+ *             of the two may meet an input or the other.
+ *   dalpha : NULL, or two floats (xIELU) or one (tanh), overwritten (accumulate == 0) or added to; eight terms at a time in binary32, these joined in binary64, in a fixed
+ *             order: the same bits on every run.  What is not finite in x or dy shows in the sum that the element belongs to, and in that one alone.
  *   amax_out : NULL or one float, overwritten.
  *   workspace : fog_act_grad_workspace() bytes (40 KB), 8-byte aligned, where dalpha or amax_out is given; contents on entry do not matter.  Calls that may overlap in
  *             time need a workspace each.

@@ -1,7 +1,7 @@
 // The gradients of the activations, on the way back between the two products of the feed-forward half (tanh: in front of attention): dx = dy f'(x), its cast for
 // the products, and the sums that the activation's own parameters get.
 //
-// Bound by memory: 4 bytes read and 1 (3 with dx) written an element.  xIELU of 8192 x 14336: a call takes 113 us (5.2 TB/s; 104 without the function itself),
+// Bound by memory: 4 bytes read and 1 (3 with dx) written an element.  xIELU of 8192 x 14336: a call takes 112 us (5.2 TB/s; 104 without the function itself),
 // 5 of them the launch that joins the workgroups' sums in a fixed order; GeLU of 333 x 2736: 5 us and 2, less than a call takes on the host.
 #include <cfloat>
 
@@ -242,8 +242,10 @@ __global__ __launch_bounds__(kThreads) void act_grad_kernel(Args a) {
 // Rows of whole sixteens, or one row of any length (FLAT): a wave takes 1024 elements at a time, in two halves so that each of its loads covers whole lines, and
 // looks the entries up; two lanes store the codes of one's first and the other's second eight, sixteen bytes each.  Whole calls of xIELU, 8192 x 14336, from a graph:
 // 123 us with sixteen elements in a row a lane and the next ones' loads under way, 114 like this (110 to 115 with three workgroups of 512 threads a compute unit and
-// spilled registers, 115 with the loads under way); 104 without the function: the rest is memory and two launches.  One workgroup a compute unit fills its table once.
-// Against entries that are computed in chunks of eight, 8192 x 14336 / 4096 x 4096 (an earlier form of this kernel): xIELU 142 -> 119 / 28.7 -> 23.4 us, GeLU 123 -> 115.
+// spilled registers, 115 with the loads under way), 112 with the sums chosen instead of their terms; 104 without the function: the rest is memory and two launches.
+// One workgroup a compute unit fills its table once.
+// Against the other kernel, 8192 x 14336 / 4096 x 4096 / 1024 x 4096: xIELU 138 -> 112 / 29.3 -> 20.8 / 11.9 -> 10.6 us, GeLU 140 -> 107 / 28.8 -> 19.1 / 11.1 -> 9.2, tanh
+// 136 -> 107 / 25.6 -> 19.7 / 10.9 -> 10.0.
 FOG_DEVICE uint32_t beside(uint32_t v) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xF, 0xF, false); }
 template <int ACT, int FMT, bool FLAT>
 __global__ __launch_bounds__(kTableThreads) void act_grad_table_kernel(Args a) {

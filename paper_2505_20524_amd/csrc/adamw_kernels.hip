@@ -1,7 +1,7 @@
 // The AdamW step over many tensors, states in binary32 or in FP8 with a scale for each 128 elements.
 //
 // Bound by memory: 28 bytes an element with bf16 weights, bf16 gradients, a binary32 master copy and binary32 states, 16 with FP8 states.
-// Two blocks at 8B scale, 487 M elements: 2300 to 2340 us (5.9 TB/s) and 1330 to 1410 us (5.7 TB/s); 49 tensors of 4.8 M: 27 us.
+// Two blocks at 8B scale, 487 M elements: 2300 to 2360 us (5.9 TB/s) and 1320 to 1400 us (5.7 TB/s); 49 tensors of 4.8 M: 27 us.
 // As the gradients' norm and clipping: up to BATCH tensors a launch, cut into pieces of PIECE elements, a workgroup for each piece.
 //
 // Every operation on the moments is rounded once to binary32, in the order that the header states (no fused multiply-adds), so that a
@@ -27,8 +27,8 @@ constexpr int BATCH = 50;                // descriptions that fit a launch's arg
 // Elements of a piece, a multiple of a scale's 128.
 constexpr int F32_PIECE = 2048, FP8_PIECE = 4096;
 // Large launches of binary32 states (seven streams an element) are faster with fewer workgroups in flight: beyond MANY pieces (32 M elements) each asks for so much
-// LDS that five fit a compute unit, and keeps four elements a thread in flight instead of eight.  us, without -> with: 4.8 M elements 28.3 -> 30.3, 33.6 M 160.9 ->
-// 160.7, 101 M 487 -> 481, 403 M 2028 -> 1894.  (Pieces of 4096 and 8192 elements: 403 M 2019 and 2105.  FP8 states, whose arithmetic wants the waves: 1136 with
+// LDS that five fit a compute unit, and keeps four elements a thread in flight instead of eight.  us, without -> with: 4.8 M elements 26.5 -> 28.3, 33.6 M 163.7 ->
+// 160.6, 101 M 494 -> 475, 403 M 1989 -> 1885.  (Pieces of 4096 and 8192 elements, without: 403 M 2019 and 2105.  FP8 states, whose arithmetic wants the waves: 1136 with
 // pieces of 4096 and sixteen elements in flight, 1167 with 2048 and eight, 1438 with fewer workgroups.)
 constexpr int MANY = 16384;
 constexpr size_t ROOM = 32 << 10;

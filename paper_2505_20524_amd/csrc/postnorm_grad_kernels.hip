@@ -4,7 +4,7 @@
 // Bound by memory: 6 bytes read and 3 (5 with dy) written an element.  A row belongs to W waves that keep it in registers between the sums over
 // it and its results, so that every tensor is read once.  A lane keeps its columns over all rows of its wave, so that the gains' gradient is summed in registers;
 // a workgroup's waves join in LDS, the workgroups' sums in a second launch, in a fixed order: the same bits on every run.
-// 8192 x 4096: 55 us (5.4 TB/s) and 6 us for the second launch; 777 x 2064: 10 us and 4.
+// 8192 x 4096: 55 us (5.4 TB/s) and 5 us for the second launch; 777 x 2064: 9 to 9.5 us and 4.5.
 #include <cfloat>
 
 #include "common.h"

@@ -2,7 +2,7 @@
 // layout to the heads that attention reads, in one pass; and the way back.
 //
 // Bound by memory: forward 2 bytes read and 1 written an element, backward 2 (4 with the norm) and 1 or 3.  Q and K of 2 x 4096 tokens, 32 and 8 heads of 128, and V:
-// a whole call of the forward 31 to 32.5 us (50 M elements, 4.9 TB/s), of which some 4 are the launch behind it that takes the maxima together, backward with the
+// a whole call of the forward 31.5 us (50 M elements, 4.9 TB/s), of which some 4 are the launch behind it that takes the maxima together, backward with the
 // norm 49.5 us (4.8 TB/s); 24 single tokens: 5 us and 2, less than a call takes on the host.  (That launch stands in for a zeroed word and an atomic from each of some thousand workgroups.  A call by one
 // workgroup, without it, was slower even at the smallest sizes: 13 us.)
 //
@@ -112,7 +112,7 @@ FOG_DEVICE void store_codes(uint8_t* p, uint2 w, int n) {
   }
 }
 // Codes of two runs whose next ones the neighbour lane has: the even lane stores both first runs, the odd one both second runs.  Written through: without, the next
-// launch waits for what the caches still have to write back (31.6 -> 30.3 us forward, 51.6 -> 50.3 backward); past the caches 33.5 us, and 39 in pieces of eight.
+// launch waits for what the caches still have to write back (31.7 -> 30.6 us forward, 51.7 -> 50.5 backward); past the caches 33.5 us, and 39 in pieces of eight.
 FOG_DEVICE uint32_t beside(uint32_t v) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xF, 0xF, false); }
 FOG_DEVICE void store_even(uint8_t* to, int offA, int offB, uint2 a, uint2 e, bool odd) {
   const uint32_t x = beside(odd ? a.x : e.x), y = beside(odd ? a.y : e.y);
@@ -455,7 +455,7 @@ __global__ __launch_bounds__(kTopThreads) void rope_top_kernel(Tops t, const uin
 }
 
 // cos and sin of every position and pair from binary64 angles: far positions turn 10^5 times and more.  A thread keeps its pair's frequency for
-// sixteen positions and more.
+// sixteen positions and more.  Bound by the binary64 functions: 4096 x 128 7 us, 131072 x 128 35 (10 for its stores alone), once for a program.
 constexpr int TABLE_ROWS = 64;
 __global__ __launch_bounds__(kThreads) void rope_table_kernel(fog_rope_scaling sc, int64_t first, int64_t positions, int half, float* __restrict__ table) {
   for (int i = threadIdx.x & 63; i < half; i += 64) {
